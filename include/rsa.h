@@ -231,6 +231,116 @@ int rsa_sparse_attn_rectified_static(const rsa_shape* shape, const void* Q, cons
                                      const uint32_t* Mc_bits, const float* Vp, int flags,
                                      void* O, float* lse, void* stream);
 
+/*
+ * The 8-bit key/value cache: keys and values of earlier frames or tokens, kept for queries that arrive
+ * later (frame by frame, token by token). Four calls work on it:
+ *
+ *   rsa_cache_write    new keys and values into their pages
+ *   rsa_cache_read     a range of tokens back in bf16
+ *   rsa_cache_select   which blocks a group of query tokens reads, by a cheap score
+ *   rsa_cache_attn     attention of new queries over all blocks, or over those lists
+ *
+ * A page holds one block of `block` tokens of all key/value heads; `table` says which page each block of
+ * a sequence is. Entries that are no page (negative, or >= pages) hold no tokens: what is written there
+ * is dropped, attention and selection pass over them, reading leaves those rows as they were. A page may stand in several rows of the
+ * table (a shared prefix) as long as no write reaches it through two of them at once.
+ *
+ * Codes are e4m3 with one power-of-two scale for each (page, key/value head) of K and of V:
+ *   value = code * 2^e,  e the least >= -126 with max |value| <= 448 * 2^e,  rounded to nearest even.
+ * A token that joins a block that was begun earlier can only raise e; the older codes are then rounded
+ * to the new scale. A block begun by the call (its first token among the new ones) takes its e
+ * from the new tokens alone. Infinities and NaN are stored as NaN and count neither for e nor for the mean.
+ * The mean of a page's keys (of the stored values of the tokens that it holds) is kept in 8 bits too:
+ *   mean = int8 * 2^em,  em the least >= -100 with max |mean| <= 127 * 2^em.
+ * Everything but the rounding to 4 (8) bits is exact, so that pages are the same bits however calls are cut,
+ * up to values below 2^-6 of a block's scale that were rounded twice.
+ *
+ * A page of the codes is opaque but for its size; `scales` is {2^eK, 2^eV, 2^em, 0}. The library reads nothing of a page
+ * that was not written; codes, scales and means need no initial values.
+ */
+typedef struct rsa_cache {
+  int32_t batch;       /* sequences, >= 1 */
+  int32_t heads_kv;    /* >= 1; batch * heads_kv <= 65535 */
+  int32_t head_dim;    /* 64 or 128 */
+  int32_t block;       /* tokens of a page: 64 or 128 */
+  int32_t max_blocks;  /* entries of a row of the table, >= 1 */
+  int64_t pages;       /* 1 .. 2^31 - 1 */
+  void* k_codes;       /* device, [pages][heads_kv][block * head_dim] bytes, 16-byte aligned */
+  void* v_codes;       /* the same */
+  float* scales;       /* device, [pages][heads_kv][4], 16-byte aligned */
+  int8_t* k_mean;      /* device, [pages][heads_kv][head_dim], 16-byte aligned */
+  const int32_t* table;/* device, [batch][max_blocks] */
+} rsa_cache;
+
+/* Rows of new keys and values, or of queries and outputs: bf16 at ptr[b*stride_b + h*stride_h + t*stride_t + c],
+ * strides in elements, multiples of 8; pointers 16-byte aligned. */
+typedef struct rsa_rows {
+  int32_t heads;       /* K, V: heads_kv. Q, O: a multiple of heads_kv; head h reads key/value head h / (heads / heads_kv) */
+  int32_t t;           /* rows of a sequence, >= 1 (shorter sequences of a batch say so in `count` or `q_len`) */
+  int64_t stride_b, stride_h, stride_t;
+} rsa_rows;
+
+#define RSA_CACHE_CAUSAL 1           /* a query sees the keys up to its own position */
+#define RSA_CACHE_MAX_SELECT 16384   /* largest max_blocks of rsa_cache_select */
+
+/* Host only. Bytes of k_codes (and of v_codes), of scales and of k_mean; the pointers in `cache` may be NULL here. */
+int rsa_cache_bytes(const rsa_cache* cache, size_t* code_bytes, size_t* scale_bytes, size_t* mean_bytes);
+
+/* Host only. Bytes of device scratch of rsa_cache_select and rsa_cache_attn for queries `rows` in groups of `group`
+ * (0: no lists), whatever list_len <= max_blocks. The pointers in `cache` may be NULL. */
+int rsa_cache_workspace_bytes(const rsa_cache* cache, const rsa_rows* rows, int group, size_t* select_ws_bytes,
+                              size_t* attn_ws_bytes);
+
+/*
+ * Tokens start[b] .. start[b] + count[b] - 1 of every sequence b (device int32 [batch]; count NULL: all rows->t,
+ * more than rows->t counts as rows->t, less than 1 as none, a negative start as none) take rows 0 .. count[b] - 1 of K and V.
+ * Tokens behind the table are dropped. Of the blocks that are touched, pages, scales and mean are renewed: tokens
+ * before start[b] stay, what the block held from start[b] + count[b] on is gone (so a sequence may be taken
+ * back to an earlier length by writing there).
+ */
+int rsa_cache_write(const rsa_cache* cache, const rsa_rows* rows, const void* K, const void* V, const int32_t* start,
+                    const int32_t* count, void* stream);
+
+/* The same range of tokens back into rows 0 .. count[b] - 1 of K and V (exact: a code has 4 significant bits).
+ * Rows behind count[b], or of tokens without a page, are left as they were. */
+int rsa_cache_read(const rsa_cache* cache, const rsa_rows* rows, const int32_t* start, const int32_t* count, void* K,
+                   void* V, void* stream);
+
+/*
+ * Query token i < q_len[b] of sequence b stands at position kv_len[b] - q_len[b] + i; its own key is in the cache
+ * by then (kv_len: device int32 [batch], tokens in the cache; q_len NULL: all rows->t). Tokens are taken in groups of `group` >= 1
+ * from i = 0 on; a group and a key/value head have one list, for all query heads that share it.
+ *   visible   the blocks of the first kv_len[b] tokens; with RSA_CACHE_CAUSAL up to the block of the group's last position
+ *   score     q8 . mean * 2^em, q8 the sum of the group's queries over its tokens and heads (finite values), rounded
+ *             to 8 bits as the means are; exact, so that equal scores are equal: the lower block goes first
+ *   forced    blocks below `first`; and, where last >= 1, from `last` - 1 before the block of the group's first
+ *             position to the block of its last one
+ * Kept are the visible forced blocks and, by score, as many others as make `keep` in all.
+ *   block_idx [batch][heads_kv][groups][list_len]  kept blocks, ascending, then -1;  groups = ceil(rows->t / group)
+ *   kept      [batch][heads_kv][groups]            how many
+ * list_len must be at least min(max_blocks, max(keep, first + last + ceil(group / block) + 1)) (RSA_E_RANGE).
+ * max_blocks <= RSA_CACHE_MAX_SELECT (RSA_E_UNSUPPORTED). ws: select_ws_bytes, 256-byte aligned; may be NULL (slower where few groups score many blocks).
+ */
+int rsa_cache_select(const rsa_cache* cache, const rsa_rows* rows, const void* Q, const int32_t* kv_len,
+                     const int32_t* q_len, int group, int keep, int first, int last, int flags, int32_t* block_idx,
+                     int32_t* kept, int list_len, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * O = softmax(scale * Q K^T) V over the cached tokens that a query sees: the first kv_len[b], with RSA_CACHE_CAUSAL
+ * those up to its own position; with lists (block_idx and kept not NULL, as rsa_cache_select leaves them, `group`
+ * as there) of the listed blocks only. Entries of a list that are negative or behind the last visible block are passed over; a block
+ * listed twice counts twice. scale 0 selects 1/sqrt(head_dim). A query that sees no key gets 0 and a log-sum-exp of -inf. A NaN among
+ * the stored keys or values reaches the queries that see its token and no others.
+ * Without lists both pointers are NULL and `group` and `list_len` are ignored.
+ *   O    as Q (may be Q). Rows behind q_len[b] are left as they were
+ *   lse  (nullable) [batch][heads][t] fp32, natural log of the softmax denominator including the maximum
+ *   ws   attn_ws_bytes, 256-byte aligned (RSA_E_WORKSPACE); NULL: the key axis is not split over workgroups (slower
+ *        where there are few query rows; the last bits differ). A workspace belongs to one call at a time.
+ */
+int rsa_cache_attn(const rsa_cache* cache, const rsa_rows* rows, const void* Q, const int32_t* kv_len,
+                   const int32_t* q_len, float scale, int flags, const int32_t* block_idx, const int32_t* kept, int group,
+                   int list_len, void* O, float* lse, void* ws, size_t ws_bytes, void* stream);
+
 /* Static string for a return code. */
 const char* rsa_status_string(int status);
 

@@ -22,10 +22,13 @@ RSA_COMPENSATE = 2
 RSA_DENSE = 4
 RSA_MAX_BLOCKS = 4096
 RSA_STATIC_SCRATCH_BYTES = 16 << 20
+RSA_CACHE_CAUSAL = 1
+RSA_CACHE_MAX_SELECT = 16384
 
 EXPORTS = (
     "rsa_block_counts", "rsa_workspace_bytes", "rsa_pool", "rsa_pool_values", "rsa_implicit_attention", "rsa_adjacency_mask", "rsa_reorder_tokens", "rsa_select_blocks",
     "rsa_sparse_attn_rectified", "rsa_sparse_attn_rectified_static", "rsa_status_string",
+    "rsa_cache_bytes", "rsa_cache_workspace_bytes", "rsa_cache_write", "rsa_cache_read", "rsa_cache_select", "rsa_cache_attn",
 )
 
 
@@ -43,6 +46,22 @@ class rsa_shape(ctypes.Structure):
         ("t_video", ctypes.c_int64), ("t_text", ctypes.c_int64),
         ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64), ("stride_t", ctypes.c_int64),
         ("scale", ctypes.c_float),
+    ]
+
+
+class rsa_cache(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("heads_kv", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("block", ctypes.c_int32),
+        ("max_blocks", ctypes.c_int32), ("pages", ctypes.c_int64),
+        ("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("k_mean", ctypes.c_void_p),
+        ("table", ctypes.c_void_p),
+    ]
+
+
+class rsa_rows(ctypes.Structure):
+    _fields_ = [
+        ("heads", ctypes.c_int32), ("t", ctypes.c_int32),
+        ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64), ("stride_t", ctypes.c_int64),
     ]
 
 
@@ -80,6 +99,19 @@ def _lib() -> ctypes.CDLL:
         lib.rsa_adjacency_mask.restype = ctypes.c_int
         lib.rsa_reorder_tokens.argtypes = [shp, ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32), ctypes.c_int, vp, vp, vp]
         lib.rsa_reorder_tokens.restype = ctypes.c_int
+        cap, rwp, i = ctypes.POINTER(rsa_cache), ctypes.POINTER(rsa_rows), ctypes.c_int
+        lib.rsa_cache_bytes.argtypes = [cap, szp, szp, szp]
+        lib.rsa_cache_bytes.restype = i
+        lib.rsa_cache_workspace_bytes.argtypes = [cap, rwp, i, szp, szp]
+        lib.rsa_cache_workspace_bytes.restype = i
+        lib.rsa_cache_write.argtypes = [cap, rwp] + [vp] * 5
+        lib.rsa_cache_write.restype = i
+        lib.rsa_cache_read.argtypes = [cap, rwp] + [vp] * 5
+        lib.rsa_cache_read.restype = i
+        lib.rsa_cache_select.argtypes = [cap, rwp] + [vp] * 3 + [i] * 5 + [vp, vp, i, vp, ctypes.c_size_t, vp]
+        lib.rsa_cache_select.restype = i
+        lib.rsa_cache_attn.argtypes = [cap, rwp] + [vp] * 3 + [ctypes.c_float, i, vp, vp, i, i, vp, vp, vp, ctypes.c_size_t, vp]
+        lib.rsa_cache_attn.restype = i
         lib.rsa_status_string.argtypes = [ctypes.c_int]
         lib.rsa_status_string.restype = ctypes.c_char_p
         _LIB = lib
@@ -237,4 +269,157 @@ def rectified_sparse_attention(Q, K, V, O, buf: LayerBuffers, sparsity: float, p
                       buf.count, buf.R, stream)
     rsa_sparse_attn_rectified(buf.shape, Q, K, buf.Vt, buf.block_idx, buf.count, buf.mask_bits, buf.R, buf.Apool,
                               buf.Mc_bits, buf.Vp, flags, O, lse, buf.attn_ws, stream)
+    return O
+
+
+# ---- the 8-bit key/value cache ---------------------------------------------------------
+@dataclass
+class KVCache:
+    """Caller-owned device buffers of an 8-bit key/value cache and the record of them that the calls take."""
+    desc: rsa_cache
+    k_codes: torch.Tensor      # uint8 [pages, heads_kv, block * head_dim], opaque
+    v_codes: torch.Tensor
+    scales: torch.Tensor       # fp32  [pages, heads_kv, 4]
+    k_mean: torch.Tensor       # int8  [pages, heads_kv, head_dim]
+    table: torch.Tensor        # int32 [batch, max_blocks]: page of each block of a sequence, -1 where there is none
+
+    def __post_init__(self):
+        self.ref = ctypes.byref(self.desc)
+        self.device = self.k_codes.device
+
+
+def cache_of(k_codes, v_codes, scales, k_mean, table, block: int) -> KVCache:
+    """Record of a cache whose buffers exist. They may be filled and the table changed in place later."""
+    pages, heads_kv, page = k_codes.shape
+    want = ((k_codes, torch.uint8, (pages, heads_kv, page)), (v_codes, torch.uint8, (pages, heads_kv, page)),
+            (scales, torch.float32, (pages, heads_kv, 4)), (k_mean, torch.int8, (pages, heads_kv, page // block)),
+            (table, torch.int32, (table.shape[0], table.shape[-1])))
+    for x, dtype, shape in want:
+        if x.dtype != dtype or tuple(x.shape) != shape or not x.is_contiguous() or x.device != k_codes.device:
+            raise ValueError(f"expect a contiguous {dtype} tensor of shape {shape} on {k_codes.device}, got {x.dtype} {tuple(x.shape)} on {x.device}")
+    if page % block:
+        raise ValueError(f"a page of {page} codes is no block of {block} tokens")
+    desc = rsa_cache(table.shape[0], heads_kv, page // block, block, table.shape[1], pages, _ptr(k_codes), _ptr(v_codes),
+                     _ptr(scales), _ptr(k_mean), _ptr(table))
+    return KVCache(desc, k_codes, v_codes, scales, k_mean, table)
+
+
+def allocate_cache(batch: int, heads_kv: int, head_dim: int, block: int, pages: int, max_blocks: int, device="cuda:0") -> KVCache:
+    """An empty cache: no page is in the table yet."""
+    probe = rsa_cache(batch, heads_kv, head_dim, block, max_blocks, pages)
+    code, scale, mean = rsa_cache_bytes(probe)
+    u8 = dict(dtype=torch.uint8, device=device)
+    return cache_of(torch.empty(code, **u8).view(pages, heads_kv, block * head_dim),
+                    torch.empty(code, **u8).view(pages, heads_kv, block * head_dim),
+                    torch.empty(scale // 4, dtype=torch.float32, device=device).view(pages, heads_kv, 4),
+                    torch.empty(mean, dtype=torch.int8, device=device).view(pages, heads_kv, head_dim),
+                    torch.full((batch, max_blocks), -1, dtype=torch.int32, device=device), block)
+
+
+def make_rows(x: torch.Tensor) -> rsa_rows:
+    """Row record of a [batch, heads, t, head_dim] bf16 view (any b/h/t strides): new keys and values, or queries and outputs."""
+    assert x.dim() == 4 and x.stride(3) == 1 and x.dtype == torch.bfloat16, "expect bf16 [batch, heads, t, head_dim], last dim contiguous"
+    # (torch leaves the stride of a dimension of one element open)
+    sb, sh, st = (x.stride(i) if x.shape[i] > 1 else -(-x.shape[3] // 8) * 8 for i in range(3))
+    return rsa_rows(x.shape[1], x.shape[2], sb, sh, st)
+
+
+def _same_rows(cache: KVCache, rows: rsa_rows, *tensors) -> None:
+    """The tensors that go with one row record: bf16, of its sizes and strides, on the cache's device."""
+    for x in tensors:
+        if (x.dtype != torch.bfloat16 or x.dim() != 4 or x.shape[0] != cache.desc.batch or x.shape[1] != rows.heads or x.shape[2] != rows.t
+                or x.shape[3] != cache.desc.head_dim or x.device != cache.device
+                or (x.shape[0] > 1 and x.stride(0) != rows.stride_b) or (x.shape[1] > 1 and x.stride(1) != rows.stride_h)
+                or (x.shape[2] > 1 and x.stride(2) != rows.stride_t) or x.stride(3) != 1):
+            raise ValueError(f"tensor {x.dtype} {tuple(x.shape)} strides {x.stride()} on {x.device} is not what the row record says")
+
+
+def _lengths(cache: KVCache, x: Optional[torch.Tensor]) -> Optional[int]:
+    if x is None:
+        return None
+    if x.dtype != torch.int32 or x.numel() != cache.desc.batch or not x.is_contiguous() or x.device != cache.device:
+        raise ValueError("expect contiguous int32 lengths, one for each sequence, on the cache's device")
+    return x.data_ptr()
+
+
+def _lists(cache: KVCache, rows: rsa_rows, group: int, block_idx: torch.Tensor, kept: torch.Tensor) -> None:
+    groups = -(-rows.t // max(1, group))
+    shape = (cache.desc.batch, cache.desc.heads_kv, groups)
+    if (block_idx.dtype != torch.int32 or kept.dtype != torch.int32 or block_idx.shape[:3] != shape or kept.shape != shape
+            or block_idx.dim() != 4 or not block_idx.is_contiguous() or not kept.is_contiguous() or block_idx.device != cache.device or kept.device != cache.device):
+        raise ValueError(f"expect contiguous int32 lists {shape} + [list_len] and counts {shape} on the cache's device")
+
+
+def _call(cache: KVCache, stream, where: str, fn, *args) -> None:
+    """One call on the cache's device: on `stream`, or on that device's current stream."""
+    dev = cache.device.index
+    raw = torch.cuda.current_stream(dev).cuda_stream if stream is None else stream.cuda_stream
+    if torch.cuda.current_device() == dev:
+        status = fn(cache.ref, *args, raw)
+    else:
+        with torch.cuda.device(dev):
+            status = fn(cache.ref, *args, raw)
+    _check(status, where)
+
+
+def _scratch(ws: Optional[torch.Tensor]):
+    return (None, 0) if ws is None else (_ptr(ws), ws.numel() * ws.element_size())
+
+
+def rsa_cache_bytes(desc: rsa_cache):
+    a, b, c = ctypes.c_size_t(), ctypes.c_size_t(), ctypes.c_size_t()
+    _check(_lib().rsa_cache_bytes(ctypes.byref(desc), ctypes.byref(a), ctypes.byref(b), ctypes.byref(c)), "rsa_cache_bytes")
+    return a.value, b.value, c.value
+
+
+def rsa_cache_workspace_bytes(cache: KVCache, rows: rsa_rows, group: int = 0):
+    a, b = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(_lib().rsa_cache_workspace_bytes(cache.ref, ctypes.byref(rows), int(group), ctypes.byref(a), ctypes.byref(b)),
+           "rsa_cache_workspace_bytes")
+    return a.value, b.value
+
+
+def rsa_cache_write(cache: KVCache, rows, K, V, start, count=None, stream=None):
+    _same_rows(cache, rows, K, V)
+    _call(cache, stream, "rsa_cache_write", _lib().rsa_cache_write, ctypes.byref(rows), K.data_ptr(), V.data_ptr(),
+          _lengths(cache, start), _lengths(cache, count))
+
+
+def rsa_cache_read(cache: KVCache, rows, start, count, K, V, stream=None):
+    _same_rows(cache, rows, K, V)
+    _call(cache, stream, "rsa_cache_read", _lib().rsa_cache_read, ctypes.byref(rows), _lengths(cache, start), _lengths(cache, count),
+          K.data_ptr(), V.data_ptr())
+
+
+def rsa_cache_select(cache: KVCache, rows, Q, kv_len, q_len, group, keep, first, last, flags, block_idx, kept, ws=None, stream=None):
+    _same_rows(cache, rows, Q)
+    _lists(cache, rows, group, block_idx, kept)
+    _call(cache, stream, "rsa_cache_select", _lib().rsa_cache_select, ctypes.byref(rows), Q.data_ptr(), _lengths(cache, kv_len),
+          _lengths(cache, q_len), int(group), int(keep), int(first), int(last), int(flags), block_idx.data_ptr(), kept.data_ptr(),
+          block_idx.shape[3], *_scratch(ws))
+
+
+def rsa_cache_attn(cache: KVCache, rows, Q, kv_len, q_len, scale, flags, block_idx, kept, group, O, lse=None, ws=None, stream=None):
+    _same_rows(cache, rows, Q, O)
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != O.shape[:3] or not lse.is_contiguous() or lse.device != cache.device):
+        raise ValueError("expect a contiguous fp32 lse [batch, heads, t] on the cache's device")
+    if block_idx is not None and kept is not None:
+        _lists(cache, rows, group, block_idx, kept)
+    _call(cache, stream, "rsa_cache_attn", _lib().rsa_cache_attn, ctypes.byref(rows), Q.data_ptr(), _lengths(cache, kv_len),
+          _lengths(cache, q_len), float(scale), int(flags), _ptr(block_idx), _ptr(kept), int(group),
+          block_idx.shape[3] if block_idx is not None else 0, O.data_ptr(), _ptr(lse), *_scratch(ws))
+
+
+def cached_sparse_attention(cache: KVCache, K, V, Q, O, kv_len, q_len, group: int, keep: int, block_idx, kept, first: int = 1,
+                            last: int = 1, flags: int = RSA_CACHE_CAUSAL, start=None, lse=None, ws=None, stream=None):
+    """One step of a sequence of frames or tokens: the new rows into the cache, the blocks that each group of them reads, and
+    their attention; three C-ABI calls on one stream, no host sync. `kv_len` counts the new rows, `start` = kv_len - q_len
+    (computed here when it is not given)."""
+    if start is None:
+        with torch.cuda.stream(stream):                # (None: the current stream)
+            start = kv_len - (q_len if q_len is not None else Q.shape[2])
+    rows_kv, rows = make_rows(K), make_rows(Q)
+    rsa_cache_write(cache, rows_kv, K, V, start, q_len, stream)
+    rsa_cache_select(cache, rows, Q, kv_len, q_len, group, keep, first, last, flags, block_idx, kept, ws, stream)
+    rsa_cache_attn(cache, rows, Q, kv_len, q_len, 0.0, flags, block_idx, kept, group, O, lse, ws, stream)
     return O

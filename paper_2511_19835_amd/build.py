@@ -27,6 +27,10 @@ SOURCES = [
     "reorder_kernels.hip",
     "attn_side_kernels.hip",
     "attn_kernels.hip",
+    "cache_api.hip",
+    "cache_page_kernels.hip",
+    "cache_select_kernels.hip",
+    "cache_attn_kernels.hip",
 ]
 
 # Packed-fp32 VALU forms (v_pk_*_f32) are switched off for every device translation unit.

@@ -1,0 +1,452 @@
+// Attention of new queries over the 8-bit key/value cache, over all blocks or over listed ones.
+//
+// A tile is 16 QT query rows of one (sequence, key/value head): rows are (token, query head of the key/value head), token
+// by token, so that one pass over the keys serves all heads that share them. Each wave computes, with 16x16x32 products,
+//     S^T = K Q^T      (M = key, N = query, k = channel; e4m3 -> bf16, exact)
+//     O^T += V^T P^T   (M = channel, N = query, k = key; e4m3 -> fp16, exact)
+// with the softmax between them lane-local: codes lie in the page in operand order (cache_common.hpp), so the loop needs
+// neither LDS nor a barrier; the codes go from memory into the registers that the products read. The scale of a block's
+// keys goes into the scores, that of its values into the exponent of P (below).
+//
+// P is rounded to fp16 (11 bits; V has 4): half a step is 2^-12 of p, against the output's own 2^-9 in bf16. Range: the
+// running reference m of a row follows its maximum lazily (only when a score passes it by more than 8 in log2), so p <= 2^8;
+// O is held over 2^eo, eo within 8 of the exponent of the values' scale, so what P carries for it is at most 2^8 again.
+//
+// The four waves of a workgroup take every fourth step of 64 keys and are joined in LDS; where there are few tiles the key
+// axis is also split over workgroups, whose normalised parts (fp32) cache_join_kernel adds in a fixed order.
+#include "cache_common.hpp"
+
+namespace rsa {
+namespace {
+
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kNoReference = -3.0e38f;     // of a row that has seen no key; finite, so that differences stay defined
+constexpr float kLazy = 8.f;
+constexpr int kCus = 256;                    // compute units of an MI355X
+
+// Sixteen codes as the bf16 / fp16 operands of two products (bytes 0-7 and 8-15).
+__device__ __forceinline__ void widen(const uint4& v, bf16x8 (&o)[2]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], 1.0f, false);
+    const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], 1.0f, true);
+    o[i / 2][i % 2 * 4 + 0] = lo[0]; o[i / 2][i % 2 * 4 + 1] = lo[1];
+    o[i / 2][i % 2 * 4 + 2] = hi[0]; o[i / 2][i % 2 * 4 + 3] = hi[1];
+  }
+}
+__device__ __forceinline__ void widen(const uint4& v, halfx8 (&o)[2]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const halfx2 lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[i], 1.0f, false);
+    const halfx2 hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[i], 1.0f, true);
+    o[i / 2][i % 2 * 4 + 0] = lo[0]; o[i / 2][i % 2 * 4 + 1] = lo[1];
+    o[i / 2][i % 2 * 4 + 2] = hi[0]; o[i / 2][i % 2 * 4 + 3] = hi[1];
+  }
+}
+// 0xff in every byte that holds the code of NaN.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
+  const uint32_t top = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+  return (top >> 7) * 255u;
+}
+
+// What a tile is, the same in every lane.
+struct Tile {
+  int b, hk;            // sequence, key/value head
+  int t0;               // first token of its group
+  int row0, rows;       // first row among the group's (token, head) rows, and how many the group has
+  int lrow;             // row of the lists (also without lists: the row of partial results)
+  int64_t kv;           // tokens in the cache
+  int ql;               // query tokens of the sequence
+  int units;            // blocks to walk: listed ones, or all that any row of the tile sees
+  int blocks;           // blocks that hold a visible key
+  int64_t lo_seen;      // keys that every row of the tile sees
+};
+struct TileGrid {
+  int rows_per_tile;    // 16 QT
+  int per_group;        // tiles of a group
+  int splits;
+  int stored;           // rows of a partial result: min(16 QT, rows of a group)
+};
+
+__device__ __forceinline__ Tile tile_of(const CacheDims& c, const RowDims& r, const CacheAttnArgs& a, const TileGrid& tg, int64_t id) {
+  Tile t;
+  const int G = r.heads / c.heads_kv;
+  const int k = (int)(id % tg.per_group);
+  t.lrow = (int)(id / tg.per_group);
+  const int bh = t.lrow / a.groups, grp = t.lrow % a.groups;
+  t.b = bh / c.heads_kv;
+  t.hk = bh % c.heads_kv;
+  t.t0 = grp * a.group;
+  t.rows = min(a.group, r.t - t.t0) * G;
+  t.row0 = k * tg.rows_per_tile;
+  t.kv = max(a.kv_len[t.b], 0);
+  t.ql = a.q_len ? min(a.q_len[t.b], r.t) : r.t;
+  const int last_row = min(t.row0 + tg.rows_per_tile, t.rows) - 1;
+  const int first_tok = t.t0 + t.row0 / G, last_tok = min(t.t0 + last_row / G, t.ql - 1);
+  int64_t hi = 0;
+  t.lo_seen = 0;
+  if (t.row0 < t.rows && first_tok < t.ql) {       // some row of the tile is a query
+    t.lo_seen = a.causal ? min(max(t.kv - t.ql + first_tok + 1, (int64_t)0), t.kv) : t.kv;
+    hi = a.causal ? min(max(t.kv - t.ql + last_tok + 1, (int64_t)0), t.kv) : t.kv;
+  }
+  t.blocks = (int)min((hi + c.blk - 1) / c.blk, (int64_t)c.max_blocks);
+  t.units = t.blocks;
+  if (a.block_idx) t.units = t.blocks > 0 ? min(max(a.kept[t.lrow], 0), a.list_len) : 0;
+  return t;
+}
+
+template <int D, int BLK, int QT>
+__global__ __launch_bounds__(256) void cache_attn_kernel(CacheDims c, RowDims r, CacheAttnArgs a, TileGrid tg) {
+  constexpr int KC = D / 64, VC = D / 16;          // 16-byte loads of a lane for 16 keys / for 64 keys
+  constexpr int SPB = BLK / 64;                    // steps of 64 keys in a block
+  constexpr int PITCH = D + 4;                     // floats of a row in the joining buffer
+  __shared__ __align__(16) float join[4][16][PITCH];
+  __shared__ float join_m[4][16], join_l[4][16];
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const int g = lane / 16, n = lane % 16;
+  const int split = blockIdx.x % tg.splits;
+  const int64_t id = blockIdx.x / tg.splits;
+  const Tile t = tile_of(c, r, a, tg, id);
+  const int G = r.heads / c.heads_kv;
+
+  // queries of this lane's columns, as operands, and how many keys each sees
+  bf16x8 q[QT][2 * KC];
+  int64_t seen[QT];
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    const int row = t.row0 + 16 * x + n, tok = t.t0 + row / G;
+    const bool is = row < t.rows && tok < t.ql;
+    seen[x] = !is ? 0 : a.causal ? min(max(t.kv - t.ql + tok + 1, (int64_t)0), t.kv) : t.kv;
+    const uint16_t* src = a.Q + (int64_t)t.b * r.sb + (int64_t)(t.hk * G + row % G) * r.sh + (int64_t)tok * r.st;
+#pragma unroll
+    for (int k = 0; k < KC; ++k)
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (is) v = *reinterpret_cast<const uint4*>(src + k * 64 + g * 16 + hf * 8);
+        q[x][2 * k + hf] = __builtin_bit_cast(bf16x8, v);
+      }
+  }
+  floatx4 o[QT][VC];
+  float m[QT], l[QT];
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    m[x] = kNoReference;
+    l[x] = 0.f;
+#pragma unroll
+    for (int v = 0; v < VC; ++v) o[x][v] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  int eo = -200, top = -200;                       // o is held over 2^eo; the largest exponent of a scale so far
+
+  const int u0 = (int)((int64_t)t.units * split / tg.splits), u1 = (int)((int64_t)t.units * (split + 1) / tg.splits);
+  const int steps = (u1 - u0) * SPB;
+  // this wave's steps are wave, wave + 4, ...; lane i looks up the i-th of the next 64
+  for (int base = wave; base < steps; base += 256) {
+    int my_blk = -1, my_page = -1;
+    float my_k = 0.f, my_v = 0.f;
+    const int my_step = base + lane * 4;
+    if (my_step < steps) {
+      my_blk = u0 + my_step / SPB;
+      if (a.block_idx) my_blk = a.block_idx[(int64_t)t.lrow * a.list_len + my_blk];
+      if (my_blk < t.blocks) my_page = cache_page(c, t.b, my_blk);
+      if (my_page >= 0) {
+        const float2 sc = *reinterpret_cast<const float2*>(c.scales + ((int64_t)my_page * c.heads_kv + t.hk) * 4);
+        my_k = sc.x;
+        my_v = sc.y;
+      }
+    }
+    unsigned long long todo = __ballot(my_page >= 0);
+    uint4 kc[4 * KC], vc[VC];
+    auto load_k = [&](int i) __attribute__((always_inline)) {
+      const int64_t rec = (int64_t)__builtin_amdgcn_readlane(my_page, i) * c.heads_kv + t.hk;
+      const uint8_t* p = c.k + rec * (BLK * D) + ((base + i * 4) % SPB) * (64 * D) + lane * 16;
+#pragma unroll
+      for (int x = 0; x < 4 * KC; ++x) kc[x] = *reinterpret_cast<const uint4*>(p + x * 1024);
+    };
+    auto load_v = [&](int i) __attribute__((always_inline)) {
+      const int64_t rec = (int64_t)__builtin_amdgcn_readlane(my_page, i) * c.heads_kv + t.hk;
+      const uint8_t* p = c.v + rec * (BLK * D) + ((base + i * 4) % SPB) * (64 * D) + lane * 16;
+#pragma unroll
+      for (int x = 0; x < VC; ++x) vc[x] = *reinterpret_cast<const uint4*>(p + x * 1024);
+    };
+    int i = todo ? __builtin_ctzll(todo) : -1;
+    if (i >= 0) { load_k(i); load_v(i); }
+    while (i >= 0) {
+      todo &= todo - 1;
+      const int next = todo ? __builtin_ctzll(todo) : -1;
+      const int64_t key0 = (int64_t)__builtin_amdgcn_readlane(my_blk, i) * BLK + ((base + i * 4) % SPB) * 64;
+      const float ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_k), i)) * a.scale_log2e;
+      const int ev = exponent_of(__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_v), i)));
+
+      floatx4 s[QT][4];
+#pragma unroll
+      for (int x = 0; x < QT; ++x)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) s[x][y] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+#pragma unroll
+        for (int k = 0; k < KC; ++k) {
+          bf16x8 op[2];
+          widen(kc[y * KC + k], op);
+#pragma unroll
+          for (int x = 0; x < QT; ++x) {
+            s[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op[0], q[x][2 * k], s[x][y], 0, 0, 0);
+            s[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op[1], q[x][2 * k + 1], s[x][y], 0, 0, 0);
+          }
+        }
+      if (next >= 0) load_k(next);
+
+      // scores; keys that a row does not see leave its softmax
+      const bool partly = key0 + 64 > t.lo_seen;
+      bool over = false;
+#pragma unroll
+      for (int x = 0; x < QT; ++x) {
+        const int left = (int)min(max(seen[x] - key0, (int64_t)-1), (int64_t)64);   // of the 64
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float z = s[x][y][e] * ks;
+            if (partly) z = 16 * y + 4 * g + e < left ? z : -INFINITY;
+            s[x][y][e] = z;
+            over |= z > m[x] + kLazy;
+          }
+      }
+      if (__any(over)) {
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          float mx = kNoReference;
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[x][y][e]);
+          mx = fmaxf(mx, __shfl_xor(mx, 16));
+          mx = fmaxf(mx, __shfl_xor(mx, 32));
+          if (mx > m[x] + kLazy) {                 // the same in the four lanes of a column
+            const float down = exp2f(m[x] - mx);
+            m[x] = mx;
+            l[x] *= down;
+#pragma unroll
+            for (int v = 0; v < VC; ++v) o[x][v] *= down;
+          }
+        }
+      }
+      // the exponent of the values' scale: o follows it, P makes up for the rest
+      if (ev > eo || ev < eo - 8) {
+        top = max(top, ev);
+        const int to = max(ev, top - 80);          // o may grow by 2^80 and stay finite
+        if (to != eo) {
+          const int by = max(min(eo - to, 120), -126);
+          const float f = exp2_int(by);
+#pragma unroll
+          for (int x = 0; x < QT; ++x)
+#pragma unroll
+            for (int v = 0; v < VC; ++v) o[x][v] *= f;
+          eo = to;
+        }
+      }
+      const float pe = exp2_int(max(ev - eo, -126));
+      halfx8 p[QT][2];
+#pragma unroll
+      for (int x = 0; x < QT; ++x)
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float w = __builtin_amdgcn_exp2f(s[x][y][e] - m[x]);
+            l[x] += w;
+            p[x][y / 2][y % 2 * 4 + e] = (_Float16)(w * pe);
+          }
+
+      // a value that is NaN under a key that a row does not see must not reach it through 0 * NaN
+      bool odd = false;
+      if (partly) {
+        uint32_t bad = 0;
+#pragma unroll
+        for (int v = 0; v < VC; ++v) bad |= nan_bytes(vc[v].x) | nan_bytes(vc[v].y) | nan_bytes(vc[v].z) | nan_bytes(vc[v].w);
+        odd = __any(bad != 0);
+      }
+      if (odd) {
+        halfx8 see[QT][2];
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          const int left = (int)min(max(seen[x] - key0, (int64_t)-1), (int64_t)64);
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) see[x][y / 2][y % 2 * 4 + e] = 16 * y + 4 * g + e < left ? (_Float16)1.f : (_Float16)0.f;
+        }
+#pragma unroll
+        for (int v = 0; v < VC; ++v) {
+          const uint4 w = vc[v];
+          const uint4 nb = make_uint4(nan_bytes(w.x), nan_bytes(w.y), nan_bytes(w.z), nan_bytes(w.w));
+          vc[v] = make_uint4(w.x & ~nb.x, w.y & ~nb.y, w.z & ~nb.z, w.w & ~nb.w);
+          halfx8 is[2];
+          widen(make_uint4(nb.x & 0x38383838u, nb.y & 0x38383838u, nb.z & 0x38383838u, nb.w & 0x38383838u), is);   // 1.0
+#pragma unroll
+          for (int x = 0; x < QT; ++x) {
+            floatx4 hit = {0.f, 0.f, 0.f, 0.f};
+            hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(is[0], see[x][0], hit, 0, 0, 0);
+            hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(is[1], see[x][1], hit, 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (hit[e] > 0.f) o[x][v][e] = __builtin_nanf("");
+          }
+        }
+      }
+#pragma unroll
+      for (int v = 0; v < VC; ++v) {
+        halfx8 op[2];
+        widen(vc[v], op);
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          o[x][v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op[0], p[x][0], o[x][v], 0, 0, 0);
+          o[x][v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op[1], p[x][1], o[x][v], 0, 0, 0);
+        }
+      }
+      if (next >= 0) load_v(next);
+      i = next;
+    }
+  }
+
+  // join the four waves, 16 rows at a time
+  const float unit = eo < -126 ? 0.f : exp2_int(min(eo, 127));
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    float sum = l[x];
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (x > 0) __syncthreads();
+    if (g == 0) {
+      join_m[wave][n] = m[x];
+      join_l[wave][n] = sum;
+    }
+    __syncthreads();
+    float most = join_m[0][n];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) most = fmaxf(most, join_m[w][n]);
+    float total = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) total += join_l[w][n] * exp2f(join_m[w][n] - most);
+    const float f = total == 0.f ? 0.f : exp2f(m[x] - most) / total * unit;
+#pragma unroll
+    for (int v = 0; v < VC; ++v)
+      *reinterpret_cast<floatx4*>(&join[wave][n][16 * v + 4 * g]) = o[x][v] * f;
+    __syncthreads();
+    constexpr int CPR = D / 8;
+    for (int u = tid; u < 16 * CPR; u += 256) {
+      const int rr = u / CPR, ch = u % CPR * 8, row = t.row0 + 16 * x + rr, tok = t.t0 + row / G;
+      if (row >= t.rows || tok >= t.ql) continue;
+      float z[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] = (join[0][rr][ch + e] + join[1][rr][ch + e]) + (join[2][rr][ch + e] + join[3][rr][ch + e]);
+      if (tg.splits == 1) {
+        uint4 v = make_uint4(pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]), pack_bf16x2(z[4], z[5]), pack_bf16x2(z[6], z[7]));
+        *reinterpret_cast<uint4*>(a.O + (int64_t)t.b * r.sb + (int64_t)(t.hk * G + row % G) * r.sh + (int64_t)tok * r.st + ch) = v;
+      } else {
+        float* dst = a.parts + ((int64_t)blockIdx.x * tg.stored + 16 * x + rr) * D + ch;
+        *reinterpret_cast<float4*>(dst) = make_float4(z[0], z[1], z[2], z[3]);
+        *reinterpret_cast<float4*>(dst + 4) = make_float4(z[4], z[5], z[6], z[7]);
+      }
+    }
+    const int row = t.row0 + 16 * x + n, tok = t.t0 + row / G;
+    if (tid < 16 && row < t.rows && tok < t.ql) {
+      const float lse2 = total == 0.f ? -INFINITY : most + log2f(total);
+      if (tg.splits > 1) (a.parts + (int64_t)gridDim.x * tg.stored * D)[(int64_t)blockIdx.x * tg.stored + 16 * x + n] = lse2;
+      else if (a.lse) a.lse[((int64_t)t.b * r.heads + t.hk * G + row % G) * r.t + tok] = lse2 * kLn2;
+    }
+  }
+}
+
+// Parts of a tile's rows, weighted by their share of the softmax denominator and added in the order of the keys.
+template <int D>
+__global__ __launch_bounds__(256) void cache_join_kernel(CacheDims c, RowDims r, CacheAttnArgs a, TileGrid tg, int64_t tiles) {
+  constexpr int CPR = D / 8;
+  const int G = r.heads / c.heads_kv;
+  const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int ch = (int)(u % CPR) * 8, rr = (int)(u / CPR % tg.stored);
+  const int64_t id = u / CPR / tg.stored;
+  if (id >= tiles) return;
+  const int lrow = (int)(id / tg.per_group), k = (int)(id % tg.per_group);
+  const int bh = lrow / a.groups, grp = lrow % a.groups, b = bh / c.heads_kv, hk = bh % c.heads_kv;
+  const int t0 = grp * a.group, row = k * tg.rows_per_tile + rr, tok = t0 + row / G;
+  const int ql = a.q_len ? min(a.q_len[b], r.t) : r.t;
+  if (row >= min(a.group, r.t - t0) * G || tok >= ql) return;
+  const int64_t first = id * tg.splits;
+  const float* part_lse = a.parts + tiles * tg.splits * tg.stored * D;
+  float most = -INFINITY;
+  for (int s = 0; s < tg.splits; ++s) most = fmaxf(most, part_lse[(first + s) * tg.stored + rr]);
+  float z[8] = {0, 0, 0, 0, 0, 0, 0, 0}, total = 0.f;
+  for (int s = 0; s < tg.splits; ++s) {
+    const float p = part_lse[(first + s) * tg.stored + rr];
+    const float w = p == -INFINITY ? 0.f : exp2f(p - most);
+    const float* src = a.parts + ((first + s) * tg.stored + rr) * D + ch;
+    const float4 lo = *reinterpret_cast<const float4*>(src), hi = *reinterpret_cast<const float4*>(src + 4);
+    total += w;
+    z[0] += w * lo.x; z[1] += w * lo.y; z[2] += w * lo.z; z[3] += w * lo.w;
+    z[4] += w * hi.x; z[5] += w * hi.y; z[6] += w * hi.z; z[7] += w * hi.w;
+  }
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+  const uint4 v = make_uint4(pack_bf16x2(z[0] * inv, z[1] * inv), pack_bf16x2(z[2] * inv, z[3] * inv),
+                             pack_bf16x2(z[4] * inv, z[5] * inv), pack_bf16x2(z[6] * inv, z[7] * inv));
+  *reinterpret_cast<uint4*>(a.O + (int64_t)b * r.sb + (int64_t)(hk * G + row % G) * r.sh + (int64_t)tok * r.st + ch) = v;
+  if (ch == 0 && a.lse) a.lse[((int64_t)b * r.heads + hk * G + row % G) * r.t + tok] = total == 0.f ? -INFINITY : (most + log2f(total)) * kLn2;
+}
+
+struct Plan {
+  int qt;
+  int64_t tiles;
+  TileGrid grid;
+};
+// Rows of a group fill tiles of 16 or 32. The key axis is split until there are about four workgroups to a compute unit
+// or every wave has one step of 64 keys.
+Plan plan_of(const CacheDims& c, const RowDims& r, int group, int list_len) {
+  Plan p;
+  const int G = r.heads / c.heads_kv;
+  const int per = group > 0 && group < r.t ? group : r.t;
+  const int64_t rows = (int64_t)per * G;
+  p.qt = rows <= 16 ? 1 : 2;
+  p.grid.rows_per_tile = 16 * p.qt;
+  p.grid.per_group = (int)((rows + p.grid.rows_per_tile - 1) / p.grid.rows_per_tile);
+  p.grid.stored = (int)(rows < p.grid.rows_per_tile ? rows : p.grid.rows_per_tile);
+  p.tiles = (int64_t)((r.t + per - 1) / per) * p.grid.per_group * c.batch * c.heads_kv;
+  const int64_t steps = (int64_t)(list_len > 0 ? list_len : c.max_blocks) * (c.blk / 64);
+  const int64_t most = (steps + 3) / 4;
+  int64_t s = (4 * kCus + p.tiles - 1) / p.tiles;
+  if (s > most) s = most;
+  if (s > 64) s = 64;
+  p.grid.splits = (int)(s < 1 ? 1 : s);
+  return p;
+}
+
+template <int D, int BLK>
+hipError_t launch_t(const CacheDims& c, const RowDims& r, const CacheAttnArgs& a, const Plan& p, hipStream_t s) {
+  const dim3 grid((uint32_t)(p.tiles * p.grid.splits)), block(256);
+  if (p.qt == 1) hipLaunchKernelGGL((cache_attn_kernel<D, BLK, 1>), grid, block, 0, s, c, r, a, p.grid);
+  else hipLaunchKernelGGL((cache_attn_kernel<D, BLK, 2>), grid, block, 0, s, c, r, a, p.grid);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.grid.splits == 1) return e;
+  const int64_t threads = p.tiles * p.grid.stored * (D / 8);
+  hipLaunchKernelGGL((cache_join_kernel<D>), dim3((uint32_t)((threads + 255) / 256)), block, 0, s, c, r, a, p.grid, p.tiles);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t cache_attn_parts_bytes(const CacheDims& c, const RowDims& r, int group, int list_len) {
+  const Plan p = plan_of(c, r, group, list_len);
+  return p.grid.splits == 1 ? 0 : (size_t)p.tiles * p.grid.splits * p.grid.stored * (c.d + 1) * sizeof(float);
+}
+
+hipError_t launch_cache_attn(const CacheDims& c, const RowDims& r, const CacheAttnArgs& a, hipStream_t s) {
+  Plan p = plan_of(c, r, a.block_idx ? a.group : 0, a.block_idx ? a.list_len : 0);
+  if (!a.parts) p.grid.splits = 1;
+  if (p.tiles * p.grid.splits >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
+  if (c.d == 128) return c.blk == 128 ? launch_t<128, 128>(c, r, a, p, s) : launch_t<128, 64>(c, r, a, p, s);
+  return c.blk == 128 ? launch_t<64, 128>(c, r, a, p, s) : launch_t<64, 64>(c, r, a, p, s);
+}
+
+}  // namespace rsa
