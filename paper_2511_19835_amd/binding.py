@@ -284,8 +284,10 @@ class KVCache:
     table: torch.Tensor        # int32 [batch, max_blocks]: page of each block of a sequence, -1 where there is none
 
     def __post_init__(self):
+        # what every call needs of the record, at hand
         self.ref = ctypes.byref(self.desc)
         self.device = self.k_codes.device
+        self.batch, self.heads_kv, self.head_dim = self.desc.batch, self.desc.heads_kv, self.desc.head_dim
 
 
 def cache_of(k_codes, v_codes, scales, k_mean, table, block: int) -> KVCache:
@@ -321,45 +323,46 @@ def make_rows(x: torch.Tensor) -> rsa_rows:
     assert x.dim() == 4 and x.stride(3) == 1 and x.dtype == torch.bfloat16, "expect bf16 [batch, heads, t, head_dim], last dim contiguous"
     # (torch leaves the stride of a dimension of one element open)
     sb, sh, st = (x.stride(i) if x.shape[i] > 1 else -(-x.shape[3] // 8) * 8 for i in range(3))
-    return rsa_rows(x.shape[1], x.shape[2], sb, sh, st)
+    rows = rsa_rows(x.shape[1], x.shape[2], sb, sh, st)
+    rows.shape, rows.strides, rows.ref = x.shape, x.stride(), ctypes.byref(rows)
+    return rows
 
 
-def _same_rows(cache: KVCache, rows: rsa_rows, *tensors) -> None:
-    """The tensors that go with one row record: bf16, of its sizes and strides, on the cache's device."""
-    for x in tensors:
-        if (x.dtype != torch.bfloat16 or x.dim() != 4 or x.shape[0] != cache.desc.batch or x.shape[1] != rows.heads or x.shape[2] != rows.t
-                or x.shape[3] != cache.desc.head_dim or x.device != cache.device
-                or (x.shape[0] > 1 and x.stride(0) != rows.stride_b) or (x.shape[1] > 1 and x.stride(1) != rows.stride_h)
-                or (x.shape[2] > 1 and x.stride(2) != rows.stride_t) or x.stride(3) != 1):
-            raise ValueError(f"tensor {x.dtype} {tuple(x.shape)} strides {x.stride()} on {x.device} is not what the row record says")
+def _row_tensor(cache: KVCache, rows: rsa_rows, x: torch.Tensor) -> int:
+    """Address of a tensor that goes with a row record: bf16, of its sizes and strides, on the cache's device."""
+    shape = x.shape
+    if (x.dtype is not torch.bfloat16 or shape != rows.shape or shape[0] != cache.batch or shape[3] != cache.head_dim or x.device != cache.device
+            or x.stride() != rows.strides and any(n > 1 and p != q for n, p, q in zip(shape, x.stride(), rows.strides))):
+        raise ValueError(f"tensor {x.dtype} {tuple(shape)} strides {x.stride()} on {x.device} is not what the row record says")
+    return x.data_ptr()
 
 
 def _lengths(cache: KVCache, x: Optional[torch.Tensor]) -> Optional[int]:
     if x is None:
         return None
-    if x.dtype != torch.int32 or x.numel() != cache.desc.batch or not x.is_contiguous() or x.device != cache.device:
+    if x.dtype is not torch.int32 or x.numel() != cache.batch or not x.is_contiguous() or x.device != cache.device:
         raise ValueError("expect contiguous int32 lengths, one for each sequence, on the cache's device")
     return x.data_ptr()
 
 
 def _lists(cache: KVCache, rows: rsa_rows, group: int, block_idx: torch.Tensor, kept: torch.Tensor) -> None:
-    groups = -(-rows.t // max(1, group))
-    shape = (cache.desc.batch, cache.desc.heads_kv, groups)
-    if (block_idx.dtype != torch.int32 or kept.dtype != torch.int32 or block_idx.shape[:3] != shape or kept.shape != shape
-            or block_idx.dim() != 4 or not block_idx.is_contiguous() or not kept.is_contiguous() or block_idx.device != cache.device or kept.device != cache.device):
+    shape = (cache.batch, cache.heads_kv, -(-rows.shape[2] // max(1, group)))
+    if (block_idx.dtype is not torch.int32 or kept.dtype is not torch.int32 or block_idx.dim() != 4 or block_idx.shape[:3] != shape or kept.shape != shape
+            or not block_idx.is_contiguous() or not kept.is_contiguous() or block_idx.device != cache.device or kept.device != cache.device):
         raise ValueError(f"expect contiguous int32 lists {shape} + [list_len] and counts {shape} on the cache's device")
 
 
 def _call(cache: KVCache, stream, where: str, fn, *args) -> None:
     """One call on the cache's device: on `stream`, or on that device's current stream."""
     dev = cache.device.index
-    raw = torch.cuda.current_stream(dev).cuda_stream if stream is None else stream.cuda_stream
+    raw = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
     if torch.cuda.current_device() == dev:
         status = fn(cache.ref, *args, raw)
     else:
         with torch.cuda.device(dev):
             status = fn(cache.ref, *args, raw)
-    _check(status, where)
+    if status != 0:
+        raise RsaError(status, where)
 
 
 def _scratch(ws: Optional[torch.Tensor]):
@@ -374,40 +377,35 @@ def rsa_cache_bytes(desc: rsa_cache):
 
 def rsa_cache_workspace_bytes(cache: KVCache, rows: rsa_rows, group: int = 0):
     a, b = ctypes.c_size_t(), ctypes.c_size_t()
-    _check(_lib().rsa_cache_workspace_bytes(cache.ref, ctypes.byref(rows), int(group), ctypes.byref(a), ctypes.byref(b)),
+    _check(_lib().rsa_cache_workspace_bytes(cache.ref, rows.ref, int(group), ctypes.byref(a), ctypes.byref(b)),
            "rsa_cache_workspace_bytes")
     return a.value, b.value
 
 
 def rsa_cache_write(cache: KVCache, rows, K, V, start, count=None, stream=None):
-    _same_rows(cache, rows, K, V)
-    _call(cache, stream, "rsa_cache_write", _lib().rsa_cache_write, ctypes.byref(rows), K.data_ptr(), V.data_ptr(),
+    _call(cache, stream, "rsa_cache_write", _lib().rsa_cache_write, rows.ref, _row_tensor(cache, rows, K), _row_tensor(cache, rows, V),
           _lengths(cache, start), _lengths(cache, count))
 
 
 def rsa_cache_read(cache: KVCache, rows, start, count, K, V, stream=None):
-    _same_rows(cache, rows, K, V)
-    _call(cache, stream, "rsa_cache_read", _lib().rsa_cache_read, ctypes.byref(rows), _lengths(cache, start), _lengths(cache, count),
-          K.data_ptr(), V.data_ptr())
+    _call(cache, stream, "rsa_cache_read", _lib().rsa_cache_read, rows.ref, _lengths(cache, start), _lengths(cache, count),
+          _row_tensor(cache, rows, K), _row_tensor(cache, rows, V))
 
 
 def rsa_cache_select(cache: KVCache, rows, Q, kv_len, q_len, group, keep, first, last, flags, block_idx, kept, ws=None, stream=None):
-    _same_rows(cache, rows, Q)
     _lists(cache, rows, group, block_idx, kept)
-    _call(cache, stream, "rsa_cache_select", _lib().rsa_cache_select, ctypes.byref(rows), Q.data_ptr(), _lengths(cache, kv_len),
-          _lengths(cache, q_len), int(group), int(keep), int(first), int(last), int(flags), block_idx.data_ptr(), kept.data_ptr(),
-          block_idx.shape[3], *_scratch(ws))
+    _call(cache, stream, "rsa_cache_select", _lib().rsa_cache_select, rows.ref, _row_tensor(cache, rows, Q), _lengths(cache, kv_len),
+          _lengths(cache, q_len), group, keep, first, last, flags, block_idx.data_ptr(), kept.data_ptr(), block_idx.shape[3], *_scratch(ws))
 
 
 def rsa_cache_attn(cache: KVCache, rows, Q, kv_len, q_len, scale, flags, block_idx, kept, group, O, lse=None, ws=None, stream=None):
-    _same_rows(cache, rows, Q, O)
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != O.shape[:3] or not lse.is_contiguous() or lse.device != cache.device):
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != rows.shape[:3] or not lse.is_contiguous() or lse.device != cache.device):
         raise ValueError("expect a contiguous fp32 lse [batch, heads, t] on the cache's device")
     if block_idx is not None and kept is not None:
         _lists(cache, rows, group, block_idx, kept)
-    _call(cache, stream, "rsa_cache_attn", _lib().rsa_cache_attn, ctypes.byref(rows), Q.data_ptr(), _lengths(cache, kv_len),
-          _lengths(cache, q_len), float(scale), int(flags), _ptr(block_idx), _ptr(kept), int(group),
-          block_idx.shape[3] if block_idx is not None else 0, O.data_ptr(), _ptr(lse), *_scratch(ws))
+    _call(cache, stream, "rsa_cache_attn", _lib().rsa_cache_attn, rows.ref, _row_tensor(cache, rows, Q), _lengths(cache, kv_len),
+          _lengths(cache, q_len), scale, flags, _ptr(block_idx), _ptr(kept), group, block_idx.shape[3] if block_idx is not None else 0,
+          _row_tensor(cache, rows, O), _ptr(lse), *_scratch(ws))
 
 
 def cached_sparse_attention(cache: KVCache, K, V, Q, O, kv_len, q_len, group: int, keep: int, block_idx, kept, first: int = 1,

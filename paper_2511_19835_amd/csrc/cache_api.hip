@@ -91,7 +91,7 @@ int rsa_cache_workspace_bytes(const rsa_cache* cache, const rsa_rows* rows, int 
   rc = make_rows(rows, c, true, &r);
   if (rc != RSA_OK) return rc;
   if (group < 0) return RSA_E_RANGE;
-  if (select_ws_bytes) *select_ws_bytes = 0;
+  if (select_ws_bytes) *select_ws_bytes = rsa::cache_select_ws_bytes(c, r, group);
   if (attn_ws_bytes) *attn_ws_bytes = rsa::cache_attn_parts_bytes(c, r, group, 0);
   return RSA_OK;
 }
@@ -134,8 +134,7 @@ int rsa_cache_select(const rsa_cache* cache, const rsa_rows* rows, const void* Q
   if (need < keep) need = keep;
   if (need > c.max_blocks) need = c.max_blocks;
   if (list_len < need) return RSA_E_RANGE;
-  (void)ws_bytes;
-  if (misaligned(ws, 256)) return RSA_E_WORKSPACE;
+  if (ws && (misaligned(ws, 256) || ws_bytes < rsa::cache_select_ws_bytes(c, r, group))) return RSA_E_WORKSPACE;
   rsa::CacheSelectArgs a = {};
   a.Q = (const uint16_t*)Q;
   a.kv_len = kv_len;

@@ -361,34 +361,52 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheDims c, RowDims r,
   }
 }
 
-// Parts of a tile's rows, weighted by their share of the softmax denominator and added in the order of the keys.
+// Parts of a tile's rows, weighted by their share of the softmax denominator and added in the order of the keys. A row
+// takes `lanes` (a power of two) threads to each chunk of eight channels, which share its parts: one thread alone waits for
+// one part after another (24 rows of 43 parts: 28.8 us with one, 5.1 with sixteen).
 template <int D>
-__global__ __launch_bounds__(256) void cache_join_kernel(CacheDims c, RowDims r, CacheAttnArgs a, TileGrid tg, int64_t tiles) {
+__global__ __launch_bounds__(256) void cache_join_kernel(CacheDims c, RowDims r, CacheAttnArgs a, TileGrid tg, int64_t tiles, int lanes) {
   constexpr int CPR = D / 8;
+  __shared__ float add[256][9];
   const int G = r.heads / c.heads_kv;
-  const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int ch = (int)(u % CPR) * 8, rr = (int)(u / CPR % tg.stored);
-  const int64_t id = u / CPR / tg.stored;
-  if (id >= tiles) return;
+  const int tid = threadIdx.x, ch = tid % CPR * 8, sl = tid / CPR % lanes;
+  const int64_t u = (int64_t)blockIdx.x * (256 / CPR / lanes) + tid / CPR / lanes;
+  const int rr = (int)(u % tg.stored);
+  const int64_t id = u / tg.stored;
   const int lrow = (int)(id / tg.per_group), k = (int)(id % tg.per_group);
   const int bh = lrow / a.groups, grp = lrow % a.groups, b = bh / c.heads_kv, hk = bh % c.heads_kv;
   const int t0 = grp * a.group, row = k * tg.rows_per_tile + rr, tok = t0 + row / G;
-  const int ql = a.q_len ? min(a.q_len[b], r.t) : r.t;
-  if (row >= min(a.group, r.t - t0) * G || tok >= ql) return;
-  const int64_t first = id * tg.splits;
-  const float* part_lse = a.parts + tiles * tg.splits * tg.stored * D;
-  float most = -INFINITY;
-  for (int s = 0; s < tg.splits; ++s) most = fmaxf(most, part_lse[(first + s) * tg.stored + rr]);
-  float z[8] = {0, 0, 0, 0, 0, 0, 0, 0}, total = 0.f;
-  for (int s = 0; s < tg.splits; ++s) {
-    const float p = part_lse[(first + s) * tg.stored + rr];
-    const float w = p == -INFINITY ? 0.f : exp2f(p - most);
-    const float* src = a.parts + ((first + s) * tg.stored + rr) * D + ch;
-    const float4 lo = *reinterpret_cast<const float4*>(src), hi = *reinterpret_cast<const float4*>(src + 4);
-    total += w;
-    z[0] += w * lo.x; z[1] += w * lo.y; z[2] += w * lo.z; z[3] += w * lo.w;
-    z[4] += w * hi.x; z[5] += w * hi.y; z[6] += w * hi.z; z[7] += w * hi.w;
+  bool is = id < tiles && row < min(a.group, r.t - t0) * G;
+  if (is) is = tok < (a.q_len ? min(a.q_len[b], r.t) : r.t);
+  float most = -INFINITY, z[8] = {0, 0, 0, 0, 0, 0, 0, 0}, total = 0.f;
+  if (is) {
+    const int64_t first = id * tg.splits;
+    const float* part_lse = a.parts + tiles * tg.splits * tg.stored * D;
+#pragma unroll 4
+    for (int s = 0; s < tg.splits; ++s) most = fmaxf(most, part_lse[(first + s) * tg.stored + rr]);
+    for (int s = sl; s < tg.splits; s += lanes) {
+      const float p = part_lse[(first + s) * tg.stored + rr];
+      const float w = p == -INFINITY ? 0.f : exp2f(p - most);
+      const float* src = a.parts + ((first + s) * tg.stored + rr) * D + ch;
+      const float4 lo = *reinterpret_cast<const float4*>(src), hi = *reinterpret_cast<const float4*>(src + 4);
+      total += w;
+      z[0] += w * lo.x; z[1] += w * lo.y; z[2] += w * lo.z; z[3] += w * lo.w;
+      z[4] += w * hi.x; z[5] += w * hi.y; z[6] += w * hi.z; z[7] += w * hi.w;
+    }
   }
+  if (lanes > 1) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) add[tid][e] = z[e];
+    add[tid][8] = total;
+    __syncthreads();
+    if (sl > 0) return;
+    for (int x = 1; x < lanes; ++x) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] += add[tid + x * CPR][e];
+      total += add[tid + x * CPR][8];
+    }
+  }
+  if (!is) return;
   const float inv = total == 0.f ? 0.f : 1.f / total;
   const uint4 v = make_uint4(pack_bf16x2(z[0] * inv, z[1] * inv), pack_bf16x2(z[2] * inv, z[3] * inv),
                              pack_bf16x2(z[4] * inv, z[5] * inv), pack_bf16x2(z[6] * inv, z[7] * inv));
@@ -429,8 +447,10 @@ hipError_t launch_t(const CacheDims& c, const RowDims& r, const CacheAttnArgs& a
   else hipLaunchKernelGGL((cache_attn_kernel<D, BLK, 2>), grid, block, 0, s, c, r, a, p.grid);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.grid.splits == 1) return e;
-  const int64_t threads = p.tiles * p.grid.stored * (D / 8);
-  hipLaunchKernelGGL((cache_join_kernel<D>), dim3((uint32_t)((threads + 255) / 256)), block, 0, s, c, r, a, p.grid, p.tiles);
+  int lanes = 1;
+  while (lanes < p.grid.splits && lanes < 256 / (D / 8)) lanes *= 2;
+  const int64_t per_wg = 256 / (D / 8) / lanes, rows = p.tiles * p.grid.stored;
+  hipLaunchKernelGGL((cache_join_kernel<D>), dim3((uint32_t)((rows + per_wg - 1) / per_wg)), block, 0, s, c, r, a, p.grid, p.tiles, lanes);
   return hipGetLastError();
 }
 

@@ -49,6 +49,45 @@ __device__ __forceinline__ int v_code_offset(int t, int ch) {
   return ((((t >> 6) * (D / 16) + (ch >> 4)) * 4 + ((t & 15) >> 2)) * 16 + (ch & 15)) * 16 + ((t & 63) >> 4) * 4 + (t & 3);
 }
 
+// Values of other lanes by the vector ALU alone (through LDS, as __shfl does it, each exchange waits some 100 cycles, and
+// the small calls of the cache are little else). Lanes of a row of 16, by control word:
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kFlip8 = 0x141 /* lane i and i ^ 7 */, kFlip16 = 0x140 /* i ^ 15 */, kXor8 = 0x128;
+template <int CTRL>
+__device__ __forceinline__ int row_lane(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xf, 0xf, true); }
+// op of a value with that of lane ^ 16 / lane ^ 32.
+template <class Op>
+__device__ __forceinline__ int with_xor16(int x, Op op) {
+  const auto r = __builtin_amdgcn_permlane16_swap((uint32_t)x, (uint32_t)x, false, false);
+  return op((int)r[0], (int)r[1]);
+}
+template <class Op>
+__device__ __forceinline__ int with_xor32(int x, Op op) {
+  const auto r = __builtin_amdgcn_permlane32_swap((uint32_t)x, (uint32_t)x, false, false);
+  return op((int)r[0], (int)r[1]);
+}
+// op over all lanes of a row of 16 / of the wave, in every lane (op is commutative and associative).
+template <class Op>
+__device__ __forceinline__ int over_row(int x, Op op) {
+  x = op(x, row_lane<kXor1>(x));
+  x = op(x, row_lane<kXor2>(x));
+  x = op(x, row_lane<kFlip8>(x));
+  return op(x, row_lane<kFlip16>(x));
+}
+template <class Op>
+__device__ __forceinline__ int over_wave(int x, Op op) { return with_xor32(with_xor16(over_row(x, op), op), op); }
+struct AddInt { __device__ __forceinline__ int operator()(int a, int b) const { return a + b; } };
+struct MaxU32 { __device__ __forceinline__ int operator()(int a, int b) const { return (int)max((uint32_t)a, (uint32_t)b); } };
+struct AddF32 {
+  __device__ __forceinline__ int operator()(int a, int b) const {
+    return __builtin_bit_cast(int, __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b));
+  }
+};
+struct MaxF32 {
+  __device__ __forceinline__ int operator()(int a, int b) const {
+    return __builtin_bit_cast(int, fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)));
+  }
+};
+
 struct CacheWriteArgs {
   const uint16_t *K, *V;
   const int32_t *start, *count;   // [batch]; count may be NULL (all t)
@@ -67,8 +106,10 @@ struct CacheSelectArgs {
   int group, groups, keep, first, last, list_len;
   bool causal;
   int32_t *block_idx, *kept;
-  void* ws;
+  void* ws;                       // NULL: scores and choice in one launch
 };
+// Bytes of `ws` (0: none is used).
+size_t cache_select_ws_bytes(const CacheDims& c, const RowDims& r, int group);
 hipError_t launch_cache_select(const CacheDims& c, const RowDims& r, const CacheSelectArgs& a, hipStream_t s);
 
 struct CacheAttnArgs {

@@ -8,6 +8,8 @@
 // One workgroup per (block of tokens that the call touches, sequence, key/value head), for K and V: the largest magnitude of
 // the new tokens decides the two exponents, so all rows of the block are in registers before the first code is made. The
 // codes go through LDS, where they are put in page order (cache_common.hpp), and leave in 16-byte pieces.
+#include <type_traits>
+
 #include "cache_common.hpp"
 
 namespace rsa {
@@ -103,6 +105,25 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheDims c, RowDims r
         if (mine && slot >= sp.lo && slot < sp.hi) x[w][p][i] = *reinterpret_cast<const uint4*>(X + slot * r.st);
       }
   }
+  // what the block holds already (its first `lo` slots): 16-byte pieces tid, tid + 256, ...
+  constexpr int PPT = PIECES / 256 > 0 ? PIECES / 256 : 1;
+  const int prow = tid % 16, pg = tid / 16 % 4;    // of all pieces of a thread: key of 16 (K) or channel of 16 (V), and g
+  uint4 was[2][PPT];
+  float held_scale[2] = {1.f, 1.f};
+  if (sp.lo > 0) {
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      held_scale[w] = c.scales[rec * 4 + w];
+      const uint8_t* src = (w == 0 ? c.k : c.v) + rec * (BLK * D);
+#pragma unroll
+      for (int u = 0; u < PPT; ++u) {
+        const int pc = tid + u * 256;
+        const int first = w == 0 ? pc / D * 16 + prow : pc / (4 * D) * 64 + 4 * pg;   // its lowest token
+        was[w][u] = make_uint4(0, 0, 0, 0);
+        if (pc < PIECES && first < sp.lo) was[w][u] = *reinterpret_cast<const uint4*>(src + pc * 16);
+      }
+    }
+  }
   if (tid < D) sums[tid] = 0;
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
@@ -110,8 +131,7 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheDims c, RowDims r
     for (int p = 0; p < NP; ++p)
 #pragma unroll
       for (int i = 0; i < 4; ++i) big[w] = finite_max(big[w], x[w][p][i]);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) big[w] = max(big[w], (uint32_t)__shfl_xor((int)big[w], o));
+    big[w] = (uint32_t)over_wave((int)big[w], MaxU32());
     if (tid % 64 == 0) red[w][tid / 64] = big[w];
   }
   __syncthreads();
@@ -119,45 +139,56 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheDims c, RowDims r
 #pragma unroll
   for (int w = 0; w < 2; ++w) e[w] = code_exponent(max(max(red[w][0], red[w][1]), max(red[w][2], red[w][3])));
 
-  // what the block holds already (its first `lo` slots), moved to the larger scale where the new tokens ask for one
+  // the older tokens, moved to the larger scale where the new ones ask for it
   if (sp.lo > 0) {
+    int part[16] = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};      // K: sums of 16 channels (the same for all pieces of a thread)
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-      const int held = min(max(exponent_of(c.scales[rec * 4 + w]), -126), 120);
+      const int held = min(max(exponent_of(held_scale[w]), -126), 120);
       const float down = exp2_int(max(held - max(held, e[w]), -126));
       e[w] = max(e[w], held);
-      const uint8_t* src = (w == 0 ? c.k : c.v) + rec * (BLK * D);
-      for (int pc = tid; pc < PIECES; pc += 256) {
-        const int row = pc % 16, g = pc / 16 % 4;
-        const int t64 = pc / (4 * D) * 64, key = pc / D * 16 + row;        // V: 64 keys are 4 D pieces; K: 16 keys D pieces
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (w == 0 ? key < sp.lo : t64 + 4 * g < sp.lo) v = *reinterpret_cast<const uint4*>(src + pc * 16);
-        uint32_t q[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int u = 0; u < PPT; ++u) {
+        const int pc = tid + u * 256;
+        uint32_t q[4] = {was[w][u].x, was[w][u].y, was[w][u].z, was[w][u].w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float f[4];
-          from_codes(q[i], f);
           if (w == 1) {                                                  // dword i: keys t64 + 16 i + 4 g .. + 3 of a channel
-            const int k0 = t64 + 16 * i + 4 * g;
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-              if (k0 + u >= sp.lo) { f[u] = 0.f; q[i] &= ~(255u << (8 * u)); }
+            const int old = sp.lo - (pc / (4 * D) * 64 + 16 * i + 4 * pg);
+            q[i] &= old <= 0 ? 0u : old >= 4 ? 0xffffffffu : 0xffffffffu >> (32 - 8 * old);
           }
           if (down != 1.f) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u) f[u] *= down;
-            q[i] = to_codes(f);
+            float f[4];
             from_codes(q[i], f);
-          }
-          if (w == 0 && key < sp.lo) {
-            const int ch = pc / 64 % (D / 64) * 64 + g * 16 + i * 4;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) atomicAdd(&sums[ch + u], code_units(f[u]));
+            for (int x = 0; x < 4; ++x) f[x] *= down;
+            q[i] = to_codes(f);
+          }
+          if (w == 0) {
+            float f[4];
+            from_codes(q[i], f);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) part[4 * i + x] += code_units(f[x]);
           }
         }
-        *reinterpret_cast<uint4*>(&codes[w][pc * 16]) = make_uint4(q[0], q[1], q[2], q[3]);
+        if (pc < PIECES) *reinterpret_cast<uint4*>(&codes[w][pc * 16]) = make_uint4(q[0], q[1], q[2], q[3]);
       }
     }
+    // over the 16 keys that the lanes of a row hold: each exchange halves the channels that a lane is left with
+    auto halve = [&](auto ctrl, int o) __attribute__((always_inline)) {
+      const bool up = (prow & o) != 0;
+#pragma unroll
+      for (int x = 0; x < 8; ++x)
+        if (x < o) {
+          const int keep = up ? part[x + o] : part[x], give = up ? part[x] : part[x + o];
+          part[x] = keep + row_lane<decltype(ctrl)::value>(give);
+        }
+    };
+    halve(std::integral_constant<int, kXor8>{}, 8);
+    halve(std::integral_constant<int, kFlip8>{}, 4);
+    halve(std::integral_constant<int, kXor2>{}, 2);
+    halve(std::integral_constant<int, kXor1>{}, 1);
+    if (tid < PIECES) atomicAdd(&sums[tid / 64 % (D / 64) * 64 + pg * 16 + prow], part[0]);
     __syncthreads();
   }
 
@@ -170,6 +201,8 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheDims c, RowDims r
 #pragma unroll
       for (int p = 0; p < NP; ++p) {
         const int slot0 = (p * QUADS + quad) * 4;
+        // (a block begun before has its zeros and older codes in place: one token costs one wave its conversion, not all)
+        if (sp.lo > 0 && (slot0 >= sp.hi || slot0 + 4 <= sp.lo)) continue;
         uint32_t cd[8];                             // by channel: byte i = token slot0 + i
 #pragma unroll
         for (int q = 0; q < 4; ++q) {               // channels 2 q, 2 q + 1
@@ -216,7 +249,11 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheDims c, RowDims r
       }
     }
 #pragma unroll
-    for (int ch = 0; ch < 8; ++ch) atomicAdd(&sums[cc * 8 + ch], part[ch]);
+    for (int ch = 0; ch < 8; ++ch) {                // over the runs of tokens of this wave
+      if (CPR == 8) part[ch] += row_lane<kXor8>(part[ch]);
+      part[ch] = with_xor32(with_xor16(part[ch], AddInt()), AddInt());
+      if (tid % 64 < CPR && part[ch]) atomicAdd(&sums[cc * 8 + ch], part[ch]);
+    }
   }
   __syncthreads();
 #pragma unroll
@@ -226,12 +263,11 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheDims c, RowDims r
   }
 
   // the mean of the block's keys in 8 bits: sums are exact, the division is the one rounding before the code's own
-  if (tid < 64) {
-    uint32_t most = 0;
+  if (tid < D) {
+    uint32_t most = 0;                              // of all channels, in each wave
 #pragma unroll
-    for (int ch = tid; ch < D; ch += 64) most = max(most, (uint32_t)abs(sums[ch]));
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o));
+    for (int ch = tid % 64; ch < D; ch += 64) most = max(most, (uint32_t)abs(sums[ch]));
+    most = (uint32_t)over_wave((int)most, MaxU32());
     const double n = (double)sp.hi;
     int em = -100;
     if (most) {
@@ -239,9 +275,7 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheDims c, RowDims r
       const double m = frexp((double)most / n, &xp);
       em = max(xp - 7 + (m > 127.0 / 128.0 ? 1 : 0) + e[0] - 9, -100);
     }
-#pragma unroll
-    for (int ch = tid; ch < D; ch += 64)
-      c.mean[rec * D + ch] = (int8_t)(int)rint(ldexp((double)sums[ch] / n, e[0] - 9 - em));
+    c.mean[rec * D + tid] = (int8_t)(int)rint(ldexp((double)sums[tid] / n, e[0] - 9 - em));
     if (tid == 0) *reinterpret_cast<float4*>(c.scales + rec * 4) = make_float4(exp2_int(e[0]), exp2_int(e[1]), exp2_int(em), 0.f);
   }
 }

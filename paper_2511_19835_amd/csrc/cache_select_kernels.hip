@@ -4,9 +4,11 @@
 // power-of-two scale (that of q8 is common to a row and left out). The dot product is integer work and the scale moves no
 // bit, so a score is exact, equal scores are equal, and the choice does not depend on an order of sums.
 //
-// One workgroup per (sequence, key/value head, group): sum of the queries (fp64: exact for bf16 terms within 40 binades of
-// each other), scores of all blocks into LDS as order-preserving keys, the threshold key by four passes over eight bits
-// each, and the kept blocks in ascending order.
+// One workgroup per row = (sequence, key/value head, group): the sum of the queries (fp64: exact for bf16 terms within 40
+// binades of each other), the scores of all blocks as order-preserving keys, the threshold key bit by bit with ballot
+// counts (keys in registers, each wave owning a run of blocks), and the kept blocks in ascending order. What bounds it is
+// latency: five loads that wait for one another, and the search. Where there are few rows and many blocks the scores are
+// a launch of their own, in runs of blocks over many workgroups.
 #include "cache_common.hpp"
 
 namespace rsa {
@@ -16,196 +18,411 @@ __device__ __forceinline__ uint32_t ordered_key(float x) {
   const uint32_t u = __builtin_bit_cast(uint32_t, x);
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
+__device__ __forceinline__ float score_of(uint32_t key) {
+  return __builtin_bit_cast(float, (key & 0x80000000u) ? key & 0x7fffffffu : ~key);
+}
+// The value of the lane N before in its row of 16, 0 where there is none.
+template <int N>
+__device__ __forceinline__ int row_up(int x) { return __builtin_amdgcn_update_dpp(0, x, 0x110 + N, 0xf, 0xf, true); }
 __device__ __forceinline__ double finite_or_zero(uint32_t bits16) {
   return (bits16 & 0x7f80u) == 0x7f80u ? 0.0 : (double)bf16_bits_to_float(bits16);
 }
-constexpr uint32_t kUnseen = 0u, kForced = 0xffffffffu;   // below and above every score
+constexpr uint32_t kUnseen = 0u;                   // below every score
+constexpr float kLargest = 3.4028234663852886e38f;
+constexpr uint32_t kLowest = 0x00800000u;          // key of -kLargest, also of what is no number (a page that was never written)
+constexpr int kRunBlocks = 1024;                   // blocks that a workgroup of the scoring launch takes
 
-// Sum of an int over the workgroup's threads before this one, and over all of them; `red`: 4 ints.
-__device__ __forceinline__ int scan_threads(int v, int* red, int* all) {
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  int in = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int up = __shfl_up(in, o);
-    if (lane >= o) in += up;
-  }
-  __syncthreads();
-  if (lane == 63) red[wave] = in;
-  __syncthreads();
-  int before = 0, total = 0;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    if (w < wave) before += red[w];
-    total += red[w];
-  }
-  *all = total;
-  return before + in - v;
+struct Row {
+  int b, hk, G;
+  int t0, t1;                                      // its tokens
+  int seen;                                        // blocks that may be chosen: [0, seen)
+  int lo_forced, hi_forced;                        // forced beside those below `first`
+};
+__device__ __forceinline__ Row row_of(const CacheDims& c, const RowDims& r, const CacheSelectArgs& a, int row) {
+  Row w;
+  const int grp = row % a.groups, bh = row / a.groups;
+  w.b = bh / c.heads_kv;
+  w.hk = bh % c.heads_kv;
+  w.G = r.heads / c.heads_kv;
+  const int shift = c.blk == 128 ? 7 : 6;          // (a shift of a negative position rounds down)
+  const int64_t kv = a.kv_len[w.b];
+  const int ql = a.q_len ? min(a.q_len[w.b], r.t) : r.t;
+  w.t0 = grp * a.group;
+  w.t1 = min(w.t0 + a.group, ql);
+  const int64_t p0 = kv - ql + w.t0, p1 = kv - ql + w.t1 - 1;              // positions of the first and the last
+  int64_t seen = a.causal ? max((p1 >> shift) + 1, (int64_t)0) : (kv + c.blk - 1) >> shift;
+  if (w.t1 <= w.t0 || kv <= 0) seen = 0;
+  w.seen = (int)min(seen, (int64_t)c.max_blocks);
+  w.lo_forced = a.last > 0 ? (int)max((int64_t)0, (p0 >> shift) - a.last + 1) : 0x7fffffff;
+  w.hi_forced = a.last > 0 ? (int)(p1 >> shift) : -1;
+  return w;
 }
 
 template <int D>
-__global__ __launch_bounds__(256) void cache_select_kernel(CacheDims c, RowDims r, CacheSelectArgs a) {
+struct QueryLds {
+  double sums[256 / (D / 8)][D];
+  uint32_t most[2];
+  __align__(16) int8_t q8[D];
+};
+// A chunk of the queries of a row: eight rows of every stripe.
+constexpr int kQueryRows = 8;
+template <int D>
+__device__ __forceinline__ void request_queries(const RowDims& r, const CacheSelectArgs& a, const Row& w, int from, uint4 (&v)[kQueryRows]) {
   constexpr int CPR = D / 8, STRIPES = 256 / CPR;
-  extern __shared__ uint32_t keys[];               // [max_blocks]
-  __shared__ double qs[STRIPES][D];
-  __shared__ __align__(16) int8_t q8[D];
-  __shared__ uint32_t hist[256];
-  __shared__ int red[4];
-  __shared__ uint32_t pick[2];
-  const int tid = threadIdx.x;
-  const int grp = blockIdx.x % a.groups, bh = blockIdx.x / a.groups;
-  const int b = bh / c.heads_kv, hk = bh % c.heads_kv, G = r.heads / c.heads_kv;
-  const int64_t row = (int64_t)bh * a.groups + grp;
-  int32_t* list = a.block_idx + row * a.list_len;
+  const int cc = threadIdx.x % CPR, rows = (w.t1 - w.t0) * w.G;
+  const uint16_t* Q = a.Q + (int64_t)w.b * r.sb + (int64_t)w.hk * w.G * r.sh + (int64_t)w.t0 * r.st + cc * 8;
+  int i = from + (int)threadIdx.x / CPR, tok = i / w.G, head = i - tok * w.G;
+  const int dt = STRIPES / w.G, dh = STRIPES - dt * w.G;       // (a division a row would take longer than the load)
+#pragma unroll
+  for (int u = 0; u < kQueryRows; ++u) {
+    v[u] = make_uint4(0, 0, 0, 0);
+    if (i < rows) v[u] = *reinterpret_cast<const uint4*>(Q + head * r.sh + tok * r.st);
+    i += STRIPES;
+    tok += dt;
+    head += dh;
+    if (head >= w.G) { head -= w.G; ++tok; }
+  }
+}
+// The row's query in 8 bits, into L.q8 (ends with a barrier); `v`: the first chunk, requested earlier.
+template <int D>
+__device__ __forceinline__ void sum_queries(const RowDims& r, const CacheSelectArgs& a, const Row& w, uint4 (&v)[kQueryRows], QueryLds<D>& L) {
+  constexpr int CPR = D / 8, STRIPES = 256 / CPR;
+  const int tid = threadIdx.x, cc = tid % CPR;
+  double acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  const int rows = (w.t1 - w.t0) * w.G;
+  for (int from = 0; from < rows; from += kQueryRows * STRIPES) {
+    if (from > 0) request_queries<D>(r, a, w, from, v);
+#pragma unroll
+    for (int u = 0; u < kQueryRows; ++u) {
+      if (from + u * STRIPES >= rows) break;
+      const uint32_t x[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        acc[2 * e] += finite_or_zero(x[e] & 0xffffu);
+        acc[2 * e + 1] += finite_or_zero(x[e] >> 16);
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) L.sums[tid / CPR][cc * 8 + e] = acc[e];
+  __syncthreads();
+  if (tid < D) {
+    const int stripes = min(rows, STRIPES);        // the others hold zeros
+    double s = 0;
+#pragma unroll 4
+    for (int x = 0; x < stripes; ++x) s += L.sums[x][tid];
+    // the least e with max|s| <= 127 * 2^e: by the largest exponent x (max < 2^x), and whether anything passes 127 * 2^(x-7)
+    const uint32_t top = (uint32_t)(__builtin_bit_cast(uint64_t, s) >> 52) & 0x7ffu;
+    const uint32_t most = (uint32_t)over_wave((int)top, MaxU32());
+    if (tid % 64 == 0) L.most[tid / 64] = most;
+    L.sums[0][tid] = s;                            // (column tid is this thread's own)
+  }
+  __syncthreads();
+  if (tid < D) {
+    const int x = (int)max(L.most[0], L.most[D / 64 - 1]) - 1022;
+    bool over = false;
+#pragma unroll
+    for (int ch = tid % 64; ch < D; ch += 64) over |= fabs(L.sums[0][ch]) > ldexp(127.0, x - 7);
+    const int e = max(x - 7 + (__any(over) ? 1 : 0), -100);
+    L.q8[tid] = (int8_t)(int)rint(ldexp(L.sums[0][tid], -e));
+  }
+  __syncthreads();
+}
 
-  int64_t kv = a.kv_len[b];
-  int64_t ql = a.q_len ? a.q_len[b] : r.t;
-  if (ql > r.t) ql = r.t;
-  const int64_t t0 = (int64_t)grp * a.group, t1 = min(t0 + a.group, ql);   // tokens of the group
-  const int64_t p0 = kv - ql + t0, p1 = kv - ql + t1 - 1;                  // their positions
-  int64_t seen64 = a.causal ? (p1 < 0 ? 0 : p1 / c.blk + 1) : (kv + c.blk - 1) / c.blk;
-  if (t1 <= t0 || kv <= 0) seen64 = 0;
-  const int seen = (int)min(seen64, (int64_t)c.max_blocks);
-  if (seen <= 0) {                                 // nothing to choose from (the whole workgroup)
+// The means of a round of blocks, on their way: 16 channels to a lane, kRound passes requested together (pages lie
+// anywhere, so that a round of loads waits some 2500 cycles).
+constexpr int kRound = 16;
+struct Means {
+  int page[kRound];
+  int4 k[kRound];
+  float scale[kRound];
+};
+template <int D>
+__device__ __forceinline__ void request_means(const CacheDims& c, const Row& w, int from, int to, Means& x) {
+  constexpr int LPB = D / 16, BPP = 256 / LPB;     // lanes to a block, blocks to a pass
+  const int m0 = from + (int)threadIdx.x / LPB;
+#pragma unroll
+  for (int u = 0; u < kRound; ++u) x.page[u] = m0 + u * BPP < to ? cache_page(c, w.b, m0 + u * BPP) : -1;
+#pragma unroll
+  for (int u = 0; u < kRound; ++u) {
+    x.k[u] = make_int4(0, 0, 0, 0);
+    x.scale[u] = 0.f;
+    if (x.page[u] >= 0) {
+      const int64_t rec = (int64_t)x.page[u] * c.heads_kv + w.hk;
+      x.k[u] = *reinterpret_cast<const int4*>(c.mean + rec * D + threadIdx.x % LPB * 16);
+      x.scale[u] = c.scales[rec * 4 + 2];
+    }
+  }
+}
+// Keys of blocks [from, to) of the row into keys[0 ..); `x`: the first round, requested earlier.
+template <int D>
+__device__ __forceinline__ void score_blocks(const CacheDims& c, const Row& w, const int8_t* q8, int from, int to, Means& x, uint32_t* keys) {
+  constexpr int LPB = D / 16, BPP = 256 / LPB;
+  const int part = threadIdx.x % LPB;
+  const int4 q = *reinterpret_cast<const int4*>(&q8[part * 16]);
+  for (int at = from; at < to; at += kRound * BPP) {
+    if (at > from) request_means<D>(c, w, at, to, x);
+#pragma unroll
+    for (int u = 0; u < kRound; ++u) {
+      const int m = at + u * BPP + (int)threadIdx.x / LPB;
+      int dot = __builtin_amdgcn_sdot4(q.x, x.k[u].x, 0, false);
+      dot = __builtin_amdgcn_sdot4(q.y, x.k[u].y, dot, false);
+      dot = __builtin_amdgcn_sdot4(q.z, x.k[u].z, dot, false);
+      dot = __builtin_amdgcn_sdot4(q.w, x.k[u].w, dot, false);
+      dot += row_lane<kXor1>(dot);
+      dot += row_lane<kXor2>(dot);
+      if (LPB == 8) dot += row_lane<kFlip8>(dot);
+      // 2^-22 keeps the largest scale finite; the product is exact (|dot| < 2^21)
+      const float z = (float)dot * 0x1p-22f * x.scale[u];
+      if (part == 0 && m < to) keys[m - from] = x.page[u] < 0 ? kUnseen : fabsf(z) <= kLargest ? ordered_key(z) : kLowest;
+    }
+  }
+}
+
+// Workgroups go round the eight XCDs in turn; numbered like this, those of an XCD take rows that follow one another: the
+// heads of a sequence, whose scales share lines, and the groups of a head, which read the same means.
+__device__ __forceinline__ int xcd_run(int id, int all) {
+  const int x = id % 8, per = all / 8, more = all % 8;
+  return x * per + min(x, more) + id / 8;
+}
+
+// Scores of a run of blocks, for rows that are few.
+template <int D>
+__global__ __launch_bounds__(256) void cache_score_kernel(CacheDims c, RowDims r, CacheSelectArgs a, int runs) {
+  __shared__ QueryLds<D> L;
+  __shared__ uint32_t keys[kRunBlocks];
+  const int id = xcd_run(blockIdx.x, gridDim.x), row = id / runs;
+  const Row w = row_of(c, r, a, row);
+  const int from = id % runs * kRunBlocks, to = min(from + kRunBlocks, w.seen);
+  if (from >= to) return;
+  uint4 q[kQueryRows];
+  Means x;
+  request_queries<D>(r, a, w, 0, q);
+  request_means<D>(c, w, from, to, x);
+  sum_queries<D>(r, a, w, q, L);
+  score_blocks<D>(c, w, L.q8, from, to, x, keys);
+  __syncthreads();
+  uint32_t* out = (uint32_t*)a.ws + (int64_t)row * c.max_blocks;
+  for (int m = from + (int)threadIdx.x; m < to; m += 256) out[m] = keys[m - from];
+}
+
+// NI keys to a thread (rows of up to 256 NI blocks); SCORED: the keys are in the workspace.
+template <int D, int NI, bool SCORED>
+__global__ __launch_bounds__(256) void cache_select_kernel(CacheDims c, RowDims r, CacheSelectArgs a) {
+  __shared__ QueryLds<D> L;
+  __shared__ uint32_t keys[SCORED ? 1 : 256 * NI];
+  __shared__ __align__(16) int counts[2][4][4];
+  __shared__ int totals[3][4];
+  __shared__ uint32_t ends[2][4], few[64];
+  __shared__ __align__(16) int hist[256];
+  __shared__ int n_few;
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const int row = xcd_run(blockIdx.x, gridDim.x);
+  const Row w = row_of(c, r, a, row);
+  int32_t* list = a.block_idx + (int64_t)row * a.list_len;
+  if (w.seen <= 0) {                               // nothing to choose from (the whole workgroup)
     for (int i = tid; i < a.list_len; i += 256) list[i] = -1;
     if (tid == 0) a.kept[row] = 0;
     return;
   }
-
-  // the group's query, in 8 bits
-  {
-    const int cc = tid % CPR, stripe = tid / CPR;
-    double acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    const int rows = (int)(t1 - t0) * G;
-    for (int i = stripe; i < rows; i += STRIPES) {
-      const uint4 v = *reinterpret_cast<const uint4*>(a.Q + (int64_t)b * r.sb + (int64_t)(hk * G + i % G) * r.sh + (t0 + i / G) * r.st + cc * 8);
-      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        acc[2 * e] += finite_or_zero(w[e] & 0xffffu);
-        acc[2 * e + 1] += finite_or_zero(w[e] >> 16);
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) qs[stripe][cc * 8 + e] = acc[e];
-    __syncthreads();
-    if (tid < D) {
-      double s = 0;
-      for (int i = 0; i < STRIPES; ++i) s += qs[i][tid];
-      qs[0][tid] = s;
-    }
-    __syncthreads();
-    if (tid < 64) {
-      double most = 0;
-      for (int ch = tid; ch < D; ch += 64) most = fmax(most, fabs(qs[0][ch]));
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) most = fmax(most, __shfl_xor(most, o));
-      int e = -100;
-      if (most > 0) {
-        int xp;
-        const double m = frexp(most, &xp);
-        e = max(xp - 7 + (m > 127.0 / 128.0 ? 1 : 0), -100);
-      }
-      for (int ch = tid; ch < D; ch += 64) q8[ch] = (int8_t)(int)rint(ldexp(qs[0][ch], -e));
-    }
+  if (!SCORED) {
+    uint4 q[kQueryRows];
+    Means x;
+    request_queries<D>(r, a, w, 0, q);
+    request_means<D>(c, w, 0, w.seen, x);
+    sum_queries<D>(r, a, w, q, L);
+    score_blocks<D>(c, w, L.q8, 0, w.seen, x, keys);
     __syncthreads();
   }
-
-  // keys of the blocks
-  const int lo_forced = a.last > 0 ? (int)max((int64_t)0, p0 / c.blk - (p0 < 0 && p0 % c.blk ? 1 : 0) - a.last + 1) : 0x7fffffff;
-  const int hi_forced = a.last > 0 && p1 >= 0 ? (int)(p1 / c.blk) : -1;
-  int n_seen = 0, n_forced = 0;
-  {
-    constexpr int LPB = D / 16;                    // lanes to a block: 16 channels each
-    const int part = tid % LPB;
-    const int4 q = *reinterpret_cast<const int4*>(&q8[part * 16]);
-    for (int m0 = 0; m0 < seen; m0 += 256 / LPB) {
-      const int m = m0 + tid / LPB;
-      const int page = m < seen ? cache_page(c, b, m) : -1;
-      int dot = 0;
-      float scale = 0.f;
-      if (page >= 0) {
-        const int64_t rec = (int64_t)page * c.heads_kv + hk;
-        const int4 k = *reinterpret_cast<const int4*>(c.mean + rec * D + part * 16);
-        scale = c.scales[rec * 4 + 2];
-        dot = __builtin_amdgcn_sdot4(q.x, k.x, dot, false);
-        dot = __builtin_amdgcn_sdot4(q.y, k.y, dot, false);
-        dot = __builtin_amdgcn_sdot4(q.z, k.z, dot, false);
-        dot = __builtin_amdgcn_sdot4(q.w, k.w, dot, false);
-      }
+  // this wave's run of blocks, slot i of lane l being block m0 + 64 i + l
+  const int m0 = wave * 64 * NI;
+  const uint32_t* src = SCORED ? (const uint32_t*)a.ws + (int64_t)row * c.max_blocks : keys;
+  uint32_t key[NI];
+  unsigned long long must = 0;                     // bit i: slot i is forced
+  int n_seen = 0, n_must = 0;
+  uint32_t kmax = 0, nkmin = 0;                    // over the blocks that scores decide on
 #pragma unroll
-      for (int o = 1; o < LPB; o <<= 1) dot += __shfl_xor(dot, o);
-      if (part == 0 && m < seen) {
-        // 2^-22 keeps the largest scale finite; the product is exact (|dot| < 2^21)
-        uint32_t key = ordered_key((float)dot * 0x1p-22f * scale);
-        const bool forced = m < a.first || (m >= lo_forced && m <= hi_forced);
-        if (forced) key = kForced;
-        key = page < 0 ? kUnseen : max(key, kUnseen + 1);
-        keys[m] = key;
-        n_seen += page >= 0;
-        n_forced += page >= 0 && forced;
-      }
+  for (int i = 0; i < NI; ++i) {
+    const int m = m0 + 64 * i + lane;
+    key[i] = m < w.seen ? src[m] : kUnseen;
+    const bool there = key[i] != kUnseen, forced = there && (m < a.first || (m >= w.lo_forced && m <= w.hi_forced));
+    n_seen += __popcll(__ballot(there));
+    n_must += __popcll(__ballot(forced));
+    if (forced) {
+      must |= 1ull << i;
+      key[i] = kUnseen;
     }
+    kmax = max(kmax, key[i]);
+    nkmin = max(nkmin, key[i] != kUnseen ? ~key[i] : 0u);
   }
-  int all_seen, all_forced;
-  scan_threads(n_seen, red, &all_seen);
-  scan_threads(n_forced, red, &all_forced);        // (its barriers also publish the keys)
-  const int want = min(min(max(a.keep, all_forced), all_seen), a.list_len);
+  kmax = (uint32_t)over_wave((int)kmax, MaxU32());
+  nkmin = (uint32_t)over_wave((int)nkmin, MaxU32());
+  hist[tid] = 0;
+  if (tid == 0) n_few = 0;
+  if (lane == 0) {
+    totals[0][wave] = n_seen;
+    totals[1][wave] = n_must;
+    ends[0][wave] = kmax;
+    ends[1][wave] = nkmin;
+  }
+  __syncthreads();
+  n_seen = totals[0][0] + totals[0][1] + totals[0][2] + totals[0][3];
+  n_must = totals[1][0] + totals[1][1] + totals[1][2] + totals[1][3];
+  kmax = max(max(ends[0][0], ends[0][1]), max(ends[0][2], ends[0][3]));
+  const uint32_t kmin = ~max(max(ends[1][0], ends[1][1]), max(ends[1][2], ends[1][3]));
+  const int want = min(max(a.keep, n_must), n_seen);
+  const int by_score = want - n_must;
 
-  // the want-th largest key, eight bits at a time
-  uint32_t tau = 0;
-  int left = want;                                 // how many of the keys with the prefix found so far are wanted
-  for (int shift = 24; shift >= 0 && want > 0; shift -= 8) {
-    hist[tid] = 0;
+  // The by_score-th largest key `tau`; kept: key > tau, and `ties` of those equal to it. First a histogram of 256 even steps
+  // between the lowest and the highest score, which leaves a few keys to be ranked against each other; where it leaves more
+  // than a wave has lanes (equal scores, scales far apart), bit by bit with ballot counts.
+  uint32_t tau = 0xffffffffu;
+  int ties = 0;
+  if (by_score > 0) {
+    const float smin = score_of(kmin), range = score_of(kmax) - smin;
+    const float steps = range > 0.f && range <= kLargest ? 255.f / range : 0.f;
+    auto step_of = [&](uint32_t k) __attribute__((always_inline)) { return (int)((score_of(k) - smin) * steps); };   // monotone
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      if (key[i] != kUnseen) atomicAdd(&hist[step_of(key[i])], 1);
     __syncthreads();
-    for (int m = tid; m < seen; m += 256) {
-      const uint32_t k = keys[m];
-      if (shift == 24 || (k >> (shift + 8)) == (tau >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+    // in every wave: lane l has steps 255 - 4 l down to 252 - 4 l
+    const int4 h = *reinterpret_cast<const int4*>(&hist[252 - 4 * lane]);
+    const int four = h.x + h.y + h.z + h.w;
+    int upto = four;
+    upto += row_up<1>(upto);
+    upto += row_up<2>(upto);
+    upto += row_up<4>(upto);
+    upto += row_up<8>(upto);
+    const int r0 = __builtin_amdgcn_readlane(upto, 15), r1 = __builtin_amdgcn_readlane(upto, 31), r2 = __builtin_amdgcn_readlane(upto, 47);
+    upto += (lane >= 16 ? r0 : 0) + (lane >= 32 ? r1 : 0) + (lane >= 48 ? r2 : 0);
+    const int at = __builtin_ctzll(__ballot(upto >= by_score));          // (the last lane counts all keys)
+    int above = __builtin_amdgcn_readlane(upto - four, at), step = 255 - 4 * at, n = 0;
+    const int h3[4] = {__builtin_amdgcn_readlane(h.w, at), __builtin_amdgcn_readlane(h.z, at), __builtin_amdgcn_readlane(h.y, at),
+                       __builtin_amdgcn_readlane(h.x, at)};
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      if (n == 0 && above + h3[x] >= by_score) {
+        step -= x;
+        n = h3[x];
+      } else if (n == 0) {
+        above += h3[x];
+      }
+    if (n <= 64) {                                 // n keys share the step that holds tau (the same in every wave)
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+        if (key[i] != kUnseen && step_of(key[i]) == step) few[atomicAdd(&n_few, 1)] = key[i];
+      __syncthreads();
+      const uint32_t mine = lane < n ? few[lane] : kUnseen;              // (their order does not matter)
+      int more = 0, same = 0;
+      for (int x = 0; x < n; ++x) {
+        const uint32_t other = (uint32_t)__builtin_amdgcn_readlane((int)mine, x);
+        more += other > mine;
+        same += other == mine;
+      }
+      const int need = by_score - above;
+      const int who = __builtin_ctzll(__ballot(lane < n && more < need && more + same >= need));
+      tau = (uint32_t)__builtin_amdgcn_readlane((int)mine, who);
+      ties = need - __builtin_amdgcn_readlane(more, who);
+    } else {
+      // from the highest bit in which keys of the row differ down; done as soon as exactly by_score keys reach a candidate
+      const int vary = 32 - __builtin_clz((kmax ^ kmin) | 1u);
+      tau = vary >= 32 ? 0u : (kmax >> vary) << vary;
+      bool exact = false;
+      int over = 0, turn = 0;                      // keys above tau's range so far
+      // two bits a turn (three candidates): the turns wait for a barrier, not for the counting
+      for (int bit = (vary + 1) / 2 * 2 - 2; bit >= 0 && !exact; bit -= 2, turn ^= 1) {
+        int c3[3] = {0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+          for (int x = 0; x < 3; ++x) c3[x] += __popcll(__ballot(key[i] >= (tau | (uint32_t)(x + 1) << bit)));
+        if (lane == 0) *reinterpret_cast<int4*>(&counts[turn][wave][0]) = make_int4(c3[0], c3[1], c3[2], 0);
+        __syncthreads();                           // (two sets of counts: the next turn writes the other one)
+#pragma unroll
+        for (int x = 0; x < 3; ++x) c3[x] = (counts[turn][0][x] + counts[turn][1][x]) + (counts[turn][2][x] + counts[turn][3][x]);
+        const int digit = c3[2] >= by_score ? 3 : c3[1] >= by_score ? 2 : c3[0] >= by_score ? 1 : 0;
+        if (digit < 3) over = c3[digit];
+        tau |= (uint32_t)digit << bit;
+        if (digit > 0 && c3[digit - 1] == by_score) {
+          tau -= 1;
+          exact = true;
+        }
+      }
+      ties = exact ? 0 : by_score - over;          // equal to tau: the lowest blocks
     }
-    __syncthreads();
-    int all;
-    const int mine = (int)hist[255 - tid];         // thread i: digit 255 - i
-    const int above = scan_threads(mine, red, &all);
-    if (above < left && above + mine >= left) {
-      pick[0] = 255 - tid;
-      pick[1] = above;
-    }
-    __syncthreads();
-    tau |= pick[0] << shift;
-    left -= (int)pick[1];
-    __syncthreads();
   }
-  // now `left` of the blocks equal to tau are kept, the lowest; thread i owns a run of blocks
-  const int run = (seen + 255) / 256;
-  const int m0 = min(tid * run, seen), m1 = min(m0 + run, seen);
-  int n_eq = 0, all;
-  for (int m = m0; m < m1; ++m) n_eq += keys[m] == tau;
-  int eq_before = scan_threads(n_eq, red, &all);
+
+  // kept blocks, ascending: how many before this wave, then before each slot
+  int n_eq = 0;
+#pragma unroll
+  for (int i = 0; i < NI; ++i) n_eq += ties > 0 ? __popcll(__ballot(key[i] == tau)) : 0;
+  if (lane == 0) totals[2][wave] = n_eq;
+  __syncthreads();
+  int eq_left = ties;
+  for (int x = 0; x < wave; ++x) eq_left -= min(eq_left, totals[2][x]);
+  unsigned long long out = 0;
   int n_out = 0;
-  {
-    int eq = eq_before;
-    for (int m = m0; m < m1; ++m) {
-      const uint32_t k = keys[m];
-      n_out += want > 0 && k != kUnseen && (k > tau || (k == tau && eq++ < left));
-    }
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const bool eq = ties > 0 && key[i] == tau;
+    const unsigned long long eqs = __ballot(eq);
+    const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(eqs >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)eqs, 0));
+    const bool keep = (must >> i & 1) || (key[i] > tau) || (eq && before < eq_left);
+    eq_left -= min(eq_left, (int)__popcll(eqs));
+    if (keep) out |= 1ull << i;
+    n_out += __popcll(__ballot(keep));
   }
-  int at = scan_threads(n_out, red, &all);
-  for (int m = m0; m < m1; ++m) {
-    const uint32_t k = keys[m];
-    if (want > 0 && k != kUnseen && (k > tau || (k == tau && eq_before++ < left))) list[at++] = m;
+  if (lane == 0) ends[0][wave] = (uint32_t)n_out;
+  __syncthreads();
+  int at = 0;
+  for (int x = 0; x < wave; ++x) at += (int)ends[0][x];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const bool keep = out >> i & 1;
+    const unsigned long long all = __ballot(keep);
+    if (keep) list[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0))] = m0 + 64 * i + lane;
+    at += __popcll(all);
   }
   for (int i = want + tid; i < a.list_len; i += 256) list[i] = -1;
   if (tid == 0) a.kept[row] = want;
 }
 
+// A launch for the scores where the rows leave most compute units idle and a row has several runs of blocks. Both sides,
+// us: 8 rows of 16 384 blocks 0 and 0, of 2048 0 and 0; 64 rows of 4096 0 and 0.
+bool scores_apart(const CacheDims& c, int64_t rows) { return rows < 128 && c.max_blocks > 2 * kRunBlocks; }
+
+template <int D>
+hipError_t launch_t(const CacheDims& c, const RowDims& r, const CacheSelectArgs& a, hipStream_t s) {
+  const int64_t rows = (int64_t)a.groups * c.batch * c.heads_kv;
+  const dim3 grid((uint32_t)rows), block(256);
+  const bool apart = a.ws && scores_apart(c, rows);
+  if (apart) {
+    const int runs = (c.max_blocks + kRunBlocks - 1) / kRunBlocks;
+    hipLaunchKernelGGL((cache_score_kernel<D>), dim3((uint32_t)(rows * runs)), block, 0, s, c, r, a, runs);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (c.max_blocks <= 4096) hipLaunchKernelGGL((cache_select_kernel<D, 16, true>), grid, block, 0, s, c, r, a);
+    else hipLaunchKernelGGL((cache_select_kernel<D, 64, true>), grid, block, 0, s, c, r, a);
+    return hipGetLastError();
+  }
+  if (c.max_blocks <= 512) hipLaunchKernelGGL((cache_select_kernel<D, 2, false>), grid, block, 0, s, c, r, a);
+  else if (c.max_blocks <= 1024) hipLaunchKernelGGL((cache_select_kernel<D, 4, false>), grid, block, 0, s, c, r, a);
+  else if (c.max_blocks <= 4096) hipLaunchKernelGGL((cache_select_kernel<D, 16, false>), grid, block, 0, s, c, r, a);
+  else hipLaunchKernelGGL((cache_select_kernel<D, 64, false>), grid, block, 0, s, c, r, a);
+  return hipGetLastError();
+}
+
 }  // namespace
 
+size_t cache_select_ws_bytes(const CacheDims& c, const RowDims& r, int group) {
+  const int per = group > 0 && group < r.t ? group : r.t;
+  const int64_t rows = (int64_t)((r.t + per - 1) / per) * c.batch * c.heads_kv;
+  return c.max_blocks <= RSA_CACHE_MAX_SELECT && scores_apart(c, rows) ? (size_t)rows * c.max_blocks * sizeof(uint32_t) : 0;
+}
+
 hipError_t launch_cache_select(const CacheDims& c, const RowDims& r, const CacheSelectArgs& a, hipStream_t s) {
-  const dim3 grid(a.groups * c.batch * c.heads_kv);
-  const size_t lds = (size_t)c.max_blocks * sizeof(uint32_t);
-  if (c.d == 128) hipLaunchKernelGGL((cache_select_kernel<128>), grid, dim3(256), lds, s, c, r, a);
-  else hipLaunchKernelGGL((cache_select_kernel<64>), grid, dim3(256), lds, s, c, r, a);
-  return hipGetLastError();
+  return c.d == 128 ? launch_t<128>(c, r, a, s) : launch_t<64>(c, r, a, s);
 }
 
 }  // namespace rsa
