@@ -61,7 +61,7 @@ struct Tile {
   int ql;               // query tokens of the sequence
   int units;            // blocks to walk: listed ones, or all that any row of the tile sees
   int blocks;           // blocks that hold a visible key
-  int64_t lo_seen;      // keys that every row of the tile sees
+  int lo_seen;          // keys that every row of the tile sees
 };
 struct TileGrid {
   int rows_per_tile;    // 16 QT
@@ -70,6 +70,11 @@ struct TileGrid {
   int stored;           // rows of a partial result: min(16 QT, rows of a group)
 };
 
+// Keys that query token `tok` of the tile's sequence sees.
+__device__ __forceinline__ int visible_keys(const CacheDims& c, const CacheAttnArgs& a, const Tile& t, int tok) {
+  const int64_t n = a.causal ? min(max(t.kv - t.ql + tok + 1, (int64_t)0), t.kv) : t.kv;
+  return (int)min(n, (int64_t)c.max_blocks * c.blk);
+}
 __device__ __forceinline__ Tile tile_of(const CacheDims& c, const RowDims& r, const CacheAttnArgs& a, const TileGrid& tg, int64_t id) {
   Tile t;
   const int G = r.heads / c.heads_kv;
@@ -85,16 +90,38 @@ __device__ __forceinline__ Tile tile_of(const CacheDims& c, const RowDims& r, co
   t.ql = a.q_len ? min(a.q_len[t.b], r.t) : r.t;
   const int last_row = min(t.row0 + tg.rows_per_tile, t.rows) - 1;
   const int first_tok = t.t0 + t.row0 / G, last_tok = min(t.t0 + last_row / G, t.ql - 1);
-  int64_t hi = 0;
+  int hi = 0;
   t.lo_seen = 0;
   if (t.row0 < t.rows && first_tok < t.ql) {       // some row of the tile is a query
-    t.lo_seen = a.causal ? min(max(t.kv - t.ql + first_tok + 1, (int64_t)0), t.kv) : t.kv;
-    hi = a.causal ? min(max(t.kv - t.ql + last_tok + 1, (int64_t)0), t.kv) : t.kv;
+    t.lo_seen = visible_keys(c, a, t, first_tok);
+    hi = visible_keys(c, a, t, last_tok);
   }
-  t.blocks = (int)min((hi + c.blk - 1) / c.blk, (int64_t)c.max_blocks);
+  t.blocks = (int)(((int64_t)hi + c.blk - 1) >> (c.blk == 128 ? 7 : 6));
   t.units = t.blocks;
   if (a.block_idx) t.units = t.blocks > 0 ? min(max(a.kept[t.lrow], 0), a.list_len) : 0;
   return t;
+}
+
+// One run of 16 value codes of a lane (channel tile v): where NaN stands under a key that a column sees (the first left[x] of
+// the 64), the column's output becomes NaN.
+template <int QT, int VC>
+__device__ __forceinline__ void mark_nan(const uint4& w, const int (&left)[QT], int g, int v, floatx4 (&o)[QT][VC]) {
+  halfx8 is[2];                                    // 1.0 for a NaN
+  widen(make_uint4(nan_bytes(w.x) & 0x38383838u, nan_bytes(w.y) & 0x38383838u, nan_bytes(w.z) & 0x38383838u, nan_bytes(w.w) & 0x38383838u), is);
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    halfx8 see[2];
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) see[y / 2][y % 2 * 4 + e] = 16 * y + 4 * g + e < left[x] ? (_Float16)1.f : (_Float16)0.f;
+    floatx4 hit = {0.f, 0.f, 0.f, 0.f};
+    hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(is[0], see[0], hit, 0, 0, 0);
+    hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(is[1], see[1], hit, 0, 0, 0);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (hit[e] > 0.f) o[x][v][e] = __builtin_nanf("");
+  }
 }
 
 template <int D, int BLK, int QT>
@@ -113,12 +140,12 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheDims c, RowDims r,
 
   // queries of this lane's columns, as operands, and how many keys each sees
   bf16x8 q[QT][2 * KC];
-  int64_t seen[QT];
+  int seen[QT];
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
     const int row = t.row0 + 16 * x + n, tok = t.t0 + row / G;
     const bool is = row < t.rows && tok < t.ql;
-    seen[x] = !is ? 0 : a.causal ? min(max(t.kv - t.ql + tok + 1, (int64_t)0), t.kv) : t.kv;
+    seen[x] = !is ? 0 : visible_keys(c, a, t, tok);
     const uint16_t* src = a.Q + (int64_t)t.b * r.sb + (int64_t)(t.hk * G + row % G) * r.sh + (int64_t)tok * r.st;
 #pragma unroll
     for (int k = 0; k < KC; ++k)
@@ -176,7 +203,7 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheDims c, RowDims r,
     while (i >= 0) {
       todo &= todo - 1;
       const int next = todo ? __builtin_ctzll(todo) : -1;
-      const int64_t key0 = (int64_t)__builtin_amdgcn_readlane(my_blk, i) * BLK + ((base + i * 4) % SPB) * 64;
+      const int key0 = __builtin_amdgcn_readlane(my_blk, i) * BLK + ((base + i * 4) % SPB) * 64;
       const float ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_k), i)) * a.scale_log2e;
       const int ev = exponent_of(__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_v), i)));
 
@@ -204,7 +231,7 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheDims c, RowDims r,
       bool over = false;
 #pragma unroll
       for (int x = 0; x < QT; ++x) {
-        const int left = (int)min(max(seen[x] - key0, (int64_t)-1), (int64_t)64);   // of the 64
+        const int left = seen[x] - key0;             // of the 64
 #pragma unroll
         for (int y = 0; y < 4; ++y)
 #pragma unroll
@@ -223,8 +250,7 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheDims c, RowDims r,
           for (int y = 0; y < 4; ++y)
 #pragma unroll
             for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[x][y][e]);
-          mx = fmaxf(mx, __shfl_xor(mx, 16));
-          mx = fmaxf(mx, __shfl_xor(mx, 32));
+          mx = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, mx), MaxF32()), MaxF32()));
           if (mx > m[x] + kLazy) {                 // the same in the four lanes of a column
             const float down = exp2f(m[x] - mx);
             m[x] = mx;
@@ -270,31 +296,14 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheDims c, RowDims r,
         odd = __any(bad != 0);
       }
       if (odd) {
-        halfx8 see[QT][2];
+        int left[QT];
 #pragma unroll
-        for (int x = 0; x < QT; ++x) {
-          const int left = (int)min(max(seen[x] - key0, (int64_t)-1), (int64_t)64);
-#pragma unroll
-          for (int y = 0; y < 4; ++y)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) see[x][y / 2][y % 2 * 4 + e] = 16 * y + 4 * g + e < left ? (_Float16)1.f : (_Float16)0.f;
-        }
+        for (int x = 0; x < QT; ++x) left[x] = seen[x] - key0;
 #pragma unroll
         for (int v = 0; v < VC; ++v) {
           const uint4 w = vc[v];
-          const uint4 nb = make_uint4(nan_bytes(w.x), nan_bytes(w.y), nan_bytes(w.z), nan_bytes(w.w));
-          vc[v] = make_uint4(w.x & ~nb.x, w.y & ~nb.y, w.z & ~nb.z, w.w & ~nb.w);
-          halfx8 is[2];
-          widen(make_uint4(nb.x & 0x38383838u, nb.y & 0x38383838u, nb.z & 0x38383838u, nb.w & 0x38383838u), is);   // 1.0
-#pragma unroll
-          for (int x = 0; x < QT; ++x) {
-            floatx4 hit = {0.f, 0.f, 0.f, 0.f};
-            hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(is[0], see[x][0], hit, 0, 0, 0);
-            hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(is[1], see[x][1], hit, 0, 0, 0);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (hit[e] > 0.f) o[x][v][e] = __builtin_nanf("");
-          }
+          mark_nan<QT, VC>(w, left, g, v, o);
+          vc[v] = make_uint4(w.x & ~nan_bytes(w.x), w.y & ~nan_bytes(w.y), w.z & ~nan_bytes(w.z), w.w & ~nan_bytes(w.w));
         }
       }
 #pragma unroll
@@ -316,9 +325,7 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheDims c, RowDims r,
   const float unit = eo < -126 ? 0.f : exp2_int(min(eo, 127));
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
-    float sum = l[x];
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
+    const float sum = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, l[x]), AddF32()), AddF32()));
     if (x > 0) __syncthreads();
     if (g == 0) {
       join_m[wave][n] = m[x];
@@ -358,6 +365,286 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheDims c, RowDims r,
       if (tg.splits > 1) (a.parts + (int64_t)gridDim.x * tg.stored * D)[(int64_t)blockIdx.x * tg.stored + 16 * x + n] = lse2;
       else if (a.lse) a.lse[((int64_t)t.b * r.heads + t.hk * G + row % G) * r.t + tok] = lse2 * kLn2;
     }
+  }
+}
+
+// The same for many query rows, bound by the matrix pipe and the vector ALU beside it. 64 QT rows to a workgroup, 16 QT to
+// a wave: every wave needs all codes, so they are widened once for the workgroup, a quarter by each wave, into LDS in the
+// order of the operands (each 1 KB that a wave reads is lanes times 16 bytes: no conflicts, no address work). Two buffers, one
+// barrier a step of 64 keys: while a step is computed the codes of the next are widened and those of the one after are on
+// their way. 64 KB of LDS at d = 128, so that two workgroups share a compute unit and the softmax of one runs beside the
+// products of the other.
+constexpr int kAhead = 256;                        // steps that are looked up together
+template <int D, int BLK, int QT>
+__global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims r, CacheAttnArgs a, TileGrid tg) {
+  constexpr int KC = D / 64, VC = D / 16, VW = VC / 4;   // VW: 1 KB pieces of values that a wave widens (of keys: KC)
+  constexpr int SPB = BLK / 64;
+  constexpr int KBYTES = 4 * KC * 2048, BYTES = KBYTES + VC * 2048;       // of a buffer: keys, then values
+  __shared__ __align__(16) uint8_t lds[2][BYTES];
+  __shared__ int st_page[kAhead], st_key[kAhead], odd[2][4], n_valid[4];
+  __shared__ float2 st_scale[kAhead];
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const int g = lane / 16, n = lane % 16;
+  // tiles of one key/value head that walk the same part of the keys follow one another on an XCD
+  const int inner = tg.per_group * a.groups;
+  const int id = xcd_run(blockIdx.x, gridDim.x);
+  const int split = id / inner % tg.splits;
+  const int64_t tile = (int64_t)(id / inner / tg.splits) * inner + id % inner;
+  const Tile t = tile_of(c, r, a, tg, tile);
+  const int G = r.heads / c.heads_kv;
+
+  bf16x8 q[QT][2 * KC];
+  int seen[QT];
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    const int row = t.row0 + (wave * QT + x) * 16 + n, tok = t.t0 + row / G;
+    const bool is = row < t.rows && tok < t.ql;
+    seen[x] = !is ? 0 : visible_keys(c, a, t, tok);
+    const uint16_t* src = a.Q + (int64_t)t.b * r.sb + (int64_t)(t.hk * G + row % G) * r.sh + (int64_t)tok * r.st;
+#pragma unroll
+    for (int k = 0; k < KC; ++k)
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (is) v = *reinterpret_cast<const uint4*>(src + k * 64 + g * 16 + hf * 8);
+        q[x][2 * k + hf] = __builtin_bit_cast(bf16x8, v);
+      }
+  }
+  floatx4 o[QT][VC];
+  float m[QT], l[QT];
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    m[x] = kNoReference;
+    l[x] = 0.f;
+#pragma unroll
+    for (int v = 0; v < VC; ++v) o[x][v] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  int eo = -200, top = -200;
+
+  const int u0 = (int)((int64_t)t.units * split / tg.splits), u1 = (int)((int64_t)t.units * (split + 1) / tg.splits);
+  const int steps = (u1 - u0) * SPB;
+  for (int base = 0; base < steps; base += kAhead) {
+    // the next steps: those with a page, put together in order (one look-up for the workgroup, so that its waves walk the
+    // same steps whatever happens to the table meanwhile)
+    __syncthreads();
+    {
+      const int s = base + tid;
+      int blk = -1, page = -1;
+      if (s < steps) {
+        blk = u0 + s / SPB;
+        if (a.block_idx) blk = a.block_idx[(int64_t)t.lrow * a.list_len + blk];
+        if (blk < t.blocks) page = cache_page(c, t.b, blk);
+      }
+      const unsigned long long all = __ballot(page >= 0);
+      if (lane == 0) n_valid[wave] = __popcll(all);
+      __syncthreads();
+      int at = __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
+      for (int w = 0; w < wave; ++w) at += n_valid[w];
+      if (page >= 0) {
+        st_page[at] = page;
+        st_key[at] = blk * BLK + s % SPB * 64;
+        st_scale[at] = *reinterpret_cast<const float2*>(c.scales + ((int64_t)page * c.heads_kv + t.hk) * 4);
+      }
+      __syncthreads();
+    }
+    const int count = __builtin_amdgcn_readfirstlane(n_valid[0] + n_valid[1] + n_valid[2] + n_valid[3]);
+    uint4 raw[KC + VW];
+    auto request = [&](int i) __attribute__((always_inline)) {
+      const int page = __builtin_amdgcn_readfirstlane(st_page[i]), sub = __builtin_amdgcn_readfirstlane(st_key[i]) % BLK;
+      const int64_t at = ((int64_t)page * c.heads_kv + t.hk) * (BLK * D) + sub * D + lane * 16;
+#pragma unroll
+      for (int x = 0; x < KC; ++x) raw[x] = *reinterpret_cast<const uint4*>(c.k + at + (wave * KC + x) * 1024);
+#pragma unroll
+      for (int x = 0; x < VW; ++x) raw[KC + x] = *reinterpret_cast<const uint4*>(c.v + at + (wave * VW + x) * 1024);
+    };
+    auto store = [&](int i) __attribute__((always_inline)) {              // widens what request(i) brought
+      uint8_t* to = lds[i & 1] + lane * 16;
+      if (__builtin_amdgcn_readfirstlane(st_key[i]) + 64 > t.lo_seen) {   // a row of the tile does not see all keys: no NaN into 0 * NaN
+        uint32_t bad = 0;
+#pragma unroll
+        for (int x = 0; x < VW; ++x) {
+          uint4& w = raw[KC + x];
+          const uint4 nb = make_uint4(nan_bytes(w.x), nan_bytes(w.y), nan_bytes(w.z), nan_bytes(w.w));
+          bad |= nb.x | nb.y | nb.z | nb.w;
+          w = make_uint4(w.x & ~nb.x, w.y & ~nb.y, w.z & ~nb.z, w.w & ~nb.w);
+        }
+        const bool any = __any(bad != 0);
+        if (lane == 0) odd[i & 1][wave] = any;
+      }
+#pragma unroll
+      for (int x = 0; x < KC; ++x) {
+        bf16x8 op[2];
+        widen(raw[x], op);
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) *reinterpret_cast<bf16x8*>(to + (wave * KC + x) * 2048 + hf * 1024) = op[hf];
+      }
+#pragma unroll
+      for (int x = 0; x < VW; ++x) {
+        halfx8 op[2];
+        widen(raw[KC + x], op);
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) *reinterpret_cast<halfx8*>(to + KBYTES + (wave * VW + x) * 2048 + hf * 1024) = op[hf];
+      }
+    };
+    if (count > 0) {
+      request(0);
+      store(0);
+      if (count > 1) request(1);
+    }
+    for (int i = 0; i < count; ++i) {
+      __syncthreads();
+      const uint8_t* buf = lds[i & 1] + lane * 16;
+      const int key0 = __builtin_amdgcn_readfirstlane(st_key[i]);
+      const float ks = fmaxf(st_scale[i].x * a.scale_log2e, 0x1p-126f);
+      const int ev = exponent_of(__builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, st_scale[i].y))));
+
+      floatx4 s[QT][4];
+#pragma unroll
+      for (int x = 0; x < QT; ++x)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) s[x][y] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+#pragma unroll
+        for (int k = 0; k < 2 * KC; ++k) {
+          const bf16x8 op = *reinterpret_cast<const bf16x8*>(buf + (y * 2 * KC + k) * 1024);
+#pragma unroll
+          for (int x = 0; x < QT; ++x) s[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op, q[x][k], s[x][y], 0, 0, 0);
+        }
+      if (i + 1 < count) {
+        store(i + 1);
+        if (i + 2 < count) request(i + 2);
+      }
+
+      const bool partly = key0 + 64 > t.lo_seen;
+      if (partly) {
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          const int left = seen[x] - key0;
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[x][y][e] = 16 * y + 4 * g + e < left ? s[x][y][e] : -INFINITY;
+        }
+      }
+      float most[QT];
+      bool over = false;
+#pragma unroll
+      for (int x = 0; x < QT; ++x) {
+        most[x] = -INFINITY;
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) most[x] = fmaxf(fmaxf(most[x], s[x][y][e]), s[x][y][e + 1]);
+        most[x] *= ks;
+        over |= most[x] > m[x] + kLazy;
+      }
+      if (__any(over)) {
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          float mx = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, most[x]), MaxF32()), MaxF32()));
+          if (mx > m[x] + kLazy) {
+            const float down = __builtin_amdgcn_exp2f(m[x] - mx);
+            m[x] = mx;
+            l[x] *= down;
+#pragma unroll
+            for (int v = 0; v < VC; ++v) o[x][v] *= down;
+          }
+        }
+      }
+      if (ev > eo || ev < eo - 8) {
+        top = max(top, ev);
+        const int to = max(ev, top - 80);
+        if (to != eo) {
+          const float f = exp2_int(max(min(eo - to, 120), -126));
+#pragma unroll
+          for (int x = 0; x < QT; ++x)
+#pragma unroll
+            for (int v = 0; v < VC; ++v) o[x][v] *= f;
+          eo = to;
+        }
+      }
+      // P over 2^(eo - ev), so that it goes with o; the sums take it back
+      const int pe = max(ev - eo, -120);
+      const float back = exp2_int(-pe);
+      halfx8 p[QT][2];
+#pragma unroll
+      for (int x = 0; x < QT; ++x) {
+        const float ref = m[x] - (float)pe;
+        float sum = 0.f;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          float w[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            w[e] = __builtin_amdgcn_exp2f(fmaf(s[x][y][e], ks, -ref));
+            sum += w[e];
+          }
+          const halfx2 lo = __builtin_convertvector(floatx2{w[0], w[1]}, halfx2), hi = __builtin_convertvector(floatx2{w[2], w[3]}, halfx2);
+          p[x][y / 2][y % 2 * 4 + 0] = lo[0]; p[x][y / 2][y % 2 * 4 + 1] = lo[1];
+          p[x][y / 2][y % 2 * 4 + 2] = hi[0]; p[x][y / 2][y % 2 * 4 + 3] = hi[1];
+        }
+        l[x] += sum * back;
+      }
+      if (partly) {
+        const int4 f = *reinterpret_cast<const int4*>(odd[i & 1]);
+        if (__builtin_amdgcn_readfirstlane(f.x | f.y | f.z | f.w)) {
+          const int64_t at = ((int64_t)__builtin_amdgcn_readfirstlane(st_page[i]) * c.heads_kv + t.hk) * (BLK * D) + key0 % BLK * D + lane * 16;
+          int left[QT];
+#pragma unroll
+          for (int x = 0; x < QT; ++x) left[x] = seen[x] - key0;
+#pragma unroll
+          for (int v = 0; v < VC; ++v) mark_nan<QT, VC>(*reinterpret_cast<const uint4*>(c.v + at + v * 1024), left, g, v, o);
+        }
+      }
+#pragma unroll
+      for (int v = 0; v < VC; ++v)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          const halfx8 op = *reinterpret_cast<const halfx8*>(buf + KBYTES + (v * 2 + hf) * 1024);
+#pragma unroll
+          for (int x = 0; x < QT; ++x) o[x][v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op, p[x][hf], o[x][v], 0, 0, 0);
+        }
+    }
+  }
+
+  // rows out: normalised, turned through the wave's share of a buffer
+  const float unit = eo < -126 ? 0.f : exp2_int(min(eo, 127));
+  constexpr int PITCH = D + 8;                     // bf16 of a row
+  static_assert(4 * 16 * PITCH * 2 <= 2 * BYTES, "rows of a wave do not fit");
+  uint16_t* turn = reinterpret_cast<uint16_t*>(&lds[0][0]) + wave * 16 * PITCH;
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    const float total = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, l[x]), AddF32()), AddF32()));
+    const float f = total == 0.f ? 0.f : unit / total;
+    const int first = (wave * QT + x) * 16, row = t.row0 + first + n, tok = t.t0 + row / G;
+    const float lse2 = total == 0.f ? -INFINITY : m[x] + log2f(total);
+    const bool is = row < t.rows && tok < t.ql;
+    if (tg.splits > 1) {
+      const int64_t at = (tile * tg.splits + split) * tg.stored + first + n;
+      if (is) {
+#pragma unroll
+        for (int v = 0; v < VC; ++v) *reinterpret_cast<floatx4*>(a.parts + at * D + 16 * v + 4 * g) = o[x][v] * f;
+        if (g == 0) (a.parts + (int64_t)gridDim.x * tg.stored * D)[at] = lse2;
+      }
+      continue;
+    }
+    if (is && g == 0 && a.lse) a.lse[((int64_t)t.b * r.heads + t.hk * G + row % G) * r.t + tok] = lse2 * kLn2;
+#pragma unroll
+    for (int v = 0; v < VC; ++v) {
+      const floatx4 z = o[x][v] * f;
+      *reinterpret_cast<uint2*>(turn + n * PITCH + 16 * v + 4 * g) = make_uint2(pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]));
+    }
+    __builtin_amdgcn_wave_barrier();               // (the wave's own rows: LDS keeps a wave's order)
+#pragma unroll
+    for (int u = lane; u < 16 * (D / 8); u += 64) {
+      const int rr = u / (D / 8), ch = u % (D / 8) * 8, orow = t.row0 + first + rr, otok = t.t0 + orow / G;
+      if (orow < t.rows && otok < t.ql)
+        *reinterpret_cast<uint4*>(a.O + (int64_t)t.b * r.sb + (int64_t)(t.hk * G + orow % G) * r.sh + (int64_t)otok * r.st + ch) =
+            *reinterpret_cast<const uint4*>(turn + rr * PITCH + ch);
+    }
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -415,35 +702,49 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheDims c, RowDims r,
 }
 
 struct Plan {
+  bool tiled;           // cache_tile_kernel: 64 QT rows to a tile instead of 16 QT
   int qt;
   int64_t tiles;
   TileGrid grid;
 };
-// Rows of a group fill tiles of 16 or 32. The key axis is split until there are about four workgroups to a compute unit
-// or every wave has one step of 64 keys.
+// Up to 32 rows of a group: tiles of 16 or 32 rows whose keys the waves share out; more: tiles of 64 or 128 rows.
 Plan plan_of(const CacheDims& c, const RowDims& r, int group, int list_len) {
   Plan p;
   const int G = r.heads / c.heads_kv;
   const int per = group > 0 && group < r.t ? group : r.t;
   const int64_t rows = (int64_t)per * G;
-  p.qt = rows <= 16 ? 1 : 2;
-  p.grid.rows_per_tile = 16 * p.qt;
+  p.tiled = rows > 32;
+  p.qt = rows <= 16 || (rows > 32 && rows <= 64) ? 1 : 2;
+  p.grid.rows_per_tile = (p.tiled ? 64 : 16) * p.qt;
   p.grid.per_group = (int)((rows + p.grid.rows_per_tile - 1) / p.grid.rows_per_tile);
   p.grid.stored = (int)(rows < p.grid.rows_per_tile ? rows : p.grid.rows_per_tile);
   p.tiles = (int64_t)((r.t + per - 1) / per) * p.grid.per_group * c.batch * c.heads_kv;
   const int64_t steps = (int64_t)(list_len > 0 ? list_len : c.max_blocks) * (c.blk / 64);
-  const int64_t most = (steps + 3) / 4;
-  int64_t s = (4 * kCus + p.tiles - 1) / p.tiles;
-  if (s > most) s = most;
-  if (s > 64) s = 64;
-  p.grid.splits = (int)(s < 1 ? 1 : s);
+  int64_t best = 1;
+  if (p.tiled) {
+    // rounds of resident workgroups (two to a compute unit) times what one takes: its steps and, in steps, its start, its
+    // end and the parts that it leaves
+    int64_t cost = -1;
+    for (int64_t s = 1; s <= 16 && s <= (steps + 7) / 8; ++s) {
+      const int64_t rounds = (p.tiles * s + 2 * kCus - 1) / (2 * kCus), one = (steps + s - 1) / s + (s > 1 ? 12 : 6);
+      if (cost < 0 || rounds * one < cost) { cost = rounds * one; best = s; }
+    }
+  } else {
+    // about four workgroups to a compute unit, or one step of 64 keys to every wave
+    best = (4 * kCus + p.tiles - 1) / p.tiles;
+    if (best > (steps + 3) / 4) best = (steps + 3) / 4;
+    if (best > 64) best = 64;
+  }
+  p.grid.splits = (int)(best < 1 ? 1 : best);
   return p;
 }
 
 template <int D, int BLK>
 hipError_t launch_t(const CacheDims& c, const RowDims& r, const CacheAttnArgs& a, const Plan& p, hipStream_t s) {
   const dim3 grid((uint32_t)(p.tiles * p.grid.splits)), block(256);
-  if (p.qt == 1) hipLaunchKernelGGL((cache_attn_kernel<D, BLK, 1>), grid, block, 0, s, c, r, a, p.grid);
+  if (p.tiled && p.qt == 1) hipLaunchKernelGGL((cache_tile_kernel<D, BLK, 1>), grid, block, 0, s, c, r, a, p.grid);
+  else if (p.tiled) hipLaunchKernelGGL((cache_tile_kernel<D, BLK, 2>), grid, block, 0, s, c, r, a, p.grid);
+  else if (p.qt == 1) hipLaunchKernelGGL((cache_attn_kernel<D, BLK, 1>), grid, block, 0, s, c, r, a, p.grid);
   else hipLaunchKernelGGL((cache_attn_kernel<D, BLK, 2>), grid, block, 0, s, c, r, a, p.grid);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.grid.splits == 1) return e;

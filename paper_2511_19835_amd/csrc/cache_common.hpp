@@ -49,6 +49,13 @@ __device__ __forceinline__ int v_code_offset(int t, int ch) {
   return ((((t >> 6) * (D / 16) + (ch >> 4)) * 4 + ((t & 15) >> 2)) * 16 + (ch & 15)) * 16 + ((t & 63) >> 4) * 4 + (t & 3);
 }
 
+// Workgroups go round the eight XCDs in turn; numbered like this, those of an XCD take numbers that follow one another, so
+// that what neighbours share (a sequence's heads the lines of scales, a head's groups means and codes) is in one L2.
+__device__ __forceinline__ int xcd_run(int id, int all) {
+  const int x = id % 8, per = all / 8, more = all % 8;
+  return x * per + min(x, more) + id / 8;
+}
+
 // Values of other lanes by the vector ALU alone (through LDS, as __shfl does it, each exchange waits some 100 cycles, and
 // the small calls of the cache are little else). Lanes of a row of 16, by control word:
 constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kFlip8 = 0x141 /* lane i and i ^ 7 */, kFlip16 = 0x140 /* i ^ 15 */, kXor8 = 0x128;

@@ -179,13 +179,6 @@ __device__ __forceinline__ void score_blocks(const CacheDims& c, const Row& w, c
   }
 }
 
-// Workgroups go round the eight XCDs in turn; numbered like this, those of an XCD take rows that follow one another: the
-// heads of a sequence, whose scales share lines, and the groups of a head, which read the same means.
-__device__ __forceinline__ int xcd_run(int id, int all) {
-  const int x = id % 8, per = all / 8, more = all % 8;
-  return x * per + min(x, more) + id / 8;
-}
-
 // Scores of a run of blocks, for rows that are few.
 template <int D>
 __global__ __launch_bounds__(256) void cache_score_kernel(CacheDims c, RowDims r, CacheSelectArgs a, int runs) {
