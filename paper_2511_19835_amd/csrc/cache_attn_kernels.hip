@@ -380,10 +380,11 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
   constexpr int KC = D / 64, VC = D / 16, VW = VC / 4;   // VW: 1 KB pieces of values that a wave widens (of keys: KC)
   constexpr int SPB = BLK / 64;
   constexpr int KBYTES = 4 * KC * 2048, BYTES = KBYTES + VC * 2048;       // of a buffer: keys, then values
-  __shared__ __align__(16) uint8_t lds[2][BYTES];
-  __shared__ int st_page[kAhead], st_key[kAhead], odd[2][4], n_valid[4];
-  __shared__ float2 st_scale[kAhead];
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  __shared__ __align__(16) uint8_t lds_k[2][KBYTES], lds_v[2][BYTES - KBYTES];
+  __shared__ int4 look[kAhead];                    // page, first key, scale of the keys, scale of the values
+  __shared__ __align__(16) int odd[2][4];
+  __shared__ int n_valid[4];
+  const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int g = lane / 16, n = lane % 16;
   // tiles of one key/value head that walk the same part of the keys follow one another on an XCD
   const int inner = tg.per_group * a.groups;
@@ -410,6 +411,11 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
         q[x][2 * k + hf] = __builtin_bit_cast(bf16x8, v);
       }
   }
+  // the queries are here before the loop: a wait for them inside it would be one for every load in flight
+#pragma unroll
+  for (int x = 0; x < QT; ++x)
+#pragma unroll
+    for (int k = 0; k < 2 * KC; ++k) asm volatile("" : "+v"(q[x][k]));
   floatx4 o[QT][VC];
   float m[QT], l[QT];
 #pragma unroll
@@ -441,86 +447,124 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
       int at = __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
       for (int w = 0; w < wave; ++w) at += n_valid[w];
       if (page >= 0) {
-        st_page[at] = page;
-        st_key[at] = blk * BLK + s % SPB * 64;
-        st_scale[at] = *reinterpret_cast<const float2*>(c.scales + ((int64_t)page * c.heads_kv + t.hk) * 4);
+        const uint2 sc = *reinterpret_cast<const uint2*>(c.scales + ((int64_t)page * c.heads_kv + t.hk) * 4);
+        look[at] = make_int4(page, blk * BLK + s % SPB * 64, (int)sc.x, (int)sc.y);
       }
       __syncthreads();
     }
     const int count = __builtin_amdgcn_readfirstlane(n_valid[0] + n_valid[1] + n_valid[2] + n_valid[3]);
-    uint4 raw[KC + VW];
-    auto request = [&](int i) __attribute__((always_inline)) {
-      const int page = __builtin_amdgcn_readfirstlane(st_page[i]), sub = __builtin_amdgcn_readfirstlane(st_key[i]) % BLK;
-      const int64_t at = ((int64_t)page * c.heads_kv + t.hk) * (BLK * D) + sub * D + lane * 16;
-#pragma unroll
-      for (int x = 0; x < KC; ++x) raw[x] = *reinterpret_cast<const uint4*>(c.k + at + (wave * KC + x) * 1024);
-#pragma unroll
-      for (int x = 0; x < VW; ++x) raw[KC + x] = *reinterpret_cast<const uint4*>(c.v + at + (wave * VW + x) * 1024);
+    if (count == 0) continue;
+    // what a step is, the same in every lane
+    struct Step { int page, key; float ks; int ev; };
+    auto step_at = [&](int i) __attribute__((always_inline)) {
+      const int4 v = *reinterpret_cast<const int4*>(&look[min(i, count - 1)]);
+      Step z;
+      z.page = __builtin_amdgcn_readfirstlane(v.x);
+      z.key = __builtin_amdgcn_readfirstlane(v.y);
+      z.ks = fmaxf(__builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(v.z)) * a.scale_log2e, 0x1p-126f);
+      z.ev = exponent_of(__builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(v.w)));
+      return z;
     };
-    auto store = [&](int i) __attribute__((always_inline)) {              // widens what request(i) brought
-      uint8_t* to = lds[i & 1] + lane * 16;
-      if (__builtin_amdgcn_readfirstlane(st_key[i]) + 64 > t.lo_seen) {   // a row of the tile does not see all keys: no NaN into 0 * NaN
-        uint32_t bad = 0;
+    uint4 raw_k[KC], raw_v[VW];
+    auto request = [&](const Step& z, uint4* raw, const uint8_t* codes, int pieces) __attribute__((always_inline)) {
+      const uint8_t* src = codes + ((int64_t)z.page * c.heads_kv + t.hk) * (BLK * D) + z.key % BLK * D;
 #pragma unroll
-        for (int x = 0; x < VW; ++x) {
-          uint4& w = raw[KC + x];
-          const uint4 nb = make_uint4(nan_bytes(w.x), nan_bytes(w.y), nan_bytes(w.z), nan_bytes(w.w));
-          bad |= nb.x | nb.y | nb.z | nb.w;
-          w = make_uint4(w.x & ~nb.x, w.y & ~nb.y, w.z & ~nb.z, w.w & ~nb.w);
-        }
-        const bool any = __any(bad != 0);
-        if (lane == 0) odd[i & 1][wave] = any;
+      for (int x = 0; x < pieces; ++x) raw[x] = *reinterpret_cast<const uint4*>(src + ((wave * pieces + x) * 1024 + lane * 16));
+    };
+    // a row of the tile does not see all keys of the step: no NaN into 0 * NaN
+    auto clear_nan = [&](int buf) __attribute__((always_inline)) {
+      uint32_t bad = 0;
+#pragma unroll
+      for (int x = 0; x < VW; ++x) {
+        uint4& w = raw_v[x];
+        const uint4 nb = make_uint4(nan_bytes(w.x), nan_bytes(w.y), nan_bytes(w.z), nan_bytes(w.w));
+        bad |= nb.x | nb.y | nb.z | nb.w;
+        w = make_uint4(w.x & ~nb.x, w.y & ~nb.y, w.z & ~nb.z, w.w & ~nb.w);
       }
+      const bool any = __any(bad != 0);
+      if (lane == 0) odd[buf][wave] = any;
+    };
+    auto store_k = [&](int buf) __attribute__((always_inline)) {
+      uint8_t* to = lds_k[buf] + lane * 16;
 #pragma unroll
       for (int x = 0; x < KC; ++x) {
         bf16x8 op[2];
-        widen(raw[x], op);
+        widen(raw_k[x], op);
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) *reinterpret_cast<bf16x8*>(to + (wave * KC + x) * 2048 + hf * 1024) = op[hf];
       }
+    };
+    auto store_v = [&](int buf) __attribute__((always_inline)) {
+      uint8_t* to = lds_v[buf] + lane * 16;
 #pragma unroll
       for (int x = 0; x < VW; ++x) {
         halfx8 op[2];
-        widen(raw[KC + x], op);
+        widen(raw_v[x], op);
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) *reinterpret_cast<halfx8*>(to + KBYTES + (wave * VW + x) * 2048 + hf * 1024) = op[hf];
+        for (int hf = 0; hf < 2; ++hf) *reinterpret_cast<halfx8*>(to + (wave * VW + x) * 2048 + hf * 1024) = op[hf];
       }
     };
-    if (count > 0) {
-      request(0);
-      store(0);
-      if (count > 1) request(1);
-    }
-    for (int i = 0; i < count; ++i) {
-      __syncthreads();
-      const uint8_t* buf = lds[i & 1] + lane * 16;
-      const int key0 = __builtin_amdgcn_readfirstlane(st_key[i]);
-      const float ks = fmaxf(st_scale[i].x * a.scale_log2e, 0x1p-126f);
-      const int ev = exponent_of(__builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, st_scale[i].y))));
-
-      floatx4 s[QT][4];
+    auto scores = [&](const uint8_t* buf, floatx4 (&s)[QT][4]) __attribute__((always_inline)) {
 #pragma unroll
       for (int x = 0; x < QT; ++x)
 #pragma unroll
         for (int y = 0; y < 4; ++y) s[x][y] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int y = 0; y < 4; ++y)
+      for (int k = 0; k < 2 * KC; ++k)
 #pragma unroll
-        for (int k = 0; k < 2 * KC; ++k) {
+        for (int y = 0; y < 4; ++y) {              // (a sum is touched again 4 QT products later)
           const bf16x8 op = *reinterpret_cast<const bf16x8*>(buf + (y * 2 * KC + k) * 1024);
 #pragma unroll
           for (int x = 0; x < QT; ++x) s[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op, q[x][k], s[x][y], 0, 0, 0);
         }
-      if (i + 1 < count) {
-        store(i + 1);
-        if (i + 2 < count) request(i + 2);
-      }
+    };
 
-      const bool partly = key0 + 64 > t.lo_seen;
+    Step now = step_at(0), next = step_at(1);
+    request(now, raw_k, c.k, KC);
+    request(now, raw_v, c.v, VW);
+    if (now.key + 64 > t.lo_seen) clear_nan(0);
+    store_k(0);
+    store_v(0);
+    request(next, raw_k, c.k, KC);
+    request(next, raw_v, c.v, VW);
+    for (int i = 0; i < count; ++i) {
+      __syncthreads();
+      if (next.key + 64 > t.lo_seen) clear_nan((i + 1) & 1);
+      const Step later = step_at(i + 2);
+      const bool partly = now.key + 64 > t.lo_seen;
+      if (partly) {
+        const int4 f = *reinterpret_cast<const int4*>(odd[i & 1]);
+        if (__builtin_amdgcn_readfirstlane(f.x | f.y | f.z | f.w)) {
+          const int64_t at = ((int64_t)now.page * c.heads_kv + t.hk) * (BLK * D) + now.key % BLK * D + lane * 16;
+          int left[QT];
+#pragma unroll
+          for (int x = 0; x < QT; ++x) left[x] = seen[x] - now.key;
+#pragma unroll
+          for (int v = 0; v < VC; ++v) mark_nan<QT, VC>(*reinterpret_cast<const uint4*>(c.v + at + v * 1024), left, g, v, o);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
+      floatx4 s[QT][4];
+      scores(lds_k[i & 1] + lane * 16, s);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+#pragma unroll
+      for (int u = 0; u < 8 * KC - 4; ++u) {
+        __builtin_amdgcn_sched_group_barrier(0x008, QT, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, QT * 4, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(0);
+      store_k((i + 1) & 1);
+      store_v((i + 1) & 1);
+      request(later, raw_k, c.k, KC);
+      request(later, raw_v, c.v, VW);
       if (partly) {
 #pragma unroll
         for (int x = 0; x < QT; ++x) {
-          const int left = seen[x] - key0;
+          const int left = seen[x] - now.key;
 #pragma unroll
           for (int y = 0; y < 4; ++y)
 #pragma unroll
@@ -536,25 +580,24 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
         for (int y = 0; y < 4; ++y)
 #pragma unroll
           for (int e = 0; e < 4; e += 2) most[x] = fmaxf(fmaxf(most[x], s[x][y][e]), s[x][y][e + 1]);
-        most[x] *= ks;
+        most[x] *= now.ks;
         over |= most[x] > m[x] + kLazy;
       }
       if (__any(over)) {
 #pragma unroll
         for (int x = 0; x < QT; ++x) {
-          float mx = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, most[x]), MaxF32()), MaxF32()));
-          if (mx > m[x] + kLazy) {
-            const float down = __builtin_amdgcn_exp2f(m[x] - mx);
-            m[x] = mx;
-            l[x] *= down;
+          const float mx = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, most[x]), MaxF32()), MaxF32()));
+          const float to = mx > m[x] + kLazy ? mx : m[x];           // the same in the four lanes of a column
+          const float down = __builtin_amdgcn_exp2f(m[x] - to);
+          m[x] = to;
+          l[x] *= down;
 #pragma unroll
-            for (int v = 0; v < VC; ++v) o[x][v] *= down;
-          }
+          for (int v = 0; v < VC; ++v) o[x][v] *= down;
         }
       }
-      if (ev > eo || ev < eo - 8) {
-        top = max(top, ev);
-        const int to = max(ev, top - 80);
+      if (now.ev > eo || now.ev < eo - 8) {
+        top = max(top, now.ev);
+        const int to = max(now.ev, top - 80);
         if (to != eo) {
           const float f = exp2_int(max(min(eo - to, 120), -126));
 #pragma unroll
@@ -565,7 +608,7 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
         }
       }
       // P over 2^(eo - ev), so that it goes with o; the sums take it back
-      const int pe = max(ev - eo, -120);
+      const int pe = max(now.ev - eo, -120);
       const float back = exp2_int(-pe);
       halfx8 p[QT][2];
 #pragma unroll
@@ -577,7 +620,7 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
           float w[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            w[e] = __builtin_amdgcn_exp2f(fmaf(s[x][y][e], ks, -ref));
+            w[e] = __builtin_amdgcn_exp2f(fmaf(s[x][y][e], now.ks, -ref));
             sum += w[e];
           }
           const halfx2 lo = __builtin_convertvector(floatx2{w[0], w[1]}, halfx2), hi = __builtin_convertvector(floatx2{w[2], w[3]}, halfx2);
@@ -586,33 +629,39 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
         }
         l[x] += sum * back;
       }
-      if (partly) {
-        const int4 f = *reinterpret_cast<const int4*>(odd[i & 1]);
-        if (__builtin_amdgcn_readfirstlane(f.x | f.y | f.z | f.w)) {
-          const int64_t at = ((int64_t)__builtin_amdgcn_readfirstlane(st_page[i]) * c.heads_kv + t.hk) * (BLK * D) + key0 % BLK * D + lane * 16;
-          int left[QT];
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
+      const uint8_t* buf = lds_v[i & 1] + lane * 16;
 #pragma unroll
-          for (int x = 0; x < QT; ++x) left[x] = seen[x] - key0;
+      for (int v = 0; v < VC; v += 2)
 #pragma unroll
-          for (int v = 0; v < VC; ++v) mark_nan<QT, VC>(*reinterpret_cast<const uint4*>(c.v + at + v * 1024), left, g, v, o);
-        }
+        for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+          for (int vv = v; vv < v + 2; ++vv) {
+            const halfx8 op = *reinterpret_cast<const halfx8*>(buf + (vv * 2 + hf) * 1024);
+#pragma unroll
+            for (int x = 0; x < QT; ++x) o[x][vv] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op, p[x][hf], o[x][vv], 0, 0, 0);
+          }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+#pragma unroll
+      for (int u = 0; u < 2 * VC - 8; ++u) {
+        __builtin_amdgcn_sched_group_barrier(0x008, QT, 1);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
       }
-#pragma unroll
-      for (int v = 0; v < VC; ++v)
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          const halfx8 op = *reinterpret_cast<const halfx8*>(buf + KBYTES + (v * 2 + hf) * 1024);
-#pragma unroll
-          for (int x = 0; x < QT; ++x) o[x][v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op, p[x][hf], o[x][v], 0, 0, 0);
-        }
+      __builtin_amdgcn_sched_group_barrier(0x008, QT * 8, 1);
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(0);
+      now = next;
+      next = later;
     }
   }
 
   // rows out: normalised, turned through the wave's share of a buffer
   const float unit = eo < -126 ? 0.f : exp2_int(min(eo, 127));
   constexpr int PITCH = D + 8;                     // bf16 of a row
-  static_assert(4 * 16 * PITCH * 2 <= 2 * BYTES, "rows of a wave do not fit");
-  uint16_t* turn = reinterpret_cast<uint16_t*>(&lds[0][0]) + wave * 16 * PITCH;
+  static_assert(4 * 16 * PITCH * 2 <= 2 * KBYTES, "rows of a wave do not fit");
+  uint16_t* turn = reinterpret_cast<uint16_t*>(&lds_k[0][0]) + wave * 16 * PITCH;
   __syncthreads();
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
@@ -671,6 +720,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheDims c, RowDims r,
     const float* part_lse = a.parts + tiles * tg.splits * tg.stored * D;
 #pragma unroll 4
     for (int s = 0; s < tg.splits; ++s) most = fmaxf(most, part_lse[(first + s) * tg.stored + rr]);
+#pragma unroll 4
     for (int s = sl; s < tg.splits; s += lanes) {
       const float p = part_lse[(first + s) * tg.stored + rr];
       const float w = p == -INFINITY ? 0.f : exp2f(p - most);
@@ -749,8 +799,9 @@ hipError_t launch_t(const CacheDims& c, const RowDims& r, const CacheAttnArgs& a
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.grid.splits == 1) return e;
   int lanes = 1;
-  while (lanes < p.grid.splits && lanes < 256 / (D / 8)) lanes *= 2;
-  const int64_t per_wg = 256 / (D / 8) / lanes, rows = p.tiles * p.grid.stored;
+  const int64_t rows = p.tiles * p.grid.stored;
+  while (lanes < p.grid.splits && lanes < 256 / (D / 8) && rows * (D / 8) * lanes < (1 << 18)) lanes *= 2;   // (many rows keep the chip busy alone)
+  const int64_t per_wg = 256 / (D / 8) / lanes;
   hipLaunchKernelGGL((cache_join_kernel<D>), dim3((uint32_t)((rows + per_wg - 1) / per_wg)), block, 0, s, c, r, a, p.grid, p.tiles, lanes);
   return hipGetLastError();
 }
