@@ -125,7 +125,7 @@ __device__ __forceinline__ void mark_nan(const uint4& w, const int (&left)[QT], 
 }
 
 template <int D, int BLK, int QT>
-__global__ __launch_bounds__(256) void cache_attn_kernel(CacheDims c, RowDims r, CacheAttnArgs a, TileGrid tg) {
+__global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheDims c, RowDims r, CacheAttnArgs a, TileGrid tg) {
   constexpr int KC = D / 64, VC = D / 16;          // 16-byte loads of a lane for 16 keys / for 64 keys
   constexpr int SPB = BLK / 64;                    // steps of 64 keys in a block
   constexpr int PITCH = D + 4;                     // floats of a row in the joining buffer
@@ -780,10 +780,23 @@ Plan plan_of(const CacheDims& c, const RowDims& r, int group, int list_len) {
       if (cost < 0 || rounds * one < cost) { cost = rounds * one; best = s; }
     }
   } else {
-    // about four workgroups to a compute unit, or one step of 64 keys to every wave
-    best = (4 * kCus + p.tiles - 1) / p.tiles;
-    if (best > (steps + 3) / 4) best = (steps + 3) / 4;
-    if (best > 64) best = 64;
+    // Two workgroups to a compute unit at least, and parts of at most 64 steps, 16 to a wave, so that sequences of different
+    // length even out; of up to half as many more the number that fills its last round best (24 tiles of 3713 steps: 58 parts
+    // 261 us, 64 parts 254); never less than a step to a wave. 256 tiles of 512 steps, ragged: 2, 4, 6, 8, 12 parts 254, 256,
+    // 249, 246, 248 us; of 64 steps: 57, 59, 62, 63, 72. Up to 24 steps in one launch: the second takes longer than the
+    // steps that it saves (8 tiles of 16 steps 10.2 and 8.5 us, of 24 10.4 and 10.4, of 47 10.7 and 16.0).
+    const int64_t slots = 2 * kCus;
+    best = (slots + p.tiles - 1) / p.tiles;
+    if (best < (steps + 63) / 64) best = (steps + 63) / 64;
+    int64_t top = best + best / 2;
+    if (top > (steps + 3) / 4) top = (steps + 3) / 4;
+    if (top > 64) top = 64;
+    if (best > top) best = top;
+    for (int64_t s = best; s <= top; ++s) {        // less of its last round empty
+      const int64_t a = (p.tiles * s + slots - 1) / slots, b = (p.tiles * best + slots - 1) / slots;
+      if (a * best < b * s) best = s;
+    }
+    if (steps <= 24) best = 1;
   }
   p.grid.splits = (int)(best < 1 ? 1 : best);
   return p;
