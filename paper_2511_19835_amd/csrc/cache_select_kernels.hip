@@ -5,10 +5,11 @@
 // bit, so a score is exact, equal scores are equal, and the choice does not depend on an order of sums.
 //
 // One workgroup per row = (sequence, key/value head, group): the sum of the queries (fp64: exact for bf16 terms within 40
-// binades of each other), the scores of all blocks as order-preserving keys, the threshold key bit by bit with ballot
-// counts (keys in registers, each wave owning a run of blocks), and the kept blocks in ascending order. What bounds it is
-// latency: five loads that wait for one another, and the search. Where there are few rows and many blocks the scores are
-// a launch of their own, in runs of blocks over many workgroups.
+// binades of each other), the scores of all blocks as order-preserving keys, the threshold key by a histogram (keys in
+// registers, each wave owning a run of blocks), and the kept blocks in ascending order. What bounds it is latency and the
+// address unit: 256 rows of 512 blocks 8.3 us (its 17 MB of means would take 3.3), 696 rows of 929 19.0; the longest rows
+// take sixteen waves. Where there are few rows and many blocks the scores are a launch of their own, in runs of blocks over
+// many workgroups.
 #include "cache_common.hpp"
 
 namespace rsa {
@@ -90,7 +91,7 @@ __device__ __forceinline__ void sum_queries(const RowDims& r, const CacheSelectA
   const int tid = threadIdx.x, cc = tid % CPR;
   double acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   const int rows = (w.t1 - w.t0) * w.G;
-  for (int from = 0; from < rows; from += kQueryRows * STRIPES) {
+  for (int from = 0; tid < 256 && from < rows; from += kQueryRows * STRIPES) {
     if (from > 0) request_queries<D>(r, a, w, from, v);
 #pragma unroll
     for (int u = 0; u < kQueryRows; ++u) {
@@ -104,7 +105,8 @@ __device__ __forceinline__ void sum_queries(const RowDims& r, const CacheSelectA
     }
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) L.sums[tid / CPR][cc * 8 + e] = acc[e];
+  for (int e = 0; e < 8; ++e)
+    if (tid < 256) L.sums[tid / CPR][cc * 8 + e] = acc[e];
   __syncthreads();
   if (tid < D) {
     const int stripes = min(rows, STRIPES);        // the others hold zeros
@@ -129,54 +131,70 @@ __device__ __forceinline__ void sum_queries(const RowDims& r, const CacheSelectA
   __syncthreads();
 }
 
-// The means of a round of blocks, on their way: 16 channels to a lane, kRound passes requested together (pages lie
-// anywhere, so that a round of loads waits some 2500 cycles).
-constexpr int kRound = 16;
-struct Means {
-  int page[kRound];
-  int4 k[kRound];
-  float scale[kRound];
-};
-template <int D>
-__device__ __forceinline__ void request_means(const CacheDims& c, const Row& w, int from, int to, Means& x) {
-  constexpr int LPB = D / 16, BPP = 256 / LPB;     // lanes to a block, blocks to a pass
-  const int m0 = from + (int)threadIdx.x / LPB;
+// Scores of blocks [from, to) of a row, NI to a thread, as order-preserving keys in keys[0 ..) (ends with a barrier). The loads
+// take turns in the address unit of the compute unit, so there are few: pages and scales once, a block to a lane, the means 16
+// channels to a lane, kRound passes requested together (pages lie anywhere: a round waits some 2500 cycles).
+// Pages and scales by the lanes of each mean: 929 blocks of 696 rows 23.7 us, now 19.0.
+template <int D, int NI, int W>
+__device__ __forceinline__ void score_blocks(const CacheDims& c, const RowDims& r, const CacheSelectArgs& a, const Row& w, int from, int to,
+                                             QueryLds<D>& L, uint32_t* keys) {
+  constexpr int kRound = W == 4 ? 16 : 8;
+  constexpr int LPB = D / 16, BPP = 64 * W / LPB;  // lanes to a block, blocks to a pass
+  const int tid = threadIdx.x, part = tid % LPB;
+  uint4 query[kQueryRows];
+  if (tid < 256) request_queries<D>(r, a, w, 0, query);     // four waves' work
+  float scale[NI];
 #pragma unroll
-  for (int u = 0; u < kRound; ++u) x.page[u] = m0 + u * BPP < to ? cache_page(c, w.b, m0 + u * BPP) : -1;
-#pragma unroll
-  for (int u = 0; u < kRound; ++u) {
-    x.k[u] = make_int4(0, 0, 0, 0);
-    x.scale[u] = 0.f;
-    if (x.page[u] >= 0) {
-      const int64_t rec = (int64_t)x.page[u] * c.heads_kv + w.hk;
-      x.k[u] = *reinterpret_cast<const int4*>(c.mean + rec * D + threadIdx.x % LPB * 16);
-      x.scale[u] = c.scales[rec * 4 + 2];
-    }
+  for (int i = 0; i < NI; ++i) {
+    const int m = tid + 64 * W * i, page = from + m < to ? cache_page(c, w.b, from + m) : -1;
+    if (from + m < to) keys[m] = (uint32_t)page;
+    scale[i] = -1.f;                               // there is no page
+    if (page >= 0) scale[i] = c.scales[((int64_t)page * c.heads_kv + w.hk) * 4 + 2];
   }
-}
-// Keys of blocks [from, to) of the row into keys[0 ..); `x`: the first round, requested earlier.
-template <int D>
-__device__ __forceinline__ void score_blocks(const CacheDims& c, const Row& w, const int8_t* q8, int from, int to, Means& x, uint32_t* keys) {
-  constexpr int LPB = D / 16, BPP = 256 / LPB;
-  const int part = threadIdx.x % LPB;
-  const int4 q = *reinterpret_cast<const int4*>(&q8[part * 16]);
-  for (int at = from; at < to; at += kRound * BPP) {
-    if (at > from) request_means<D>(c, w, at, to, x);
+  __syncthreads();
+  int page[kRound];
+  int4 mean[kRound];
+  auto request = [&](int at) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < kRound; ++u) {
-      const int m = at + u * BPP + (int)threadIdx.x / LPB;
-      int dot = __builtin_amdgcn_sdot4(q.x, x.k[u].x, 0, false);
-      dot = __builtin_amdgcn_sdot4(q.y, x.k[u].y, dot, false);
-      dot = __builtin_amdgcn_sdot4(q.z, x.k[u].z, dot, false);
-      dot = __builtin_amdgcn_sdot4(q.w, x.k[u].w, dot, false);
+      const int m = at + u * BPP + tid / LPB;
+      page[u] = from + m < to ? (int)keys[m] : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < kRound; ++u) {
+      mean[u] = make_int4(0, 0, 0, 0);
+      if (page[u] >= 0) mean[u] = *reinterpret_cast<const int4*>(c.mean + ((int64_t)page[u] * c.heads_kv + w.hk) * D + part * 16);
+    }
+  };
+  request(0);
+  sum_queries<D>(r, a, w, query, L);
+  const int4 q = *reinterpret_cast<const int4*>(&L.q8[part * 16]);
+  for (int at = 0; from + at < to; at += kRound * BPP) {
+    if (at > 0) request(at);
+#pragma unroll
+    for (int u = 0; u < kRound; ++u) {
+      const int m = at + u * BPP + tid / LPB;
+      int dot = __builtin_amdgcn_sdot4(q.x, mean[u].x, 0, false);
+      dot = __builtin_amdgcn_sdot4(q.y, mean[u].y, dot, false);
+      dot = __builtin_amdgcn_sdot4(q.z, mean[u].z, dot, false);
+      dot = __builtin_amdgcn_sdot4(q.w, mean[u].w, dot, false);
       dot += row_lane<kXor1>(dot);
       dot += row_lane<kXor2>(dot);
       if (LPB == 8) dot += row_lane<kFlip8>(dot);
-      // 2^-22 keeps the largest scale finite; the product is exact (|dot| < 2^21)
-      const float z = (float)dot * 0x1p-22f * x.scale[u];
-      if (part == 0 && m < to) keys[m - from] = x.page[u] < 0 ? kUnseen : fabsf(z) <= kLargest ? ordered_key(z) : kLowest;
+      if (part == 0 && from + m < to) keys[m] = (uint32_t)dot;            // in the place of its page, which this wave has read
     }
   }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int m = tid + 64 * W * i;
+    if (from + m < to) {
+      // 2^-22 keeps the largest scale finite; the product is exact (|dot| < 2^21)
+      const float z = (float)(int)keys[m] * 0x1p-22f * scale[i];
+      keys[m] = scale[i] == -1.f ? kUnseen : fabsf(z) <= kLargest ? ordered_key(z) : kLowest;
+    }
+  }
+  __syncthreads();
 }
 
 // Scores of a run of blocks, for rows that are few.
@@ -188,48 +206,25 @@ __global__ __launch_bounds__(256) void cache_score_kernel(CacheDims c, RowDims r
   const Row w = row_of(c, r, a, row);
   const int from = id % runs * kRunBlocks, to = min(from + kRunBlocks, w.seen);
   if (from >= to) return;
-  uint4 q[kQueryRows];
-  Means x;
-  request_queries<D>(r, a, w, 0, q);
-  request_means<D>(c, w, from, to, x);
-  sum_queries<D>(r, a, w, q, L);
-  score_blocks<D>(c, w, L.q8, from, to, x, keys);
-  __syncthreads();
+  score_blocks<D, kRunBlocks / 256, 4>(c, r, a, w, from, to, L, keys);
   uint32_t* out = (uint32_t*)a.ws + (int64_t)row * c.max_blocks;
   for (int m = from + (int)threadIdx.x; m < to; m += 256) out[m] = keys[m - from];
 }
 
-// NI keys to a thread (rows of up to 256 NI blocks); SCORED: the keys are in the workspace.
-template <int D, int NI, bool SCORED>
-__global__ __launch_bounds__(256) void cache_select_kernel(CacheDims c, RowDims r, CacheSelectArgs a) {
-  __shared__ QueryLds<D> L;
-  __shared__ uint32_t keys[SCORED ? 1 : 256 * NI];
-  __shared__ __align__(16) int counts[2][4][4];
-  __shared__ int totals[3][4];
-  __shared__ uint32_t ends[2][4], few[64];
-  __shared__ __align__(16) int hist[256];
-  __shared__ int n_few;
+template <int W>
+struct ChoiceLds {
+  __align__(16) int counts[2][W][4];
+  __align__(16) int hist[256];
+  int totals[3][W], n_few;
+  uint32_t ends[2][W], few[64];
+};
+// The list of one row from the keys of its blocks, by W waves (NI keys to a thread: rows of up to 64 W NI blocks).
+template <int NI, int W>
+__device__ __forceinline__ void choose(const CacheSelectArgs& a, const Row& w, int row, const uint32_t* src, ChoiceLds<W>& L) {
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-  const int row = xcd_run(blockIdx.x, gridDim.x);
-  const Row w = row_of(c, r, a, row);
   int32_t* list = a.block_idx + (int64_t)row * a.list_len;
-  if (w.seen <= 0) {                               // nothing to choose from (the whole workgroup)
-    for (int i = tid; i < a.list_len; i += 256) list[i] = -1;
-    if (tid == 0) a.kept[row] = 0;
-    return;
-  }
-  if (!SCORED) {
-    uint4 q[kQueryRows];
-    Means x;
-    request_queries<D>(r, a, w, 0, q);
-    request_means<D>(c, w, 0, w.seen, x);
-    sum_queries<D>(r, a, w, q, L);
-    score_blocks<D>(c, w, L.q8, 0, w.seen, x, keys);
-    __syncthreads();
-  }
   // this wave's run of blocks, slot i of lane l being block m0 + 64 i + l
   const int m0 = wave * 64 * NI;
-  const uint32_t* src = SCORED ? (const uint32_t*)a.ws + (int64_t)row * c.max_blocks : keys;
   uint32_t key[NI];
   unsigned long long must = 0;                     // bit i: slot i is forced
   int n_seen = 0, n_must = 0;
@@ -250,19 +245,21 @@ __global__ __launch_bounds__(256) void cache_select_kernel(CacheDims c, RowDims 
   }
   kmax = (uint32_t)over_wave((int)kmax, MaxU32());
   nkmin = (uint32_t)over_wave((int)nkmin, MaxU32());
-  hist[tid] = 0;
-  if (tid == 0) n_few = 0;
+  if (tid < 256) L.hist[tid] = 0;
+  if (tid == 0) L.n_few = 0;
   if (lane == 0) {
-    totals[0][wave] = n_seen;
-    totals[1][wave] = n_must;
-    ends[0][wave] = kmax;
-    ends[1][wave] = nkmin;
+    L.totals[0][wave] = n_seen;
+    L.totals[1][wave] = n_must;
+    L.ends[0][wave] = kmax;
+    L.ends[1][wave] = nkmin;
   }
   __syncthreads();
-  n_seen = totals[0][0] + totals[0][1] + totals[0][2] + totals[0][3];
-  n_must = totals[1][0] + totals[1][1] + totals[1][2] + totals[1][3];
-  kmax = max(max(ends[0][0], ends[0][1]), max(ends[0][2], ends[0][3]));
-  const uint32_t kmin = ~max(max(ends[1][0], ends[1][1]), max(ends[1][2], ends[1][3]));
+  // (a wave's numbers to a lane, W <= 16: over a row of lanes)
+  auto of_waves = [&](const auto* x, auto op) __attribute__((always_inline)) { return over_row(lane % 16 < W ? (int)x[lane % 16] : 0, op); };
+  n_seen = __builtin_amdgcn_readfirstlane(of_waves(L.totals[0], AddInt()));
+  n_must = __builtin_amdgcn_readfirstlane(of_waves(L.totals[1], AddInt()));
+  kmax = (uint32_t)__builtin_amdgcn_readfirstlane(of_waves(L.ends[0], MaxU32()));
+  const uint32_t kmin = ~(uint32_t)__builtin_amdgcn_readfirstlane(of_waves(L.ends[1], MaxU32()));
   const int want = min(max(a.keep, n_must), n_seen);
   const int by_score = want - n_must;
 
@@ -277,10 +274,10 @@ __global__ __launch_bounds__(256) void cache_select_kernel(CacheDims c, RowDims 
     auto step_of = [&](uint32_t k) __attribute__((always_inline)) { return (int)((score_of(k) - smin) * steps); };   // monotone
 #pragma unroll
     for (int i = 0; i < NI; ++i)
-      if (key[i] != kUnseen) atomicAdd(&hist[step_of(key[i])], 1);
+      if (key[i] != kUnseen) atomicAdd(&L.hist[step_of(key[i])], 1);
     __syncthreads();
     // in every wave: lane l has steps 255 - 4 l down to 252 - 4 l
-    const int4 h = *reinterpret_cast<const int4*>(&hist[252 - 4 * lane]);
+    const int4 h = *reinterpret_cast<const int4*>(&L.hist[252 - 4 * lane]);
     const int four = h.x + h.y + h.z + h.w;
     int upto = four;
     upto += row_up<1>(upto);
@@ -304,9 +301,9 @@ __global__ __launch_bounds__(256) void cache_select_kernel(CacheDims c, RowDims 
     if (n <= 64) {                                 // n keys share the step that holds tau (the same in every wave)
 #pragma unroll
       for (int i = 0; i < NI; ++i)
-        if (key[i] != kUnseen && step_of(key[i]) == step) few[atomicAdd(&n_few, 1)] = key[i];
+        if (key[i] != kUnseen && step_of(key[i]) == step) L.few[atomicAdd(&L.n_few, 1)] = key[i];
       __syncthreads();
-      const uint32_t mine = lane < n ? few[lane] : kUnseen;              // (their order does not matter)
+      const uint32_t mine = lane < n ? L.few[lane] : kUnseen;              // (their order does not matter)
       int more = 0, same = 0;
       for (int x = 0; x < n; ++x) {
         const uint32_t other = (uint32_t)__builtin_amdgcn_readlane((int)mine, x);
@@ -330,10 +327,10 @@ __global__ __launch_bounds__(256) void cache_select_kernel(CacheDims c, RowDims 
         for (int i = 0; i < NI; ++i)
 #pragma unroll
           for (int x = 0; x < 3; ++x) c3[x] += __popcll(__ballot(key[i] >= (tau | (uint32_t)(x + 1) << bit)));
-        if (lane == 0) *reinterpret_cast<int4*>(&counts[turn][wave][0]) = make_int4(c3[0], c3[1], c3[2], 0);
+        if (lane == 0) *reinterpret_cast<int4*>(&L.counts[turn][wave][0]) = make_int4(c3[0], c3[1], c3[2], 0);
         __syncthreads();                           // (two sets of counts: the next turn writes the other one)
 #pragma unroll
-        for (int x = 0; x < 3; ++x) c3[x] = (counts[turn][0][x] + counts[turn][1][x]) + (counts[turn][2][x] + counts[turn][3][x]);
+        for (int x = 0; x < 3; ++x) c3[x] = __builtin_amdgcn_readfirstlane(over_row(lane % 16 < W ? L.counts[turn][lane % 16][x] : 0, AddInt()));
         const int digit = c3[2] >= by_score ? 3 : c3[1] >= by_score ? 2 : c3[0] >= by_score ? 1 : 0;
         if (digit < 3) over = c3[digit];
         tau |= (uint32_t)digit << bit;
@@ -350,10 +347,10 @@ __global__ __launch_bounds__(256) void cache_select_kernel(CacheDims c, RowDims 
   int n_eq = 0;
 #pragma unroll
   for (int i = 0; i < NI; ++i) n_eq += ties > 0 ? __popcll(__ballot(key[i] == tau)) : 0;
-  if (lane == 0) totals[2][wave] = n_eq;
+  if (lane == 0) L.totals[2][wave] = n_eq;
   __syncthreads();
   int eq_left = ties;
-  for (int x = 0; x < wave; ++x) eq_left -= min(eq_left, totals[2][x]);
+  for (int x = 0; x < wave; ++x) eq_left -= min(eq_left, L.totals[2][x]);
   unsigned long long out = 0;
   int n_out = 0;
 #pragma unroll
@@ -366,10 +363,10 @@ __global__ __launch_bounds__(256) void cache_select_kernel(CacheDims c, RowDims 
     if (keep) out |= 1ull << i;
     n_out += __popcll(__ballot(keep));
   }
-  if (lane == 0) ends[0][wave] = (uint32_t)n_out;
+  if (lane == 0) L.ends[0][wave] = (uint32_t)n_out;
   __syncthreads();
   int at = 0;
-  for (int x = 0; x < wave; ++x) at += (int)ends[0][x];
+  for (int x = 0; x < wave; ++x) at += (int)L.ends[0][x];
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     const bool keep = out >> i & 1;
@@ -377,13 +374,31 @@ __global__ __launch_bounds__(256) void cache_select_kernel(CacheDims c, RowDims 
     if (keep) list[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0))] = m0 + 64 * i + lane;
     at += __popcll(all);
   }
-  for (int i = want + tid; i < a.list_len; i += 256) list[i] = -1;
+  for (int i = want + tid; i < a.list_len; i += 64 * W) list[i] = -1;
   if (tid == 0) a.kept[row] = want;
 }
 
-// A launch for the scores where the rows leave most compute units idle and a row has several runs of blocks. Both sides,
-// us: 8 rows of 16 384 blocks 0 and 0, of 2048 0 and 0; 64 rows of 4096 0 and 0.
-bool scores_apart(const CacheDims& c, int64_t rows) { return rows < 128 && c.max_blocks > 2 * kRunBlocks; }
+// SCORED: the keys are in the workspace.
+template <int D, int NI, int W, bool SCORED>
+__global__ __launch_bounds__(64 * W) void cache_select_kernel(CacheDims c, RowDims r, CacheSelectArgs a) {
+  __shared__ QueryLds<D> L;
+  __shared__ ChoiceLds<W> choice;
+  __shared__ uint32_t keys[SCORED ? 1 : 64 * W * NI];
+  const int tid = threadIdx.x, row = xcd_run(blockIdx.x, gridDim.x);
+  const Row w = row_of(c, r, a, row);
+  if (w.seen <= 0) {                               // nothing to choose from (the whole workgroup)
+    for (int i = tid; i < a.list_len; i += 64 * W) a.block_idx[(int64_t)row * a.list_len + i] = -1;
+    if (tid == 0) a.kept[row] = 0;
+    return;
+  }
+  if (!SCORED) score_blocks<D, NI, W>(c, r, a, w, 0, w.seen, L, keys);
+  choose<NI, W>(a, w, row, SCORED ? (const uint32_t*)a.ws + (int64_t)row * c.max_blocks : keys, choice);
+}
+
+// A launch for the scores where the rows leave most compute units idle and a row has several runs of blocks. One launch and
+// two, us: 8 rows of 16 384 blocks 61 and 37, of 4096 16.8 and 15.8, of 2049 13.2 and 15.1; 64 rows of 8192 45 and 33, of 4096
+// 22.4 and 19.7, of 2049 13.9 and 15.9; 120 rows of 8192 47 and 44, of 4096 24.3 and 24.2; 200 rows of 4096 28 and 33.
+bool scores_apart(const CacheDims& c, int64_t rows) { return rows < 100 && c.max_blocks >= 4 * kRunBlocks; }
 
 template <int D>
 hipError_t launch_t(const CacheDims& c, const RowDims& r, const CacheSelectArgs& a, hipStream_t s) {
@@ -395,14 +410,14 @@ hipError_t launch_t(const CacheDims& c, const RowDims& r, const CacheSelectArgs&
     hipLaunchKernelGGL((cache_score_kernel<D>), dim3((uint32_t)(rows * runs)), block, 0, s, c, r, a, runs);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (c.max_blocks <= 4096) hipLaunchKernelGGL((cache_select_kernel<D, 16, true>), grid, block, 0, s, c, r, a);
-    else hipLaunchKernelGGL((cache_select_kernel<D, 64, true>), grid, block, 0, s, c, r, a);
+    if (c.max_blocks <= 4096) hipLaunchKernelGGL((cache_select_kernel<D, 4, 16, true>), grid, dim3(1024), 0, s, c, r, a);
+    else hipLaunchKernelGGL((cache_select_kernel<D, 16, 16, true>), grid, dim3(1024), 0, s, c, r, a);
     return hipGetLastError();
   }
-  if (c.max_blocks <= 512) hipLaunchKernelGGL((cache_select_kernel<D, 2, false>), grid, block, 0, s, c, r, a);
-  else if (c.max_blocks <= 1024) hipLaunchKernelGGL((cache_select_kernel<D, 4, false>), grid, block, 0, s, c, r, a);
-  else if (c.max_blocks <= 4096) hipLaunchKernelGGL((cache_select_kernel<D, 16, false>), grid, block, 0, s, c, r, a);
-  else hipLaunchKernelGGL((cache_select_kernel<D, 64, false>), grid, block, 0, s, c, r, a);
+  if (c.max_blocks <= 512) hipLaunchKernelGGL((cache_select_kernel<D, 2, 4, false>), grid, block, 0, s, c, r, a);
+  else if (c.max_blocks <= 1024) hipLaunchKernelGGL((cache_select_kernel<D, 4, 4, false>), grid, block, 0, s, c, r, a);
+  else if (c.max_blocks <= 4096) hipLaunchKernelGGL((cache_select_kernel<D, 4, 16, false>), grid, dim3(1024), 0, s, c, r, a);
+  else hipLaunchKernelGGL((cache_select_kernel<D, 16, 16, false>), grid, dim3(1024), 0, s, c, r, a);
   return hipGetLastError();
 }
 
