@@ -95,7 +95,9 @@ def test_sizes(lib):
     assert rb.rsa_cache_bytes(c) == (20 * 2 * 64 * 128, 20 * 2 * 16, 20 * 2 * 128)
     assert lib.rsa_cache_bytes(None, None, None, None) == -1
     a, b = ctypes.c_size_t(), ctypes.c_size_t()
-    assert lib.rsa_cache_workspace_bytes(ctypes.byref(c), ctypes.byref(_rows(heads=4)), 0, a, b) == 0 and b.value > 0
+    assert lib.rsa_cache_workspace_bytes(ctypes.byref(c), ctypes.byref(_rows(heads=4)), 0, a, b) == 0 and (a.value, b.value) == (0, 0)   # ten blocks: one launch
+    long = _cache(max_blocks=5000, k_codes=None, v_codes=None, scales=None, k_mean=None, table=None)
+    assert lib.rsa_cache_workspace_bytes(ctypes.byref(long), ctypes.byref(_rows(heads=4)), 1, a, b) == 0 and a.value == 2 * 2 * 5 * 5000 * 4 and b.value > 0
     assert lib.rsa_cache_workspace_bytes(ctypes.byref(c), ctypes.byref(_rows(heads=4)), -1, a, b) == -5
     assert lib.rsa_cache_workspace_bytes(ctypes.byref(c), ctypes.byref(_rows(heads=3)), 0, a, b) == -2
 
@@ -125,13 +127,14 @@ def test_bad_arguments_are_refused(lib):
     assert select(ws=8) == -4
     assert select(cache=_cache(max_blocks=16385), n=16385) == -3
 
-    def attn(Q=ONE, kv=ONE, scale=0.0, flags=0, idx=None, kept=None, group=0, n=0, O=ONE, ws=None, nws=0):
-        return lib.rsa_cache_attn(by(c), by(R), Q, kv, None, scale, flags, idx, kept, group, n, O, None, ws, nws, None)
+    def attn(Q=ONE, kv=ONE, scale=0.0, flags=0, idx=None, kept=None, group=0, n=0, O=ONE, ws=None, nws=0, cache=c):
+        return lib.rsa_cache_attn(by(cache), by(R), Q, kv, None, scale, flags, idx, kept, group, n, O, None, ws, nws, None)
     assert attn(Q=None) == -1 and attn(kv=None) == -1 and attn(O=None) == -1 and attn(idx=ONE) == -1 and attn(kept=ONE) == -1
     assert attn(Q=264) == -2 and attn(O=264) == -2 and attn(scale=-1.0) == -5 and attn(scale=math.nan) == -5 and attn(scale=math.inf) == -5
     assert attn(flags=2) == -5 and attn(idx=ONE, kept=ONE, group=0, n=4) == -5 and attn(idx=ONE, kept=ONE, group=1, n=0) == -5
     assert attn(idx=ONE, kept=ONE, group=1, n=11) == -5
-    assert attn(ws=ONE, nws=16) == -4 and attn(ws=264, nws=1 << 30) == -4
+    assert attn(ws=ONE, nws=16, cache=_cache(max_blocks=100)) == -4 and attn(ws=264, nws=1 << 30) == -4
+    assert select(ws=ONE, cache=_cache(max_blocks=5000), n=10) == -4                     # scores need a workspace there
 
 
 def test_binding_refuses_cpu_tensors_and_wrong_buffers(lib):
