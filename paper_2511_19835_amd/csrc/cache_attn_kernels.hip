@@ -125,7 +125,7 @@ __device__ __forceinline__ void mark_nan(const uint4& w, const int (&left)[QT], 
 }
 
 template <int D, int BLK, int QT>
-__global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheDims c, RowDims r, CacheAttnArgs a, TileGrid tg) {
+__global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void cache_attn_kernel(CacheDims c, RowDims r, CacheAttnArgs a, TileGrid tg) {
   constexpr int KC = D / 64, VC = D / 16;          // 16-byte loads of a lane for 16 keys / for 64 keys
   constexpr int SPB = BLK / 64;                    // steps of 64 keys in a block
   constexpr int PITCH = D + 4;                     // floats of a row in the joining buffer
@@ -772,12 +772,14 @@ Plan plan_of(const CacheDims& c, const RowDims& r, int group, int list_len) {
   const int64_t steps = (int64_t)(list_len > 0 ? list_len : c.max_blocks) * (c.blk / 64);
   int64_t best = 1;
   if (p.tiled) {
-    // rounds of resident workgroups (two to a compute unit) times what one takes: its steps and, in steps, its start, its
-    // end and the parts that it leaves
+    // Rounds of workgroups over the slots (two to a compute unit), the last one between what it fills and whole; what one
+    // takes is its steps and, in steps, its start, its end and the parts that it leaves. 312 tiles of 317 steps in 1, 2, 3, 4, 5,
+    // 6, 8 parts: 613, 502, 427, 417, 453, 440, 430 us; 696 tiles of 186: 577, 572, 582, 571, 589, 609, 638.
+    const int64_t slots = 2 * kCus;
     int64_t cost = -1;
     for (int64_t s = 1; s <= 16 && s <= (steps + 7) / 8; ++s) {
-      const int64_t rounds = (p.tiles * s + 2 * kCus - 1) / (2 * kCus), one = (steps + s - 1) / s + (s > 1 ? 12 : 6);
-      if (cost < 0 || rounds * one < cost) { cost = rounds * one; best = s; }
+      const int64_t one = (steps + s - 1) / s + (s > 1 ? 12 : 6), all = one * (p.tiles * s + (p.tiles * s + slots - 1) / slots * slots);
+      if (cost < 0 || all < cost) { cost = all; best = s; }
     }
   } else {
     // Two workgroups to a compute unit at least, and parts of at most 64 steps, 16 to a wave, so that sequences of different

@@ -296,6 +296,10 @@ SHAPES = [  # d, block, G, t, lens, q_len, causal
     (128, 64, 16, 2, [250, 90, 3], None, True),
     (64, 128, 1, 200, [200, 1000, 333], [200, 150, 0], True),
     (128, 128, 2, 150, [1000, 150, 500], None, False),
+    (128, 64, 4, 1, [3000, 1, 1700], None, True),                 # long enough that the key axis is split
+    (64, 128, 1, 5, [2600, 5, 2049], [5, 4, 5], True),
+    (128, 128, 3, 9, [2000, 77, 1930], None, False),
+    (64, 64, 1, 100, [2100, 100, 1000], [100, 7, 64], True),
 ]
 
 
@@ -324,6 +328,19 @@ def test_attention_over_lists(d, block, G, t, group, causal, ws):
     # any list is taken: no order, entries that are none, blocks behind the last visible one, empty ones, a block twice
     odd = {k: [[], [7, 0, 100, -1, 2], [3, 3], [8, 1, -2147483648, 2147483647]][i % 4] for i, k in enumerate(lists)}
     compare(*attend(p, Q, lens, q_len, causal=causal, lists=odd, group=min(group, t), ws=ws), d)
+
+
+@pytest.mark.parametrize("ws", [True, False])
+@pytest.mark.parametrize("t,group,G", [(1, 1, 4), (20, 20, 1), (90, 90, 1)])
+def test_attention_over_long_lists(t, group, G, ws):
+    """Forty of fifty blocks, in any order, some without a page."""
+    table = np.random.default_rng(3).permutation(60)[:50].reshape(1, 50)
+    table[0, 7], table[0, 33] = -1, 60
+    p = Pair(1, 1, 128, 64, 50, table=table, pages=60)
+    p.fill([3150])
+    Q = video_like(p.rng, 1, G, t, 128)
+    lists = {(0, 0, 0): p.rng.permutation(50)[:40].tolist()}
+    compare(*attend(p, Q, [3150], causal=True, lists=lists, group=group, ws=ws), 128)
 
 
 def test_attention_passes_over_what_is_no_page():
