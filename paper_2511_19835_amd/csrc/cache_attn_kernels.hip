@@ -456,8 +456,8 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
     if (count == 0) continue;
     // what a step is, the same in every lane
     struct Step { int page, key; float ks; int ev; };
-    auto step_at = [&](int i) __attribute__((always_inline)) {
-      const int4 v = *reinterpret_cast<const int4*>(&look[min(i, count - 1)]);
+    auto entry = [&](int i) __attribute__((always_inline)) { return look[min(i, count - 1)]; };
+    auto step_of = [&](const int4& v) __attribute__((always_inline)) {
       Step z;
       z.page = __builtin_amdgcn_readfirstlane(v.x);
       z.key = __builtin_amdgcn_readfirstlane(v.y);
@@ -519,7 +519,7 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
         }
     };
 
-    Step now = step_at(0), next = step_at(1);
+    Step now = step_of(entry(0)), next = step_of(entry(1));
     request(now, raw_k, c.k, KC);
     request(now, raw_v, c.v, VW);
     if (now.key + 64 > t.lo_seen) clear_nan(0);
@@ -530,7 +530,7 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
     for (int i = 0; i < count; ++i) {
       __syncthreads();
       if (next.key + 64 > t.lo_seen) clear_nan((i + 1) & 1);
-      const Step later = step_at(i + 2);
+      const int4 ahead = entry(i + 2);
       const bool partly = now.key + 64 > t.lo_seen;
       if (partly) {
         const int4 f = *reinterpret_cast<const int4*>(odd[i & 1]);
@@ -557,10 +557,6 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
       __builtin_amdgcn_sched_group_barrier(0x008, QT * 4, 0);
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_s_setprio(0);
-      store_k((i + 1) & 1);
-      store_v((i + 1) & 1);
-      request(later, raw_k, c.k, KC);
-      request(later, raw_v, c.v, VW);
       if (partly) {
 #pragma unroll
         for (int x = 0; x < QT; ++x) {
@@ -630,6 +626,11 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
         l[x] += sum * back;
       }
       __builtin_amdgcn_sched_barrier(0);
+      store_k((i + 1) & 1);
+      store_v((i + 1) & 1);
+      const Step later = step_of(ahead);
+      request(later, raw_k, c.k, KC);
+      request(later, raw_v, c.v, VW);
       __builtin_amdgcn_s_setprio(1);
       const uint8_t* buf = lds_v[i & 1] + lane * 16;
 #pragma unroll
@@ -643,13 +644,13 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
             for (int x = 0; x < QT; ++x) o[x][vv] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op, p[x][hf], o[x][vv], 0, 0, 0);
           }
 #pragma unroll
-      for (int u = 0; u < 8; ++u) __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+      for (int u = 0; u < 4; ++u) __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
 #pragma unroll
-      for (int u = 0; u < 2 * VC - 8; ++u) {
+      for (int u = 0; u < 2 * VC - 4; ++u) {
         __builtin_amdgcn_sched_group_barrier(0x008, QT, 1);
         __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
       }
-      __builtin_amdgcn_sched_group_barrier(0x008, QT * 8, 1);
+      __builtin_amdgcn_sched_group_barrier(0x008, QT * 4, 1);
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_s_setprio(0);
       now = next;
