@@ -253,7 +253,8 @@ int rsa_sparse_attn_rectified_static(const rsa_shape* shape, const void* Q, cons
  * The mean of a page's keys (of the stored values of the tokens that it holds) is kept in 8 bits too:
  *   mean = int8 * 2^em,  em the least >= -100 with max |mean| <= 127 * 2^em.
  * Everything but the rounding to 4 (8) bits is exact, so that pages are the same bits however calls are cut,
- * up to values below 2^-6 of a block's scale that were rounded twice.
+ * up to values below 2^-6 of a block's scale that were rounded twice. (Values from 1.9375 * 2^127 on round to 2^128, which
+ * bf16 does not hold: they are read back as infinity.)
  *
  * A page of the codes is opaque but for its size; `scales` is {2^eK, 2^eV, 2^em, 0}. The library reads nothing of a page
  * that was not written; codes, scales and means need no initial values.
@@ -276,7 +277,8 @@ typedef struct rsa_cache {
  * strides in elements, multiples of 8; pointers 16-byte aligned. */
 typedef struct rsa_rows {
   int32_t heads;       /* K, V: heads_kv. Q, O: a multiple of heads_kv; head h reads key/value head h / (heads / heads_kv) */
-  int32_t t;           /* rows of a sequence, >= 1 (shorter sequences of a batch say so in `count` or `q_len`) */
+  int32_t t;           /* rows of a sequence, >= 1 (shorter sequences of a batch say so in `count` or `q_len`);
+                          batch * heads * t < 2^28 and no more than 2^23 workgroups (RSA_E_UNSUPPORTED) */
   int64_t stride_b, stride_h, stride_t;
 } rsa_rows;
 
@@ -287,7 +289,7 @@ typedef struct rsa_rows {
 int rsa_cache_bytes(const rsa_cache* cache, size_t* code_bytes, size_t* scale_bytes, size_t* mean_bytes);
 
 /* Host only. Bytes of device scratch of rsa_cache_select and rsa_cache_attn for queries `rows` in groups of `group`
- * (0: no lists), whatever list_len <= max_blocks. The pointers in `cache` may be NULL. */
+ * (0: no lists), whatever list_len. The pointers in `cache` may be NULL. */
 int rsa_cache_workspace_bytes(const rsa_cache* cache, const rsa_rows* rows, int group, size_t* select_ws_bytes,
                               size_t* attn_ws_bytes);
 
@@ -308,7 +310,8 @@ int rsa_cache_read(const rsa_cache* cache, const rsa_rows* rows, const int32_t* 
 
 /*
  * Query token i < q_len[b] of sequence b stands at position kv_len[b] - q_len[b] + i; its own key is in the cache
- * by then (kv_len: device int32 [batch], tokens in the cache; q_len NULL: all rows->t). Tokens are taken in groups of `group` >= 1
+ * by then (kv_len: device int32 [batch], tokens in the cache, less than 0 as 0; q_len NULL: all rows->t, more than rows->t
+ * counts as rows->t). A query before position 0 sees no key under RSA_CACHE_CAUSAL. Tokens are taken in groups of `group` >= 1
  * from i = 0 on; a group and a key/value head have one list, for all query heads that share it.
  *   visible   the blocks of the first kv_len[b] tokens; with RSA_CACHE_CAUSAL up to the block of the group's last position
  *   score     q8 . mean * 2^em, q8 the sum of the group's queries over its tokens and heads (finite values), rounded

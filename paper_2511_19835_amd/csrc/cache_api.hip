@@ -8,6 +8,8 @@ namespace {
 using rsa::CacheDims;
 using rsa::RowDims;
 
+constexpr int64_t kMostWorkgroups = (int64_t)1 << 23;       // of 256 threads
+
 bool misaligned(const void* p, uintptr_t bytes) { return ((uintptr_t)p & (bytes - 1)) != 0; }
 
 int make_cache(const rsa_cache* in, bool pointers, CacheDims* out) {
@@ -44,9 +46,9 @@ int make_rows(const rsa_rows* in, const CacheDims& c, bool queries, RowDims* out
   if (queries ? in->heads % c.heads_kv != 0 : in->heads != c.heads_kv) return RSA_E_SHAPE;
   if (in->stride_t < c.d || in->stride_b < 1 || in->stride_h < 1) return RSA_E_SHAPE;
   if ((in->stride_t % 8) || (in->stride_b % 8) || (in->stride_h % 8)) return RSA_E_SHAPE;
-  // a grid has at most a workgroup for every row and key/value head, or for every 64 tokens and two more
-  if ((int64_t)in->t * (in->heads / c.heads_kv) * c.batch * c.heads_kv >= ((int64_t)1 << 28) ||
-      ((int64_t)in->t / 64 + 2) * c.batch * c.heads_kv >= ((int64_t)1 << 31))
+  // a grid has less than 2^32 threads (a workgroup for 64 tokens of a key/value head, and two more; queries: see kMostWorkgroups)
+  if ((int64_t)in->t * in->heads * c.batch >= ((int64_t)1 << 28) ||
+      (!queries && ((int64_t)in->t / 64 + 2) * c.batch * c.heads_kv > kMostWorkgroups))
     return RSA_E_UNSUPPORTED;
   out->heads = in->heads;
   out->t = in->t;
@@ -134,6 +136,8 @@ int rsa_cache_select(const rsa_cache* cache, const rsa_rows* rows, const void* Q
   if (need < keep) need = keep;
   if (need > c.max_blocks) need = c.max_blocks;
   if (list_len < need) return RSA_E_RANGE;
+  // (sixteen waves to a workgroup)
+  if (((int64_t)(r.t - 1) / group + 1) * c.batch * c.heads_kv > kMostWorkgroups / 4) return RSA_E_UNSUPPORTED;
   if (ws && (misaligned(ws, 256) || ws_bytes < rsa::cache_select_ws_bytes(c, r, group))) return RSA_E_WORKSPACE;
   rsa::CacheSelectArgs a = {};
   a.Q = (const uint16_t*)Q;
@@ -165,7 +169,7 @@ int rsa_cache_attn(const rsa_cache* cache, const rsa_rows* rows, const void* Q, 
   if (misaligned(Q, 16) || misaligned(O, 16)) return RSA_E_SHAPE;
   if (flags & ~RSA_CACHE_CAUSAL) return RSA_E_RANGE;
   if (!(scale >= 0.f) || !isfinite(scale)) return RSA_E_RANGE;
-  if (block_idx && (group < 1 || list_len < 1 || list_len > c.max_blocks)) return RSA_E_RANGE;
+  if (block_idx && (group < 1 || list_len < 1)) return RSA_E_RANGE;
   rsa::CacheAttnArgs a = {};
   a.Q = (const uint16_t*)Q;
   a.kv_len = kv_len;
@@ -179,6 +183,7 @@ int rsa_cache_attn(const rsa_cache* cache, const rsa_rows* rows, const void* Q, 
   a.scale_log2e = (scale > 0.f ? scale : 1.0f / sqrtf((float)c.d)) * 1.4426950408889634f;
   a.O = (uint16_t*)O;
   a.lse = lse;
+  if (rsa::cache_attn_workgroups(c, r, block_idx ? a.group : 0, a.list_len) > kMostWorkgroups) return RSA_E_UNSUPPORTED;
   if (ws) {
     const size_t need = rsa::cache_attn_parts_bytes(c, r, block_idx ? a.group : 0, a.list_len);
     if (ws_bytes < need || misaligned(ws, 256)) return RSA_E_WORKSPACE;

@@ -770,7 +770,7 @@ Plan plan_of(const CacheDims& c, const RowDims& r, int group, int list_len) {
   p.grid.per_group = (int)((rows + p.grid.rows_per_tile - 1) / p.grid.rows_per_tile);
   p.grid.stored = (int)(rows < p.grid.rows_per_tile ? rows : p.grid.rows_per_tile);
   p.tiles = (int64_t)((r.t + per - 1) / per) * p.grid.per_group * c.batch * c.heads_kv;
-  const int64_t steps = (int64_t)(list_len > 0 ? list_len : c.max_blocks) * (c.blk / 64);
+  const int64_t steps = (int64_t)(list_len > 0 && list_len < c.max_blocks ? list_len : c.max_blocks) * (c.blk / 64);
   int64_t best = 1;
   if (p.tiled) {
     // Rounds of workgroups over the slots (two to a compute unit), the last one between what it fills and whole; what one
@@ -799,9 +799,14 @@ Plan plan_of(const CacheDims& c, const RowDims& r, int group, int list_len) {
       const int64_t a = (p.tiles * s + slots - 1) / slots, b = (p.tiles * best + slots - 1) / slots;
       if (a * best < b * s) best = s;
     }
-    if (steps <= 24) best = 1;
+    if (steps <= 24 || p.tiles >= 16 * slots) best = 1;       // (many tiles even out by themselves)
   }
   p.grid.splits = (int)(best < 1 ? 1 : best);
+  // never more parts than without a limit on the lists: the workspace is sized for that
+  if (steps < (int64_t)c.max_blocks * (c.blk / 64)) {
+    const int most = plan_of(c, r, group, 0).grid.splits;
+    if (p.grid.splits > most) p.grid.splits = most;
+  }
   return p;
 }
 
@@ -824,6 +829,11 @@ hipError_t launch_t(const CacheDims& c, const RowDims& r, const CacheAttnArgs& a
 
 }  // namespace
 
+int64_t cache_attn_workgroups(const CacheDims& c, const RowDims& r, int group, int list_len) {
+  const Plan p = plan_of(c, r, group, list_len);
+  return p.tiles * p.grid.splits;
+}
+
 size_t cache_attn_parts_bytes(const CacheDims& c, const RowDims& r, int group, int list_len) {
   const Plan p = plan_of(c, r, group, list_len);
   return p.grid.splits == 1 ? 0 : (size_t)p.tiles * p.grid.splits * p.grid.stored * (c.d + 1) * sizeof(float);
@@ -832,7 +842,6 @@ size_t cache_attn_parts_bytes(const CacheDims& c, const RowDims& r, int group, i
 hipError_t launch_cache_attn(const CacheDims& c, const RowDims& r, const CacheAttnArgs& a, hipStream_t s) {
   Plan p = plan_of(c, r, a.block_idx ? a.group : 0, a.block_idx ? a.list_len : 0);
   if (!a.parts) p.grid.splits = 1;
-  if (p.tiles * p.grid.splits >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
   if (c.d == 128) return c.blk == 128 ? launch_t<128, 128>(c, r, a, p, s) : launch_t<128, 64>(c, r, a, p, s);
   return c.blk == 128 ? launch_t<64, 128>(c, r, a, p, s) : launch_t<64, 64>(c, r, a, p, s);
 }

@@ -130,7 +130,9 @@ struct CacheAttnArgs {
   float* lse;
   float* parts;                      // NULL: the key axis is not split
 };
-// Bytes of `parts` that a call with lists of at most `list_len` blocks (0: no lists) takes.
+// Workgroups, and bytes of `parts`, that a call with lists of `list_len` blocks (0: no lists) takes; no more bytes than without
+// a limit on the lists.
+int64_t cache_attn_workgroups(const CacheDims& c, const RowDims& r, int group, int list_len);
 size_t cache_attn_parts_bytes(const CacheDims& c, const RowDims& r, int group, int list_len);
 hipError_t launch_cache_attn(const CacheDims& c, const RowDims& r, const CacheAttnArgs& a, hipStream_t s);
 

@@ -52,9 +52,9 @@ __device__ __forceinline__ int code_units(float x) { return x == x ? (int)(x * 5
 struct BlockSpan {
   int64_t first;   // token (in the new rows) of the block's slot 0; negative where older tokens precede
   int lo, hi;      // slots that get a new token
-  int page;
+  int page;        // -1: none
 };
-// The jth block that tokens [start, start + count) of sequence b touch. `there` false: none.
+// The jth block that tokens [start, start + count) of sequence b touch; false: there is none.
 template <int BLK>
 __device__ __forceinline__ bool touched_block(const CacheDims& c, int t, const int32_t* start, const int32_t* count, int b, int j, BlockSpan* out) {
   const int64_t s = start[b];
@@ -64,7 +64,6 @@ __device__ __forceinline__ bool touched_block(const CacheDims& c, int t, const i
   const int64_t blk = s / BLK + j, at = blk * BLK;
   if (at >= s + n || blk >= c.max_blocks) return false;
   out->page = cache_page(c, b, (int)blk);
-  if (out->page < 0) return false;
   out->first = at - s;
   out->lo = s > at ? (int)(s - at) : 0;
   out->hi = s + n - at < BLK ? (int)(s + n - at) : BLK;
@@ -85,9 +84,8 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheDims c, RowDims r
   const int b = bh / c.heads_kv, h = bh % c.heads_kv;
   BlockSpan sp;
   if (!touched_block<BLK>(c, r.t, a.start, a.count, b, j, &sp)) return;   // the whole workgroup
-  const int64_t rec = (int64_t)sp.page * c.heads_kv + h;
 
-  // new rows
+  // new rows (requested while the page is looked up)
   const int cc = tid % CPR, quad = tid / CPR;
   const bool mine = quad * 4 < BLK;
   const int64_t base = (int64_t)b * r.sb + (int64_t)h * r.sh + sp.first * r.st + cc * 8;
@@ -105,6 +103,9 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheDims c, RowDims r
         if (mine && slot >= sp.lo && slot < sp.hi) x[w][p][i] = *reinterpret_cast<const uint4*>(X + slot * r.st);
       }
   }
+  if (sp.page < 0) return;                         // (the whole workgroup)
+  const int64_t rec = (int64_t)sp.page * c.heads_kv + h;
+
   // what the block holds already (its first `lo` slots): 16-byte pieces tid, tid + 256, ...
   constexpr int PPT = PIECES / 256 > 0 ? PIECES / 256 : 1;
   const int prow = tid % 16, pg = tid / 16 % 4;    // of all pieces of a thread: key of 16 (K) or channel of 16 (V), and g
@@ -242,7 +243,8 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheDims c, RowDims r
 #pragma unroll
             for (int ch = 0; ch < 8; ++ch) {
               uint32_t* dst = reinterpret_cast<uint32_t*>(&codes[1][v_code_offset<D>(slot0, cc * 8 + ch)]);
-              *dst = hold ? (*dst & hold) | (cd[ch] & ~hold) : cd[ch];
+              if (hold) atomicOr(dst, cd[ch] & ~hold);                     // the others are zero; a read would wait for LDS
+              else *dst = cd[ch];
             }
           }
         }
@@ -290,7 +292,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheDims c, RowDims r,
   const int j = blockIdx.x % blocks, bh = blockIdx.x / blocks;
   const int b = bh / c.heads_kv, h = bh % c.heads_kv;
   BlockSpan sp;
-  if (!touched_block<BLK>(c, r.t, a.start, a.count, b, j, &sp)) return;
+  if (!touched_block<BLK>(c, r.t, a.start, a.count, b, j, &sp) || sp.page < 0) return;
   const int64_t rec = (int64_t)sp.page * c.heads_kv + h;
   for (int w = 0; w < 2; ++w) {
     const uint8_t* src = (w == 0 ? c.k : c.v) + rec * (BLK * D);

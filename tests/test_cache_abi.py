@@ -132,7 +132,10 @@ def test_bad_arguments_are_refused(lib):
     assert attn(Q=None) == -1 and attn(kv=None) == -1 and attn(O=None) == -1 and attn(idx=ONE) == -1 and attn(kept=ONE) == -1
     assert attn(Q=264) == -2 and attn(O=264) == -2 and attn(scale=-1.0) == -5 and attn(scale=math.nan) == -5 and attn(scale=math.inf) == -5
     assert attn(flags=2) == -5 and attn(idx=ONE, kept=ONE, group=0, n=4) == -5 and attn(idx=ONE, kept=ONE, group=1, n=0) == -5
-    assert attn(idx=ONE, kept=ONE, group=1, n=11) == -5
+    # more workgroups than a launch takes: refused by the host
+    many = _rows(heads=4, t=1 << 23, sb=(1 << 23) * 4 * 128, sh=(1 << 23) * 128)
+    assert lib.rsa_cache_attn(by(c), by(many), ONE, ONE, None, 0.0, 0, ONE, ONE, 1, 4, ONE, None, None, 0, None) == -3
+    assert lib.rsa_cache_select(by(c), by(many), ONE, ONE, None, 1, 4, 1, 1, 0, ONE, ONE, 10, None, 0, None) == -3
     assert attn(ws=ONE, nws=16, cache=_cache(max_blocks=100)) == -4 and attn(ws=264, nws=1 << 30) == -4
     assert select(ws=ONE, cache=_cache(max_blocks=5000), n=10) == -4                     # scores need a workspace there
 

@@ -91,7 +91,7 @@ class Pair:
                 np.testing.assert_array_equal(mean[page, h], p.mean)
 
 
-def attend(pair, Q, kv_len, q_len=None, scale=0.0, causal=False, lists=None, group=0, layout="bhtd", ws=True, stream=None):
+def attend(pair, Q, kv_len, q_len=None, scale=0.0, causal=False, lists=None, group=0, layout="bhtd", ws=True, stream=None, list_len=0):
     """rsa_cache_attn on Q (numpy) -> (outputs, lse) as numpy, rows that are no query checked to be untouched."""
     Qd = bf16(Q, layout)
     O = torch.full_like(Qd, 7.0)
@@ -100,7 +100,7 @@ def attend(pair, Q, kv_len, q_len=None, scale=0.0, causal=False, lists=None, gro
     idx = kept = None
     if lists is not None:
         groups = -(-Q.shape[2] // group)
-        n = max(1, max(len(x) for x in lists.values()))
+        n = max(1, list_len, max(len(x) for x in lists.values()))
         idx = torch.full((pair.batch, pair.hk, groups, n), -1, dtype=torch.int32)
         kept = torch.zeros(pair.batch, pair.hk, groups, dtype=torch.int32)
         for (b, h, g), x in lists.items():
@@ -327,7 +327,7 @@ def test_attention_over_lists(d, block, G, t, group, causal, ws):
     compare(*attend(p, Q, lens, q_len, causal=causal, lists=lists, group=min(group, t), ws=ws), d)
     # any list is taken: no order, entries that are none, blocks behind the last visible one, empty ones, a block twice
     odd = {k: [[], [7, 0, 100, -1, 2], [3, 3], [8, 1, -2147483648, 2147483647]][i % 4] for i, k in enumerate(lists)}
-    compare(*attend(p, Q, lens, q_len, causal=causal, lists=odd, group=min(group, t), ws=ws), d)
+    compare(*attend(p, Q, lens, q_len, causal=causal, lists=odd, group=min(group, t), ws=ws, list_len=70), d)   # longer than the table, too
 
 
 @pytest.mark.parametrize("ws", [True, False])
