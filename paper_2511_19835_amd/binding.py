@@ -412,10 +412,13 @@ def cached_sparse_attention(cache: KVCache, K, V, Q, O, kv_len, q_len, group: in
                             last: int = 1, flags: int = RSA_CACHE_CAUSAL, start=None, lse=None, ws=None, stream=None):
     """One step of a sequence of frames or tokens: the new rows into the cache, the blocks that each group of them reads, and
     their attention; three C-ABI calls on one stream, no host sync. `kv_len` counts the new rows, `start` = kv_len - q_len
-    (computed here when it is not given)."""
+    (computed here when it is not given; a q_len of more than all rows counts as all). `ws` holds the larger of the two
+    workspaces: the calls use it one after the other."""
+    if K.shape[2] != Q.shape[2]:
+        raise ValueError(f"a step brings keys and queries for the same rows: got {K.shape[2]} and {Q.shape[2]}")
     if start is None:
         with torch.cuda.stream(stream):                # (None: the current stream)
-            start = kv_len - (q_len if q_len is not None else Q.shape[2])
+            start = kv_len - (q_len.clamp(max=Q.shape[2]) if q_len is not None else Q.shape[2])
     rows_kv, rows = make_rows(K), make_rows(Q)
     rsa_cache_write(cache, rows_kv, K, V, start, q_len, stream)
     rsa_cache_select(cache, rows, Q, kv_len, q_len, group, keep, first, last, flags, block_idx, kept, ws, stream)

@@ -447,6 +447,24 @@ def test_a_sequence_step_by_step(d, block, G, steps):
         p.check_pages()
 
 
+def test_a_step_with_more_queries_than_rows():
+    """A q_len beyond the rows counts as all of them, for where the keys go as for the queries' positions."""
+    p = Pair(2, 1, 64, 64, 3)
+    p.fill([70, 9])
+    K, V, Q = (video_like(p.rng, 2, h, 3, 64) for h in (1, 1, 2))
+    Kd, Vd, Qd = bf16(K), bf16(V), bf16(Q)
+    lens, r = [73, 11], [99, 2]
+    p.ref.write(f64(Kd), f64(Vd), [70, 9], [3, 2])
+    idx, kept = torch.zeros(2, 1, 3, 4, dtype=torch.int32, device=DEV), torch.zeros(2, 1, 3, dtype=torch.int32, device=DEV)
+    O, lse = torch.full_like(Qd, 7.0), torch.full(Qd.shape[:3], 7.0, device=DEV)
+    rb.cached_sparse_attention(p.gpu, Kd, Vd, Qd, O, i32(lens), i32(r), 1, 2, idx, kept, lse=lse)
+    want = p.ref.select(f64(Qd), lens, [3, 2], 1, 2, 1, 1, True)
+    compare(f64(O), lse.cpu().double().numpy(), p.ref.attend(f64(Qd), lens, [3, 2], 0.0, True, want, 1), 64)
+    p.check_pages()
+    with pytest.raises(ValueError):
+        rb.cached_sparse_attention(p.gpu, Kd[:, :, :2], Vd[:, :, :2], Qd, O, i32(lens), None, 1, 2, idx, kept)
+
+
 def test_on_another_stream_and_replayed():
     """The three calls on a stream of their own, and captured into a graph that is replayed with new contents in between eager work."""
     p = Pair(2, 2, 128, 64, 6)
