@@ -8,6 +8,11 @@
 // One workgroup per (block of tokens that the call touches, sequence, key/value head), for K and V: the largest magnitude of
 // the new tokens decides the two exponents, so all rows of the block are in registers before the first code is made. The
 // codes go through LDS, where they are put in page order (cache_common.hpp), and leave in 16-byte pieces.
+//
+// Long writes and reads are bound by memory: 119 056 tokens of 24 heads of 128 written in 451 us (2.20 GB, 4.9 TB/s), 20 280 read in
+// 80 (0.37 GB, 4.6 TB/s); a copy of 1 GiB makes 5.2. One token is bound by latency, 7.6 us for eight of eight heads: a page's scales and codes,
+// the maximum, the codes in LDS, the mean, each waiting for the one before; so pieces stay in registers and sums go by lane
+// exchanges (11.0 us with exchanges through LDS and integer divisions).
 #include <type_traits>
 
 #include "cache_common.hpp"
