@@ -376,7 +376,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void cache_attn_kernel(CacheD
 // barrier a step of 64 keys: while a step is computed the codes of the next are widened and those of the one after are on
 // their way. 64 KB of LDS at d = 128, so that two workgroups share a compute unit and the softmax of one can run beside the
 // products of the other. 1560 queries of 24 heads over 20 280 keys: 382 us, 1020 TFLOP/s; the matrix pipe is busy 45 % of the time, the
-// vector ALU 51 and LDS 56. Codes are widened and written between the softmax and the values' products: 393 us, in front of the
+// vector ALU 51 and LDS 42. Codes are widened and written between the softmax and the values' products: 393 us, in front of the
 // scores 427, behind the values' products 411. Operands are read four ahead of their products (eight 396).
 constexpr int kAhead = 256;                        // steps that are looked up together
 template <int D, int BLK, int QT>
