@@ -15,7 +15,7 @@
 // The four waves of a workgroup take every fourth step of 64 keys and are joined in LDS; where there are few tiles the key
 // axis is also split over workgroups, whose normalised parts (fp32) cache_join_kernel adds in a fixed order.
 // Bound by memory: one token of 32 sequences of up to 32 768 tokens (8 heads of 128) 240 us at 5.7 TB/s, of one of 237 600 (24 heads)
-// 250 us at 5.8, from lists of blocks 44 us at 6.0; a copy of 1 GiB makes 5.2.
+// 250 us at 5.8, from lists of 64 blocks (268 MB) 52 us at 5.1; a copy of 1 GiB makes 5.2.
 #include "cache_common.hpp"
 
 namespace rsa {

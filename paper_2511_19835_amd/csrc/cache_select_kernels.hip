@@ -7,7 +7,7 @@
 // One workgroup per row = (sequence, key/value head, group): the sum of the queries (fp64: exact for bf16 terms within 40
 // binades of each other), the scores of all blocks as order-preserving keys, the threshold key by a histogram (keys in
 // registers, each wave owning a run of blocks), and the kept blocks in ascending order. What bounds it is latency and the
-// address unit: 256 rows of 512 blocks 8.3 us (its 17 MB of means would take 3.3), 696 rows of 929 19.0; the longest rows
+// address unit: 256 rows of 512 blocks 7.9 us (its 17 MB of means would take 3.3), 696 rows of 929 18.6; the longest rows
 // take sixteen waves. Where there are few rows and many blocks the scores are a launch of their own, in runs of blocks over
 // many workgroups.
 #include "cache_common.hpp"
@@ -36,19 +36,25 @@ constexpr int kRunBlocks = 1024;                   // blocks that a workgroup of
 struct Row {
   int b, hk, G;
   int t0, t1;                                      // its tokens
+  int t_end;                                       // the same as if every row were a query
   int seen;                                        // blocks that may be chosen: [0, seen)
   int lo_forced, hi_forced;                        // forced beside those below `first`
 };
+// Where a row stands, without the lengths (its t1, seen and forced blocks are set by add_lengths).
 __device__ __forceinline__ Row row_of(const CacheDims& c, const RowDims& r, const CacheSelectArgs& a, int row) {
   Row w;
   const int grp = row % a.groups, bh = row / a.groups;
   w.b = bh / c.heads_kv;
   w.hk = bh % c.heads_kv;
   w.G = r.heads / c.heads_kv;
-  const int shift = c.blk == 128 ? 7 : 6;          // (a shift of a negative position rounds down)
-  const int64_t kv = a.kv_len[w.b];
-  const int ql = a.q_len ? min(a.q_len[w.b], r.t) : r.t;
   w.t0 = grp * a.group;
+  w.t_end = min(w.t0 + a.group, r.t);
+  return w;
+}
+__device__ __forceinline__ void add_lengths(const CacheDims& c, const RowDims& r, const CacheSelectArgs& a, int kv_len, int q_len, Row& w) {
+  const int shift = c.blk == 128 ? 7 : 6;          // (a shift of a negative position rounds down)
+  const int64_t kv = kv_len;
+  const int ql = min(q_len, r.t);
   w.t1 = min(w.t0 + a.group, ql);
   const int64_t p0 = kv - ql + w.t0, p1 = kv - ql + w.t1 - 1;              // positions of the first and the last
   int64_t seen = a.causal ? max((p1 >> shift) + 1, (int64_t)0) : (kv + c.blk - 1) >> shift;
@@ -56,7 +62,6 @@ __device__ __forceinline__ Row row_of(const CacheDims& c, const RowDims& r, cons
   w.seen = (int)min(seen, (int64_t)c.max_blocks);
   w.lo_forced = a.last > 0 ? (int)max((int64_t)0, (p0 >> shift) - a.last + 1) : 0x7fffffff;
   w.hi_forced = a.last > 0 ? (int)(p1 >> shift) : -1;
-  return w;
 }
 
 template <int D>
@@ -70,7 +75,7 @@ constexpr int kQueryRows = 8;
 template <int D>
 __device__ __forceinline__ void request_queries(const RowDims& r, const CacheSelectArgs& a, const Row& w, int from, uint4 (&v)[kQueryRows]) {
   constexpr int CPR = D / 8, STRIPES = 256 / CPR;
-  const int cc = threadIdx.x % CPR, rows = (w.t1 - w.t0) * w.G;
+  const int cc = threadIdx.x % CPR, rows = (w.t_end - w.t0) * w.G;
   const uint16_t* Q = a.Q + (int64_t)w.b * r.sb + (int64_t)w.hk * w.G * r.sh + (int64_t)w.t0 * r.st + cc * 8;
   int i = from + (int)threadIdx.x / CPR, tok = i / w.G, head = i - tok * w.G;
   const int dt = STRIPES / w.G, dh = STRIPES - dt * w.G;       // (a division a row would take longer than the load)
@@ -96,6 +101,7 @@ __device__ __forceinline__ void sum_queries(const RowDims& r, const CacheSelectA
 #pragma unroll
     for (int u = 0; u < kQueryRows; ++u) {
       if (from + u * STRIPES >= rows) break;
+      if (from + u * STRIPES + tid / CPR >= rows) continue;               // (behind the last query)
       const uint32_t x[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -131,22 +137,39 @@ __device__ __forceinline__ void sum_queries(const RowDims& r, const CacheSelectA
   __syncthreads();
 }
 
+// What a row's scores need and no length decides, requested before the lengths are here (256 rows of 512 blocks 8.3 us without and 7.9
+// so, 696 of 929 19.0 and 18.6).
+template <int NI>
+struct Early {
+  int page[NI];
+  uint4 query[kQueryRows];
+};
+template <int D, int NI, int W>
+__device__ __forceinline__ Early<NI> request_early(const CacheDims& c, const RowDims& r, const CacheSelectArgs& a, const Row& w, int from) {
+  Early<NI> v;
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int m = from + (int)threadIdx.x + 64 * W * i;
+    v.page[i] = m < c.max_blocks ? c.table[(int64_t)w.b * c.max_blocks + m] : -1;
+  }
+  if (threadIdx.x < 256) request_queries<D>(r, a, w, 0, v.query);          // four waves' work
+  return v;
+}
+
 // Scores of blocks [from, to) of a row, NI to a thread, as order-preserving keys in keys[0 ..) (ends with a barrier). The loads
 // take turns in the address unit of the compute unit, so there are few: pages and scales once, a block to a lane, the means 16
 // channels to a lane, kRound passes requested together (pages lie anywhere: a round waits some 2500 cycles).
 // Pages and scales by the lanes of each mean: 929 blocks of 696 rows 23.7 us, now 19.0.
 template <int D, int NI, int W>
 __device__ __forceinline__ void score_blocks(const CacheDims& c, const RowDims& r, const CacheSelectArgs& a, const Row& w, int from, int to,
-                                             QueryLds<D>& L, uint32_t* keys) {
+                                             Early<NI>& early, QueryLds<D>& L, uint32_t* keys) {
   constexpr int kRound = W == 4 ? 16 : 8;
   constexpr int LPB = D / 16, BPP = 64 * W / LPB;  // lanes to a block, blocks to a pass
   const int tid = threadIdx.x, part = tid % LPB;
-  uint4 query[kQueryRows];
-  if (tid < 256) request_queries<D>(r, a, w, 0, query);     // four waves' work
   float scale[NI];
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
-    const int m = tid + 64 * W * i, page = from + m < to ? cache_page(c, w.b, from + m) : -1;
+    const int m = tid + 64 * W * i, page = from + m < to && early.page[i] >= 0 && early.page[i] < c.pages ? early.page[i] : -1;
     if (from + m < to) keys[m] = (uint32_t)page;
     scale[i] = -1.f;                               // there is no page
     if (page >= 0) scale[i] = c.scales[((int64_t)page * c.heads_kv + w.hk) * 4 + 2];
@@ -167,7 +190,7 @@ __device__ __forceinline__ void score_blocks(const CacheDims& c, const RowDims& 
     }
   };
   request(0);
-  sum_queries<D>(r, a, w, query, L);
+  sum_queries<D>(r, a, w, early.query, L);
   const int4 q = *reinterpret_cast<const int4*>(&L.q8[part * 16]);
   for (int at = 0; from + at < to; at += kRound * BPP) {
     if (at > 0) request(at);
@@ -203,10 +226,13 @@ __global__ __launch_bounds__(256) void cache_score_kernel(CacheDims c, RowDims r
   __shared__ QueryLds<D> L;
   __shared__ uint32_t keys[kRunBlocks];
   const int id = xcd_run(blockIdx.x, gridDim.x), row = id / runs;
-  const Row w = row_of(c, r, a, row);
-  const int from = id % runs * kRunBlocks, to = min(from + kRunBlocks, w.seen);
+  Row w = row_of(c, r, a, row);
+  const int kv_len = a.kv_len[w.b], q_len = a.q_len ? a.q_len[w.b] : r.t, from = id % runs * kRunBlocks;
+  Early<kRunBlocks / 256> early = request_early<D, kRunBlocks / 256, 4>(c, r, a, w, from);
+  add_lengths(c, r, a, kv_len, q_len, w);
+  const int to = min(from + kRunBlocks, w.seen);
   if (from >= to) return;
-  score_blocks<D, kRunBlocks / 256, 4>(c, r, a, w, from, to, L, keys);
+  score_blocks<D, kRunBlocks / 256, 4>(c, r, a, w, from, to, early, L, keys);
   uint32_t* out = (uint32_t*)a.ws + (int64_t)row * c.max_blocks;
   for (int m = from + (int)threadIdx.x; m < to; m += 256) out[m] = keys[m - from];
 }
@@ -385,13 +411,17 @@ __global__ __launch_bounds__(64 * W) void cache_select_kernel(CacheDims c, RowDi
   __shared__ ChoiceLds<W> choice;
   __shared__ uint32_t keys[SCORED ? 1 : 64 * W * NI];
   const int tid = threadIdx.x, row = xcd_run(blockIdx.x, gridDim.x);
-  const Row w = row_of(c, r, a, row);
+  Row w = row_of(c, r, a, row);
+  const int kv_len = a.kv_len[w.b], q_len = a.q_len ? a.q_len[w.b] : r.t;
+  Early<SCORED ? 1 : NI> early;
+  if constexpr (!SCORED) early = request_early<D, NI, W>(c, r, a, w, 0);
+  add_lengths(c, r, a, kv_len, q_len, w);
   if (w.seen <= 0) {                               // nothing to choose from (the whole workgroup)
     for (int i = tid; i < a.list_len; i += 64 * W) a.block_idx[(int64_t)row * a.list_len + i] = -1;
     if (tid == 0) a.kept[row] = 0;
     return;
   }
-  if (!SCORED) score_blocks<D, NI, W>(c, r, a, w, 0, w.seen, L, keys);
+  if constexpr (!SCORED) score_blocks<D, NI, W>(c, r, a, w, 0, w.seen, early, L, keys);
   choose<NI, W>(a, w, row, SCORED ? (const uint32_t*)a.ws + (int64_t)row * c.max_blocks : keys, choice);
 }
 
