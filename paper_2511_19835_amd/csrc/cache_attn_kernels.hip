@@ -25,6 +25,9 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNoReference = -3.0e38f;     // of a row that has seen no key; finite, so that differences stay defined
 constexpr float kLazy = 8.f;
 constexpr int kCus = 256;                    // compute units of an MI355X
+// Parts that a tile's keys are split into at most, for the few tiles of a long cache. us with 64, 128 and 256: a token of 32 heads on one
+// key/value head, 131 072 keys, 29, 23, 23; of 8 heads on 65 536 keys 16, 14, 17; 64 tokens of 8 heads on 131 072 keys 63, 55, 55 (16 parts: 187).
+constexpr int kMostParts = 128;
 
 // Sixteen codes as the bf16 / fp16 operands of two products (bytes 0-7 and 8-15).
 __device__ __forceinline__ void widen(const uint4& v, bf16x8 (&o)[2]) {
@@ -703,12 +706,12 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
 }
 
 // Parts of a tile's rows, weighted by their share of the softmax denominator and added in the order of the keys. A row
-// takes `lanes` (a power of two) threads to each chunk of eight channels, which share its parts: one thread alone waits for
-// one part after another (24 rows of 43 parts: 28.8 us with one, 5.1 with sixteen).
+// takes `lanes` (a power of two) threads to each chunk of eight channels, which share its parts, each over its own largest
+// log-sum-exp: one thread alone waits for one part after another (24 rows of 43 parts: 28.8 us with one, 5.1 with sixteen).
 template <int D>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheDims c, RowDims r, CacheAttnArgs a, TileGrid tg, int64_t tiles, int lanes) {
   constexpr int CPR = D / 8;
-  __shared__ float add[256][9];
+  __shared__ float add[256][10];
   const int G = r.heads / c.heads_kv;
   const int tid = threadIdx.x, ch = tid % CPR * 8, sl = tid / CPR % lanes;
   const int64_t u = (int64_t)blockIdx.x * (256 / CPR / lanes) + tid / CPR / lanes;
@@ -724,7 +727,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheDims c, RowDims r,
     const int64_t first = id * tg.splits;
     const float* part_lse = a.parts + tiles * tg.splits * tg.stored * D;
 #pragma unroll 4
-    for (int s = 0; s < tg.splits; ++s) most = fmaxf(most, part_lse[(first + s) * tg.stored + rr]);
+    for (int s = sl; s < tg.splits; s += lanes) most = fmaxf(most, part_lse[(first + s) * tg.stored + rr]);
 #pragma unroll 4
     for (int s = sl; s < tg.splits; s += lanes) {
       const float p = part_lse[(first + s) * tg.stored + rr];
@@ -740,12 +743,19 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheDims c, RowDims r,
 #pragma unroll
     for (int e = 0; e < 8; ++e) add[tid][e] = z[e];
     add[tid][8] = total;
+    add[tid][9] = most;
     __syncthreads();
     if (sl > 0) return;
-    for (int x = 1; x < lanes; ++x) {
+    for (int x = 1; x < lanes; ++x) most = fmaxf(most, add[tid + x * CPR][9]);
+    total = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] += add[tid + x * CPR][e];
-      total += add[tid + x * CPR][8];
+    for (int e = 0; e < 8; ++e) z[e] = 0.f;
+    for (int x = 0; x < lanes; ++x) {
+      const float* part = add[tid + x * CPR];
+      const float w = part[9] == -INFINITY ? 0.f : exp2f(part[9] - most);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] += w * part[e];
+      total += w * part[8];
     }
   }
   if (!is) return;
@@ -762,7 +772,9 @@ struct Plan {
   int64_t tiles;
   TileGrid grid;
 };
-// Up to 32 rows of a group: tiles of 16 or 32 rows whose keys the waves share out; more: tiles of 64 or 128 rows.
+// Up to 32 rows of a group: tiles of 16 or 32 rows whose keys the waves share out; more: tiles of 64 or 128 rows. us, 8 heads, four
+// sequences of 32 768 keys, d = 128, and sixteen of 8192, d = 64: 20 rows in tiles of 32 59 and 43, of 64 61 and 43; 40 rows in tiles
+// of 64 65 and 45, of 32 87 and 68, of 128 82 and 55; 80 rows in tiles of 128 88 and 58, of 64 109 and 76.
 Plan plan_of(const CacheDims& c, const RowDims& r, int group, int list_len) {
   Plan p;
   const int G = r.heads / c.heads_kv;
@@ -782,7 +794,7 @@ Plan plan_of(const CacheDims& c, const RowDims& r, int group, int list_len) {
     // 6, 8 parts: 613, 502, 427, 417, 453, 440, 430 us; 696 tiles of 186: 577, 572, 582, 571, 589, 609, 638.
     const int64_t slots = 2 * kCus;
     int64_t cost = -1;
-    for (int64_t s = 1; s <= 16 && s <= (steps + 7) / 8; ++s) {
+    for (int64_t s = 1; s <= kMostParts && s <= (steps + 7) / 8; ++s) {
       const int64_t one = (steps + s - 1) / s + (s > 1 ? 12 : 6), all = one * (p.tiles * s + (p.tiles * s + slots - 1) / slots * slots);
       if (cost < 0 || all < cost) { cost = all; best = s; }
     }
@@ -797,7 +809,7 @@ Plan plan_of(const CacheDims& c, const RowDims& r, int group, int list_len) {
     if (best < (steps + 63) / 64) best = (steps + 63) / 64;
     int64_t top = best + best / 2;
     if (top > (steps + 3) / 4) top = (steps + 3) / 4;
-    if (top > 64) top = 64;
+    if (top > kMostParts) top = kMostParts;
     if (best > top) best = top;
     for (int64_t s = best; s <= top; ++s) {        // less of its last round empty
       const int64_t a = (p.tiles * s + slots - 1) / slots, b = (p.tiles * best + slots - 1) / slots;

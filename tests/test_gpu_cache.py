@@ -373,6 +373,21 @@ def test_nan_stays_with_the_rows_that_see_it(t, G):
     compare(*attend(p, Q, [198, 198 - t // 2], causal=False), 128)            # behind the length: seen by nobody
 
 
+@pytest.mark.parametrize("d,t,G", [(64, 1, 8), (128, 3, 1), (64, 40, 1), (128, 1, 70)])
+def test_few_rows_of_a_long_cache(d, t, G):
+    """One key/value head, so that the key axis falls into as many parts as there ever are; a NaN in one of them."""
+    p = Pair(1, 1, d, 64, 480)
+    K = video_like(p.rng, 1, 1, 30001, d)
+    V = p.rng.normal(size=K.shape)
+    V[0, 0, 30000, 5] = np.nan
+    p.write(K, V, [0])
+    Q = p.rng.normal(size=(1, G, t, d)) * 0.3
+    compare(*attend(p, Q, [30000], causal=True), d)
+    O, lse, ref = attend(p, Q, [30001], causal=True)
+    assert np.isnan(ref["O"][0, :, -1]).any(-1).all()
+    compare(O, lse, ref, d)
+
+
 def test_blocks_of_very_different_size():
     """Scales from 2^-40 to 2^40 in one row, and rows that attend to the smallest values alone."""
     p = Pair(1, 1, 64, 64, 8)
