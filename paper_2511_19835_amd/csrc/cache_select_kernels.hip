@@ -296,8 +296,9 @@ __device__ __forceinline__ void choose(const CacheSelectArgs& a, const Row& w, i
   int ties = 0;
   if (by_score > 0) {
     const float smin = score_of(kmin), range = score_of(kmax) - smin;
-    const float steps = range > 0.f && range <= kLargest ? 255.f / range : 0.f;
-    auto step_of = [&](uint32_t k) __attribute__((always_inline)) { return (int)((score_of(k) - smin) * steps); };   // monotone
+    // Scores may be 2^-122 apart (means of 2^-100), where 255 / range passes 32 bits: the factor stays finite, and no score finds a step outside.
+    const float steps = range > 0.f && range <= kLargest ? fminf(255.f / range, kLargest) : 0.f;
+    auto step_of = [&](uint32_t k) __attribute__((always_inline)) { return min(max((int)((score_of(k) - smin) * steps), 0), 255); };   // monotone
 #pragma unroll
     for (int i = 0; i < NI; ++i)
       if (key[i] != kUnseen) atomicAdd(&L.hist[step_of(key[i])], 1);
@@ -397,7 +398,8 @@ __device__ __forceinline__ void choose(const CacheSelectArgs& a, const Row& w, i
   for (int i = 0; i < NI; ++i) {
     const bool keep = out >> i & 1;
     const unsigned long long all = __ballot(keep);
-    if (keep) list[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0))] = m0 + 64 * i + lane;
+    const int to = at + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
+    if (keep && to < want) list[to] = m0 + 64 * i + lane;                  // (want <= list_len: whatever the scores, nothing lands behind the list)
     at += __popcll(all);
   }
   for (int i = want + tid; i < a.list_len; i += 64 * W) list[i] = -1;

@@ -282,6 +282,31 @@ def test_select_long(blocks, keep, ws):
     select(p, p.rng.normal(size=(1, 2, 3, 128)), [blocks * 64], None, 1, keep, 1, 1, True, ws=ws)
 
 
+@pytest.mark.parametrize("ws", [True, False])
+@pytest.mark.parametrize("d,blocks,keep,most", [(128, 10, 3, 1), (64, 40, 7, 3), (128, 200, 9, 3), (64, 600, 50, 1), (128, 2000, 33, 3), (64, 4200, 90, 3)])
+def test_select_among_the_smallest_scores(d, blocks, keep, most, ws):
+    """Mean keys of 0 .. 3 times 2^-100 in a channel where the query's code is 1: scores 2^-122 apart, the least there are."""
+    p = Pair(1, 2, d, 64, blocks, table=np.arange(blocks).reshape(1, blocks) % 7, pages=7)
+    K = np.zeros((1, 2, 7 * 64, d))
+    K[..., 1] = np.repeat(p.rng.permutation(7) % (most + 1), 64) * 2.0 ** -100
+    p.write(K, K, [0])
+    p.check_pages()
+    Q = np.zeros((1, 4, 3, d))
+    Q[..., 0], Q[..., 1] = 127, 1                                              # (four heads, two to a key/value head: sums of 254 and 2)
+    guard = 500
+    Qd, kv = bf16(Q), i32([blocks * 64])
+    n = keep + 1
+    buf = torch.full((2 * 3 * n + guard,), 12345, dtype=torch.int32, device=DEV)
+    idx, kept = buf[:2 * 3 * n].view(1, 2, 3, n), torch.zeros(1, 2, 3, dtype=torch.int32, device=DEV)
+    rows = rb.make_rows(Qd)
+    scratch = torch.empty(max(256, rb.rsa_cache_workspace_bytes(p.gpu, rows, 1)[0]), dtype=torch.uint8, device=DEV) if ws else None
+    rb.rsa_cache_select(p.gpu, rows, Qd, kv, None, 1, keep, 0, 0, 0, idx, kept, scratch)
+    want = p.ref.select(f64(Qd), [blocks * 64], None, 1, keep, 0, 0, False)
+    assert (buf[2 * 3 * n:] == 12345).all()
+    for (b, h, g), x in want.items():
+        assert int(kept[b, h, g]) == keep and idx[b, h, g].tolist() == x + [-1], (b, h, g)
+
+
 # ---- attention -----------------------------------------------------------------------------------
 SHAPES = [  # d, block, G, t, lens, q_len, causal
     (64, 64, 1, 1, [1], None, True),                              # one key
