@@ -469,7 +469,8 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
       Step z;
       z.page = __builtin_amdgcn_readfirstlane(v.x);
       z.key = __builtin_amdgcn_readfirstlane(v.y);
-      z.ks = fmaxf(__builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(v.z)) * a.scale_log2e, 0x1p-126f);
+      // (above 0, so that a masked score stays -inf)
+      z.ks = fmaxf(__builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(v.z)) * a.scale_log2e, 0x1p-149f);
       z.ev = exponent_of(__builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(v.w)));
       return z;
     };

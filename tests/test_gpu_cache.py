@@ -439,6 +439,30 @@ def test_scores_far_from_zero():
         compare(*attend(p, Q, [384], scale=scale, causal=scale == 1.0), 128)
 
 
+KINDS = [(64, 1, 1), (128, 3, 8), (64, 40, 1), (128, 130, 1)]     # d, t, heads: tiles of 16 and 32 rows, of 64 and 128
+
+
+def one_channel(p, scores, values, Q0, d, G, t):
+    """Into an empty cache keys of one channel, `scores` [n], and `values` [n, d]; queries of about `Q0` in that channel."""
+    n = len(scores)
+    K = np.zeros((1, 1, n, d))
+    K[0, 0, :, 0] = scores
+    p.write(K, values.reshape(1, 1, n, d), [0])
+    Q = np.zeros((1, G, t, d))
+    Q[..., 0] = Q0 * np.linspace(0.98, 1.02, G * t).reshape(1, G, t)
+    return Q
+
+
+@pytest.mark.parametrize("d,t,G", KINDS)
+def test_the_smallest_keys(d, t, G):
+    """Keys of 2^-126 and more, queries of 2^123: the scale of the keys times that of the scores is below 2^-126."""
+    p = Pair(1, 1, d, 64, 3)
+    n = 150
+    s = p.rng.integers(-15, 16, size=n) * 2.0 ** -126
+    Q = one_channel(p, s, p.rng.normal(size=(n, d)), 2.0 ** 123, d, G, t)
+    compare(*attend(p, Q, [n]), d)
+
+
 def test_offsets_past_32_bits():
     """The same tokens in the first and in the last pages of a pool of more than 4 GiB of codes for K alone."""
     pages, hk, d, block = 33000, 8, 128, 128
