@@ -54,6 +54,25 @@ def test_oracle_token_by_token_is_the_same_as_at_once():
     np.testing.assert_allclose(O["O"][0, 0, 0], np.exp(s - s.max()) @ v / np.exp(s - s.max()).sum(), rtol=1e-12)
 
 
+@pytest.mark.parametrize("by", [20, 40, 100])
+def test_the_bound_of_a_row_is_made_of_its_own_keys(by):
+    """Zeros in place of the outputs are outside the bound of the attention's tests, also beside blocks of much larger values that the row
+    is not to read or gives no weight to."""
+    rng = np.random.default_rng(0)
+    c = co.Cache(1, 64, 64, [range(8)], 8)
+    K = rng.normal(size=(1, 1, 512, 64)) * 0.1
+    V = rng.normal(size=K.shape) * np.repeat(2.0 ** np.array([0, -by, 3, by, -2, by // 2, -by // 2, 1]), 64).reshape(1, 1, 512, 1)
+    K[0, 0, 3 * 64:4 * 64, 0] = -60.0                      # no weight on the block of the largest values
+    c.write(K, V, [0])
+    Q = rng.normal(size=(1, 1, 3, 64)) * 0.1
+    Q[..., 0] = 100.0
+    for own in ([1], [1, 6], [2, 3, 7]):
+        r = c.attend(Q, [512], None, 0.0, False, {(0, 0, 0): own}, 3)
+        es = (64 + 16) * 2.0 ** -24 * r["S"]
+        bound = 2.0 ** -8 * np.abs(r["O"]) + (2.0 ** -11 + 2 * es + 4 * r["n"] * 2.0 ** -24)[..., None] * r["A"] + (r["n"] * 2.0 ** -24 * r["vmax"])[..., None]
+        assert ((np.abs(r["O"]) > bound).mean(-1) > 0.9).all()
+
+
 # ---- refusals ------------------------------------------------------------------------------------
 ONE = 256                         # an address that is never read: validation fails first
 
