@@ -8,9 +8,11 @@
 // neither LDS nor a barrier; the codes go from memory into the registers that the products read. The scale of a block's
 // keys goes into the scores, that of its values into the exponent of P (below).
 //
-// P is rounded to fp16 (11 bits; V has 4): half a step is 2^-12 of p, against the output's own 2^-9 in bf16. Range: the
-// running reference m of a row follows its maximum lazily (only when a score passes it by more than 8 in log2), so p <= 2^8;
-// O is held over 2^eo, eo within 8 of the exponent of the values' scale, so what P carries for it is at most 2^8 again.
+// P is rounded to fp16 (11 bits; V has 4): half a step is 2^-11 of p, against the output's own 2^-8 in bf16. Range: the
+// running reference m of a row follows its maximum lazily (only when a score passes it by more than 8 in log2), so p <= 2^8. A
+// row's O is held over 2^eo; where eo is within kWindow above the exponent ev of a block's values, P takes 2^(ev - eo) with it,
+// and its sum gives the sum of the weights back exactly. Other blocks move eo first (follow_values), as far as O keeps all of
+// its bits; what is then still outside (a block that is nothing beside the row's O, or whose weights are) is summed apart.
 //
 // The four waves of a workgroup take every fourth step of 64 keys and are joined in LDS; where there are few tiles the key
 // axis is also split over workgroups, whose normalised parts (fp32) cache_join_kernel adds in a fixed order.
@@ -24,6 +26,7 @@ namespace {
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNoReference = -3.0e38f;     // of a row that has seen no key; finite, so that differences stay defined
 constexpr float kLazy = 8.f;
+constexpr int kWindow = 8;
 constexpr int kCus = 256;                    // compute units of an MI355X
 // Parts that a tile's keys are split into at most, for the few tiles of a long cache. us with 64, 128 and 256: a token of 32 heads on one
 // key/value head, 131 072 keys, 29, 23, 23; of 8 heads on 65 536 keys 16, 14, 17; 64 tokens of 8 heads on 131 072 keys 63, 55, 55 (16 parts: 187).
@@ -108,6 +111,45 @@ __device__ __forceinline__ Tile tile_of(const CacheDims& c, const RowDims& r, co
   return t;
 }
 
+// o * f * 2^e.
+__device__ __forceinline__ floatx4 scaled(const floatx4& o, float f, int e) {
+  floatx4 z;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) z[i] = ldexpf(o[i] * f, e);
+  return z;
+}
+// A block with values over 2^ev is outside some column's window: each column's eo goes to ev, but only so far that its largest |o| stays
+// within 2^-90 .. 2^60 (no bit of it is lost, and what the keys still add is at most 2^55), and then as far up as the block's own
+// weights, the largest of them 2^(most - m), ask for. The columns' lowest and highest eo are left in lo and hi, the same in every lane.
+template <int QT, int VC>
+__device__ __forceinline__ void follow_values(int ev, const float (&most)[QT], const float (&m)[QT], int (&eo)[QT], floatx4 (&o)[QT][VC], int& lo, int& hi) {
+  uint32_t low = 0, high = 0;                      // eo < 512
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    float big = 0.f, top = most[x];
+#pragma unroll
+    for (int v = 0; v < VC; ++v)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) big = fmaxf(big, fabsf(o[x][v][e]));
+    big = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, big), MaxF32()), MaxF32()));
+    top = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, top), MaxF32()), MaxF32()));
+    int to = ev;
+    if (big > 0.f) {
+      const int at = exponent_of(big), weight = (int)ceilf(fminf(fmaxf(top - m[x], -1000.f), 0.f));
+      to = max(min(max(ev, eo[x] - max(60 - at, 0)), eo[x] + max(at + 90, 0)), ev + weight);
+    }
+#pragma unroll
+    for (int v = 0; v < VC; ++v)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[x][v][e] = ldexpf(o[x][v][e], eo[x] - to);
+    eo[x] = to;
+    low = max(low, (uint32_t)(512 - to));
+    high = max(high, (uint32_t)(512 + to));
+  }
+  lo = 512 - __builtin_amdgcn_readfirstlane(over_row((int)low, MaxU32()));
+  hi = __builtin_amdgcn_readfirstlane(over_row((int)high, MaxU32())) - 512;
+}
+
 // One run of 16 value codes of a lane (channel tile v): where NaN stands under a key that a column sees (the first left[x] of
 // the 64), the column's output becomes NaN.
 template <int QT, int VC>
@@ -171,7 +213,9 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void cache_attn_kernel(CacheD
 #pragma unroll
     for (int v = 0; v < VC; ++v) o[x][v] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
-  int eo = -200, top = -200;                       // o is held over 2^eo; the largest exponent of a scale so far
+  int eo[QT], lo = -512, hi = -512;                // o is held over 2^eo; the lowest and the highest of the wave's columns
+#pragma unroll
+  for (int x = 0; x < QT; ++x) eo[x] = -512;
 
   const int u0 = (int)((int64_t)t.units * split / tg.splits), u1 = (int)((int64_t)t.units * (split + 1) / tg.splits);
   const int steps = (u1 - u0) * SPB;
@@ -258,6 +302,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void cache_attn_kernel(CacheD
             for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[x][y][e]);
           mx = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, mx), MaxF32()), MaxF32()));
           if (mx > m[x] + kLazy) {                 // the same in the four lanes of a column
+            mx = floorf(mx);                       // (whole, so that what is taken from it and what it rescales stays exact)
             const float down = exp2f(m[x] - mx);
             m[x] = mx;
             l[x] *= down;
@@ -266,32 +311,44 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void cache_attn_kernel(CacheD
           }
         }
       }
-      // the exponent of the values' scale: o follows it, P makes up for the rest
-      if (ev > eo || ev < eo - 8) {
-        top = max(top, ev);
-        const int to = max(ev, top - 80);          // o may grow by 2^80 and stay finite
-        if (to != eo) {
-          const int by = max(min(eo - to, 120), -126);
-          const float f = exp2_int(by);
+      bool apart = false;
+      if (ev > lo || ev < hi - kWindow) {
+        float most[QT];
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          most[x] = -INFINITY;
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) most[x] = fmaxf(most[x], s[x][y][e]);
+        }
+        follow_values<QT, VC>(ev, most, m, eo, o, lo, hi);
+        apart = ev > lo || ev < hi - kWindow;
+        if (apart) {
 #pragma unroll
           for (int x = 0; x < QT; ++x)
 #pragma unroll
-            for (int v = 0; v < VC; ++v) o[x][v] *= f;
-          eo = to;
+            for (int y = 0; y < 4; ++y)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) l[x] += __builtin_amdgcn_exp2f(s[x][y][e] - m[x]);
         }
       }
-      const float pe = exp2_int(max(ev - eo, -126));
       halfx8 p[QT][2];
 #pragma unroll
-      for (int x = 0; x < QT; ++x)
+      for (int x = 0; x < QT; ++x) {
+        const int over_o = ev - eo[x];             // P is over 2^(eo - ev), so that it goes with o
+        const float ref = m[x] - (float)over_o;
+        float sum = 0.f;
 #pragma unroll
         for (int y = 0; y < 4; ++y)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float w = __builtin_amdgcn_exp2f(s[x][y][e] - m[x]);
-            l[x] += w;
-            p[x][y / 2][y % 2 * 4 + e] = (_Float16)(w * pe);
+            const float w = __builtin_amdgcn_exp2f(s[x][y][e] - ref);
+            sum += w;
+            p[x][y / 2][y % 2 * 4 + e] = (_Float16)w;
           }
+        l[x] += apart ? 0.f : ldexpf(sum, -over_o);
+      }
 
       // a value that is NaN under a key that a row does not see must not reach it through 0 * NaN
       bool odd = false;
@@ -328,7 +385,6 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void cache_attn_kernel(CacheD
   }
 
   // join the four waves, 16 rows at a time
-  const float unit = eo < -126 ? 0.f : exp2_int(min(eo, 127));
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
     const float sum = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, l[x]), AddF32()), AddF32()));
@@ -344,10 +400,9 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void cache_attn_kernel(CacheD
     float total = 0.f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) total += join_l[w][n] * exp2f(join_m[w][n] - most);
-    const float f = total == 0.f ? 0.f : exp2f(m[x] - most) / total * unit;
+    const float f = total == 0.f ? 0.f : exp2f(m[x] - most) / total;
 #pragma unroll
-    for (int v = 0; v < VC; ++v)
-      *reinterpret_cast<floatx4*>(&join[wave][n][16 * v + 4 * g]) = o[x][v] * f;
+    for (int v = 0; v < VC; ++v) *reinterpret_cast<floatx4*>(&join[wave][n][16 * v + 4 * g]) = scaled(o[x][v], f, eo[x]);
     __syncthreads();
     constexpr int CPR = D / 8;
     for (int u = tid; u < 16 * CPR; u += 256) {
@@ -433,7 +488,9 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
 #pragma unroll
     for (int v = 0; v < VC; ++v) o[x][v] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
-  int eo = -200, top = -200;
+  int eo[QT], lo = -512, hi = -512;
+#pragma unroll
+  for (int x = 0; x < QT; ++x) eo[x] = -512;
 
   const int u0 = (int)((int64_t)t.units * split / tg.splits), u1 = (int)((int64_t)t.units * (split + 1) / tg.splits);
   const int steps = (u1 - u0) * SPB;
@@ -592,7 +649,7 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
 #pragma unroll
         for (int x = 0; x < QT; ++x) {
           const float mx = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, most[x]), MaxF32()), MaxF32()));
-          const float to = mx > m[x] + kLazy ? mx : m[x];           // the same in the four lanes of a column
+          const float to = mx > m[x] + kLazy ? floorf(mx) : m[x];   // the same in the four lanes of a column; whole, as above
           const float down = __builtin_amdgcn_exp2f(m[x] - to);
           m[x] = to;
           l[x] *= down;
@@ -600,25 +657,24 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
           for (int v = 0; v < VC; ++v) o[x][v] *= down;
         }
       }
-      if (now.ev > eo || now.ev < eo - 8) {
-        top = max(top, now.ev);
-        const int to = max(now.ev, top - 80);
-        if (to != eo) {
-          const float f = exp2_int(max(min(eo - to, 120), -126));
+      bool apart = false;
+      if (now.ev > lo || now.ev < hi - kWindow) {
+        follow_values<QT, VC>(now.ev, most, m, eo, o, lo, hi);
+        apart = now.ev > lo || now.ev < hi - kWindow;
+        if (apart) {
 #pragma unroll
           for (int x = 0; x < QT; ++x)
 #pragma unroll
-            for (int v = 0; v < VC; ++v) o[x][v] *= f;
-          eo = to;
+            for (int y = 0; y < 4; ++y)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) l[x] += __builtin_amdgcn_exp2f(fmaf(s[x][y][e], now.ks, -m[x]));
         }
       }
-      // P over 2^(eo - ev), so that it goes with o; the sums take it back
-      const int pe = max(now.ev - eo, -120);
-      const float back = exp2_int(-pe);
       halfx8 p[QT][2];
 #pragma unroll
       for (int x = 0; x < QT; ++x) {
-        const float ref = m[x] - (float)pe;
+        const int over_o = now.ev - eo[x];
+        const float ref = m[x] - (float)over_o;
         float sum = 0.f;
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
@@ -628,11 +684,11 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
             w[e] = __builtin_amdgcn_exp2f(fmaf(s[x][y][e], now.ks, -ref));
             sum += w[e];
           }
-          const halfx2 lo = __builtin_convertvector(floatx2{w[0], w[1]}, halfx2), hi = __builtin_convertvector(floatx2{w[2], w[3]}, halfx2);
-          p[x][y / 2][y % 2 * 4 + 0] = lo[0]; p[x][y / 2][y % 2 * 4 + 1] = lo[1];
-          p[x][y / 2][y % 2 * 4 + 2] = hi[0]; p[x][y / 2][y % 2 * 4 + 3] = hi[1];
+          const halfx2 lo2 = __builtin_convertvector(floatx2{w[0], w[1]}, halfx2), hi2 = __builtin_convertvector(floatx2{w[2], w[3]}, halfx2);
+          p[x][y / 2][y % 2 * 4 + 0] = lo2[0]; p[x][y / 2][y % 2 * 4 + 1] = lo2[1];
+          p[x][y / 2][y % 2 * 4 + 2] = hi2[0]; p[x][y / 2][y % 2 * 4 + 3] = hi2[1];
         }
-        l[x] += sum * back;
+        l[x] += apart ? 0.f : ldexpf(sum, -over_o);
       }
       __builtin_amdgcn_sched_barrier(0);
       store_k((i + 1) & 1);
@@ -668,7 +724,6 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
   }
 
   // rows out: normalised, turned through the wave's share of a buffer
-  const float unit = eo < -126 ? 0.f : exp2_int(min(eo, 127));
   constexpr int PITCH = D + 8;                     // bf16 of a row
   static_assert(4 * 16 * PITCH * 2 <= 2 * KBYTES, "rows of a wave do not fit");
   uint16_t* turn = reinterpret_cast<uint16_t*>(&lds_k[0][0]) + wave * 16 * PITCH;
@@ -676,7 +731,7 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
     const float total = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, l[x]), AddF32()), AddF32()));
-    const float f = total == 0.f ? 0.f : unit / total;
+    const float f = total == 0.f ? 0.f : 1.f / total;
     const int first = (wave * QT + x) * 16, row = t.row0 + first + n, tok = t.t0 + row / G;
     const float lse2 = total == 0.f ? -INFINITY : m[x] + log2f(total);
     const bool is = row < t.rows && tok < t.ql;
@@ -684,7 +739,7 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
       const int64_t at = (tile * tg.splits + split) * tg.stored + first + n;
       if (is) {
 #pragma unroll
-        for (int v = 0; v < VC; ++v) *reinterpret_cast<floatx4*>(a.parts + at * D + 16 * v + 4 * g) = o[x][v] * f;
+        for (int v = 0; v < VC; ++v) *reinterpret_cast<floatx4*>(a.parts + at * D + 16 * v + 4 * g) = scaled(o[x][v], f, eo[x]);
         if (g == 0) (a.parts + (int64_t)gridDim.x * tg.stored * D)[at] = lse2;
       }
       continue;
@@ -692,7 +747,7 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
     if (is && g == 0 && a.lse) a.lse[((int64_t)t.b * r.heads + t.hk * G + row % G) * r.t + tok] = lse2 * kLn2;
 #pragma unroll
     for (int v = 0; v < VC; ++v) {
-      const floatx4 z = o[x][v] * f;
+      const floatx4 z = scaled(o[x][v], f, eo[x]);
       *reinterpret_cast<uint2*>(turn + n * PITCH + 16 * v + 4 * g) = make_uint2(pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]));
     }
     __builtin_amdgcn_wave_barrier();               // (the wave's own rows: LDS keeps a wave's order)

@@ -463,6 +463,57 @@ def test_the_smallest_keys(d, t, G):
     compare(*attend(p, Q, [n]), d)
 
 
+@pytest.mark.parametrize("ws", [True, False])
+@pytest.mark.parametrize("d,t,G", KINDS)
+@pytest.mark.parametrize("first", [True, False])
+def test_small_weights_of_zero_values_count(first, d, t, G, ws):
+    """Blocks whose values are all zero hold two thirds of the softmax in weights of 2^-10, beside one with values of 2^90: their exponent
+    is 208 below its own."""
+    p = Pair(1, 1, d, 64, 40)
+    n = 40 * 64
+    s = np.full(n, -1.0)
+    v = np.zeros((n, d))
+    own = slice(0, 64) if first else slice(n - 64, n)
+    s[own] = -2.0
+    s[own.start] = 0.0
+    v[own] = p.rng.normal(size=(64, d)) * 2.0 ** 90
+    Q = one_channel(p, s, v, 10 * np.log(2), d, G, t)
+    compare(*attend(p, Q, [n], scale=1.0, ws=ws), d)
+
+
+@pytest.mark.parametrize("by", [30, 90, 110])
+@pytest.mark.parametrize("d,t,G", KINDS)
+def test_large_values_without_weight(d, t, G, by):
+    """Values 2^by times larger in the first, a middle and the last block, whose weights are e^-700 and less."""
+    for where in ([0], [5], [12], [0, 5, 12]):
+        p = Pair(1, 1, d, 64, 13)
+        n = 13 * 64
+        s = p.rng.integers(-8, 9, size=n) / 8.0
+        v = p.rng.normal(size=(n, d))
+        far = np.isin(np.arange(n) // 64, where)
+        s[far] = -240.0
+        v[far] *= 2.0 ** by
+        Q = one_channel(p, s, v, 3.0, d, G, t)
+        for ws in (True, False):
+            compare(*attend(p, Q, [n], scale=1.0, ws=ws), d)
+
+
+@pytest.mark.parametrize("by", [-110, -40, 40, 110, 200])
+@pytest.mark.parametrize("d,t,G", [(64, 70, 1), (128, 130, 1), (128, 8, 4), (64, 12, 1)])
+def test_rows_before_a_block_of_another_size(d, t, G, by):
+    """Causal rows on both sides of the border of a block whose values are 2^by times those before it: the rows of one tile hold outputs
+    of very different size."""
+    p = Pair(1, 1, d, 64, 7)
+    n = 6 * 64 + t // 2
+    K = p.rng.normal(size=(1, 1, n, d))
+    V = p.rng.normal(size=K.shape) * 2.0 ** (-100 if by > 120 else 0)
+    V[0, 0, 6 * 64:] *= 2.0 ** by
+    p.write(K, V, [0])
+    Q = p.rng.normal(size=(1, G, t, d))
+    for ws in (True, False):
+        compare(*attend(p, Q, [n], causal=True, ws=ws), d)
+
+
 def test_offsets_past_32_bits():
     """The same tokens in the first and in the last pages of a pool of more than 4 GiB of codes for K alone."""
     pages, hk, d, block = 33000, 8, 128, 128
