@@ -10,9 +10,10 @@
 //
 // P is rounded to fp16 (11 bits; V has 4): half a step is 2^-11 of p, against the output's own 2^-8 in bf16. Range: the
 // running reference m of a row follows its maximum lazily (only when a score passes it by more than 8 in log2), so p <= 2^8. A
-// row's O is held over 2^eo; where eo is within kWindow above the exponent ev of a block's values, P takes 2^(ev - eo) with it,
-// and its sum gives the sum of the weights back exactly. Other blocks move eo first (follow_values), as far as O keeps all of
-// its bits; what is then still outside (a block that is nothing beside the row's O, or whose weights are) is summed apart.
+// row's O is held over 2^eo; where eo is up to kAbove below the exponent ev of a block's values, P takes 2^(ev - eo) with it: at
+// most 2^15, and never less than p, so that a weight of 2^-14 keeps its 11 bits beside a block of larger values too (of 2^-21 where
+// no block's are larger). Its sum gives the sum of the weights back exactly. Other blocks move eo first (follow_values), as far as
+// O keeps all of its bits; what is then still outside (a block that is nothing beside the row's O, or whose weights are) is summed apart.
 //
 // The four waves of a workgroup take every fourth step of 64 keys and are joined in LDS; where there are few tiles the key
 // axis is also split over workgroups, whose normalised parts (fp32) cache_join_kernel adds in a fixed order.
@@ -26,7 +27,10 @@ namespace {
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNoReference = -3.0e38f;     // of a row that has seen no key; finite, so that differences stay defined
 constexpr float kLazy = 8.f;
-constexpr int kWindow = 8;
+constexpr int kAbove = 7;
+constexpr float kWhole = 0x1p23f;            // from here on a difference of a few from a score is rounded
+// The score up to which a row keeps its reference.
+__device__ __forceinline__ float lazy_limit(float m) { return fabsf(m) < kWhole ? m + kLazy : m; }
 constexpr int kCus = 256;                    // compute units of an MI355X
 // Parts that a tile's keys are split into at most, for the few tiles of a long cache. us with 64, 128 and 256: a token of 32 heads on one
 // key/value head, 131 072 keys, 29, 23, 23; of 8 heads on 65 536 keys 16, 14, 17; 64 tokens of 8 heads on 131 072 keys 63, 55, 55 (16 parts: 187).
@@ -118,7 +122,7 @@ __device__ __forceinline__ floatx4 scaled(const floatx4& o, float f, int e) {
   for (int i = 0; i < 4; ++i) z[i] = ldexpf(o[i] * f, e);
   return z;
 }
-// A block with values over 2^ev is outside some column's window: each column's eo goes to ev, but only so far that its largest |o| stays
+// A block with values over 2^ev is outside some column's window: each column's eo goes to ev - kAbove, but only so far that its largest |o| stays
 // within 2^-90 .. 2^60 (no bit of it is lost, and what the keys still add is at most 2^55), and then as far up as the block's own
 // weights, the largest of them 2^(most - m), ask for. The columns' lowest and highest eo are left in lo and hi, the same in every lane.
 template <int QT, int VC>
@@ -133,10 +137,11 @@ __device__ __forceinline__ void follow_values(int ev, const float (&most)[QT], c
       for (int e = 0; e < 4; ++e) big = fmaxf(big, fabsf(o[x][v][e]));
     big = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, big), MaxF32()), MaxF32()));
     top = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, top), MaxF32()), MaxF32()));
-    int to = ev;
+    const int aim = ev - kAbove;
+    int to = aim;
     if (big > 0.f) {
-      const int at = exponent_of(big), weight = (int)ceilf(fminf(fmaxf(top - m[x], -1000.f), 0.f));
-      to = max(min(max(ev, eo[x] - max(60 - at, 0)), eo[x] + max(at + 90, 0)), ev + weight);
+      const int at = exponent_of(big), weight = fabsf(m[x]) < kWhole ? (int)ceilf(fminf(fmaxf(top - m[x], -1000.f), 0.f)) : 0;
+      to = max(min(max(aim, eo[x] - max(60 - at, 0)), eo[x] + max(at + 90, 0)), aim + weight);
     }
 #pragma unroll
     for (int v = 0; v < VC; ++v)
@@ -205,10 +210,10 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void cache_attn_kernel(CacheD
       }
   }
   floatx4 o[QT][VC];
-  float m[QT], l[QT];
+  float m[QT], l[QT], limit[QT];                   // limit: up to which score m stays
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
-    m[x] = kNoReference;
+    m[x] = limit[x] = kNoReference;
     l[x] = 0.f;
 #pragma unroll
     for (int v = 0; v < VC; ++v) o[x][v] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -289,7 +294,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void cache_attn_kernel(CacheD
             float z = s[x][y][e] * ks;
             if (partly) z = 16 * y + 4 * g + e < left ? z : -INFINITY;
             s[x][y][e] = z;
-            over |= z > m[x] + kLazy;
+            over |= z > limit[x];
           }
       }
       if (__any(over)) {
@@ -301,10 +306,11 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void cache_attn_kernel(CacheD
 #pragma unroll
             for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[x][y][e]);
           mx = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, mx), MaxF32()), MaxF32()));
-          if (mx > m[x] + kLazy) {                 // the same in the four lanes of a column
+          if (mx > limit[x]) {                     // the same in the four lanes of a column
             mx = floorf(mx);                       // (whole, so that what is taken from it and what it rescales stays exact)
             const float down = exp2f(m[x] - mx);
             m[x] = mx;
+            limit[x] = lazy_limit(mx);
             l[x] *= down;
 #pragma unroll
             for (int v = 0; v < VC; ++v) o[x][v] *= down;
@@ -312,7 +318,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void cache_attn_kernel(CacheD
         }
       }
       bool apart = false;
-      if (ev > lo || ev < hi - kWindow) {
+      if (ev < hi || ev > lo + kAbove) {
         float most[QT];
 #pragma unroll
         for (int x = 0; x < QT; ++x) {
@@ -323,7 +329,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void cache_attn_kernel(CacheD
             for (int e = 0; e < 4; ++e) most[x] = fmaxf(most[x], s[x][y][e]);
         }
         follow_values<QT, VC>(ev, most, m, eo, o, lo, hi);
-        apart = ev > lo || ev < hi - kWindow;
+        apart = ev < hi || ev > lo + kAbove;
         if (apart) {
 #pragma unroll
           for (int x = 0; x < QT; ++x)
@@ -336,7 +342,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void cache_attn_kernel(CacheD
       halfx8 p[QT][2];
 #pragma unroll
       for (int x = 0; x < QT; ++x) {
-        const int over_o = ev - eo[x];             // P is over 2^(eo - ev), so that it goes with o
+        const int over_o = ev - eo[x];             // P takes 2^(ev - eo) with it, so that it goes with o
         const float ref = m[x] - (float)over_o;
         float sum = 0.f;
 #pragma unroll
@@ -480,10 +486,10 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
 #pragma unroll
     for (int k = 0; k < 2 * KC; ++k) asm volatile("" : "+v"(q[x][k]));
   floatx4 o[QT][VC];
-  float m[QT], l[QT];
+  float m[QT], l[QT], limit[QT];                   // limit: up to which score m stays
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
-    m[x] = kNoReference;
+    m[x] = limit[x] = kNoReference;
     l[x] = 0.f;
 #pragma unroll
     for (int v = 0; v < VC; ++v) o[x][v] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -643,24 +649,25 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
 #pragma unroll
           for (int e = 0; e < 4; e += 2) most[x] = fmaxf(fmaxf(most[x], s[x][y][e]), s[x][y][e + 1]);
         most[x] *= now.ks;
-        over |= most[x] > m[x] + kLazy;
+        over |= most[x] > limit[x];
       }
       if (__any(over)) {
 #pragma unroll
         for (int x = 0; x < QT; ++x) {
           const float mx = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, most[x]), MaxF32()), MaxF32()));
-          const float to = mx > m[x] + kLazy ? floorf(mx) : m[x];   // the same in the four lanes of a column; whole, as above
+          const float to = mx > limit[x] ? floorf(mx) : m[x];       // the same in the four lanes of a column; whole, as above
           const float down = __builtin_amdgcn_exp2f(m[x] - to);
           m[x] = to;
+          limit[x] = lazy_limit(to);
           l[x] *= down;
 #pragma unroll
           for (int v = 0; v < VC; ++v) o[x][v] *= down;
         }
       }
       bool apart = false;
-      if (now.ev > lo || now.ev < hi - kWindow) {
+      if (now.ev < hi || now.ev > lo + kAbove) {
         follow_values<QT, VC>(now.ev, most, m, eo, o, lo, hi);
-        apart = now.ev > lo || now.ev < hi - kWindow;
+        apart = now.ev < hi || now.ev > lo + kAbove;
         if (apart) {
 #pragma unroll
           for (int x = 0; x < QT; ++x)

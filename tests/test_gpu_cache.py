@@ -514,6 +514,40 @@ def test_rows_before_a_block_of_another_size(d, t, G, by):
         compare(*attend(p, Q, [n], causal=True, ws=ws), d)
 
 
+@pytest.mark.parametrize("ws", [True, False])
+@pytest.mark.parametrize("d,t,G", KINDS)
+def test_many_small_weights_beside_a_block_of_large_values(d, t, G, ws):
+    """One key has the weight 1, 4000 have some 2^-17 each and make up the first half of the channels alone; blocks of values 2^8 times
+    larger stand between them with no weight to speak of (2^-68)."""
+    p = Pair(1, 1, d, 64, 64)
+    n = 64 * 64
+    s = np.full(n, -1.0)
+    v = np.ones((n, d))
+    out = np.arange(n) // 64 % 16 < 4
+    s[out] = -4.0
+    v[out] *= 2.0 ** 8
+    s[300] = 0.0                                                               # the dominant key (block 4)
+    v[300, :d // 2] = 0
+    Q = one_channel(p, s, v, 17 * np.log(2), d, G, t)
+    compare(*attend(p, Q, [n], scale=1.0, ws=ws), d)
+
+
+@pytest.mark.parametrize("d,t,G", KINDS)
+@pytest.mark.parametrize("size", [2.0 ** 19, 2.0 ** 22, 2.0 ** 24])
+def test_scores_of_many_millions(size, d, t, G):
+    """Scores whose neighbours in 32 bits are 1/2 to 64 apart, rising along the keys, under values of different scales: the bound leaves the
+    weights open there, but an output is a mean of the values."""
+    p = Pair(1, 1, d, 64, 12)
+    n = 12 * 64
+    s = np.sort(p.rng.integers(-15, 16, size=n) / 1.0)
+    v = p.rng.uniform(1, 2, size=(n, d)) * np.repeat(2.0 ** p.rng.integers(0, 8, size=12), 64)[:, None]
+    Q = one_channel(p, s, v, size, d, G, t)
+    for sign in (1, -1):
+        O, lse, ref = attend(p, Q * sign, [n], scale=1.0)
+        compare(O, lse, ref, d)
+        assert O.min() >= 1 and O.max() <= 256
+
+
 def test_offsets_past_32_bits():
     """The same tokens in the first and in the last pages of a pool of more than 4 GiB of codes for K alone."""
     pages, hk, d, block = 33000, 8, 128, 128
