@@ -28,9 +28,15 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNoReference = -3.0e38f;     // of a row that has seen no key; finite, so that differences stay defined
 constexpr float kLazy = 8.f;
 constexpr int kAbove = 7;
-constexpr float kWhole = 0x1p23f;            // from here on a difference of a few from a score is rounded
-// The score up to which a row keeps its reference.
-__device__ __forceinline__ float lazy_limit(float m) { return fabsf(m) < kWhole ? m + kLazy : m; }
+// From scores of kWhole on a difference of a few is rounded: there a reference follows its maximum at once, which keeps P in range.
+constexpr float kWhole = 0x1p23f;
+template <int QT>
+__device__ __forceinline__ bool far_from_zero(const float (&m)[QT]) {   // of any column of the wave
+  bool far = false;
+#pragma unroll
+  for (int x = 0; x < QT; ++x) far |= fabsf(m[x]) >= kWhole && m[x] != kNoReference;
+  return __any(far);
+}
 constexpr int kCus = 256;                    // compute units of an MI355X
 // Parts that a tile's keys are split into at most, for the few tiles of a long cache. us with 64, 128 and 256: a token of 32 heads on one
 // key/value head, 131 072 keys, 29, 23, 23; of 8 heads on 65 536 keys 16, 14, 17; 64 tokens of 8 heads on 131 072 keys 63, 55, 55 (16 parts: 187).
@@ -210,10 +216,10 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void cache_attn_kernel(CacheD
       }
   }
   floatx4 o[QT][VC];
-  float m[QT], l[QT], limit[QT];                   // limit: up to which score m stays
+  float m[QT], l[QT], lazy = kLazy;
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
-    m[x] = limit[x] = kNoReference;
+    m[x] = kNoReference;
     l[x] = 0.f;
 #pragma unroll
     for (int v = 0; v < VC; ++v) o[x][v] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -294,7 +300,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void cache_attn_kernel(CacheD
             float z = s[x][y][e] * ks;
             if (partly) z = 16 * y + 4 * g + e < left ? z : -INFINITY;
             s[x][y][e] = z;
-            over |= z > limit[x];
+            over |= z > m[x] + lazy;
           }
       }
       if (__any(over)) {
@@ -306,16 +312,16 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void cache_attn_kernel(CacheD
 #pragma unroll
             for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[x][y][e]);
           mx = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, mx), MaxF32()), MaxF32()));
-          if (mx > limit[x]) {                     // the same in the four lanes of a column
+          if (mx > m[x] + lazy) {                  // the same in the four lanes of a column
             mx = floorf(mx);                       // (whole, so that what is taken from it and what it rescales stays exact)
             const float down = exp2f(m[x] - mx);
             m[x] = mx;
-            limit[x] = lazy_limit(mx);
             l[x] *= down;
 #pragma unroll
             for (int v = 0; v < VC; ++v) o[x][v] *= down;
           }
         }
+        if (far_from_zero<QT>(m)) lazy = 0.f;
       }
       bool apart = false;
       if (ev < hi || ev > lo + kAbove) {
@@ -342,8 +348,8 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void cache_attn_kernel(CacheD
       halfx8 p[QT][2];
 #pragma unroll
       for (int x = 0; x < QT; ++x) {
-        const int over_o = ev - eo[x];             // P takes 2^(ev - eo) with it, so that it goes with o
-        const float ref = m[x] - (float)over_o;
+        const int back = eo[x] - ev;               // P takes 2^(ev - eo) with it, so that it goes with o
+        const float ref = m[x] + (float)back;
         float sum = 0.f;
 #pragma unroll
         for (int y = 0; y < 4; ++y)
@@ -353,7 +359,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void cache_attn_kernel(CacheD
             sum += w;
             p[x][y / 2][y % 2 * 4 + e] = (_Float16)w;
           }
-        l[x] += apart ? 0.f : ldexpf(sum, -over_o);
+        l[x] += apart ? 0.f : ldexpf(sum, back);
       }
 
       // a value that is NaN under a key that a row does not see must not reach it through 0 * NaN
@@ -486,10 +492,10 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
 #pragma unroll
     for (int k = 0; k < 2 * KC; ++k) asm volatile("" : "+v"(q[x][k]));
   floatx4 o[QT][VC];
-  float m[QT], l[QT], limit[QT];                   // limit: up to which score m stays
+  float m[QT], l[QT], lazy = kLazy;
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
-    m[x] = limit[x] = kNoReference;
+    m[x] = kNoReference;
     l[x] = 0.f;
 #pragma unroll
     for (int v = 0; v < VC; ++v) o[x][v] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -649,23 +655,32 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
 #pragma unroll
           for (int e = 0; e < 4; e += 2) most[x] = fmaxf(fmaxf(most[x], s[x][y][e]), s[x][y][e + 1]);
         most[x] *= now.ks;
-        over |= most[x] > limit[x];
+        over |= most[x] > m[x] + lazy;
       }
       if (__any(over)) {
 #pragma unroll
         for (int x = 0; x < QT; ++x) {
           const float mx = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, most[x]), MaxF32()), MaxF32()));
-          const float to = mx > limit[x] ? floorf(mx) : m[x];       // the same in the four lanes of a column; whole, as above
+          const float to = mx > m[x] + lazy ? floorf(mx) : m[x];    // the same in the four lanes of a column; whole, as above
           const float down = __builtin_amdgcn_exp2f(m[x] - to);
           m[x] = to;
-          limit[x] = lazy_limit(to);
           l[x] *= down;
 #pragma unroll
           for (int v = 0; v < VC; ++v) o[x][v] *= down;
         }
+        if (far_from_zero<QT>(m)) lazy = 0.f;
+      }
+      // Far from zero the multiply-add below would leave a product's own rounding, which may be 2^8 and more: rounded products, as m is one
+      float ks = now.ks;
+      if (__builtin_expect(lazy == 0.f, 0)) {
+        ks = 1.f;
+#pragma unroll
+        for (int x = 0; x < QT; ++x)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) s[x][y] *= now.ks;
       }
       bool apart = false;
-      if (now.ev < hi || now.ev > lo + kAbove) {
+      if (__builtin_expect(now.ev < hi || now.ev > lo + kAbove, 0)) {
         follow_values<QT, VC>(now.ev, most, m, eo, o, lo, hi);
         apart = now.ev < hi || now.ev > lo + kAbove;
         if (apart) {
@@ -674,28 +689,28 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
 #pragma unroll
             for (int y = 0; y < 4; ++y)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) l[x] += __builtin_amdgcn_exp2f(fmaf(s[x][y][e], now.ks, -m[x]));
+              for (int e = 0; e < 4; ++e) l[x] += __builtin_amdgcn_exp2f(fmaf(s[x][y][e], ks, -m[x]));
         }
       }
       halfx8 p[QT][2];
 #pragma unroll
       for (int x = 0; x < QT; ++x) {
-        const int over_o = now.ev - eo[x];
-        const float ref = m[x] - (float)over_o;
+        const int back = eo[x] - now.ev;
+        const float ref = m[x] + (float)back;
         float sum = 0.f;
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
           float w[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            w[e] = __builtin_amdgcn_exp2f(fmaf(s[x][y][e], now.ks, -ref));
+            w[e] = __builtin_amdgcn_exp2f(fmaf(s[x][y][e], ks, -ref));
             sum += w[e];
           }
           const halfx2 lo2 = __builtin_convertvector(floatx2{w[0], w[1]}, halfx2), hi2 = __builtin_convertvector(floatx2{w[2], w[3]}, halfx2);
           p[x][y / 2][y % 2 * 4 + 0] = lo2[0]; p[x][y / 2][y % 2 * 4 + 1] = lo2[1];
           p[x][y / 2][y % 2 * 4 + 2] = hi2[0]; p[x][y / 2][y % 2 * 4 + 3] = hi2[1];
         }
-        l[x] += apart ? 0.f : ldexpf(sum, -over_o);
+        l[x] += apart ? 0.f : ldexpf(sum, back);
       }
       __builtin_amdgcn_sched_barrier(0);
       store_k((i + 1) & 1);

@@ -533,9 +533,9 @@ def test_many_small_weights_beside_a_block_of_large_values(d, t, G, ws):
 
 
 @pytest.mark.parametrize("d,t,G", KINDS)
-@pytest.mark.parametrize("size", [2.0 ** 19, 2.0 ** 22, 2.0 ** 24])
+@pytest.mark.parametrize("size", [2.0 ** 19, 2.0 ** 22, 2.0 ** 24, 2.0 ** 26, 2.0 ** 60, 2.0 ** 110])
 def test_scores_of_many_millions(size, d, t, G):
-    """Scores whose neighbours in 32 bits are 1/2 to 64 apart, rising along the keys, under values of different scales: the bound leaves the
+    """Scores whose neighbours in 32 bits are from 1/2 apart on, rising along the keys, under values of different scales: the bound leaves the
     weights open there, but an output is a mean of the values."""
     p = Pair(1, 1, d, 64, 12)
     n = 12 * 64
