@@ -256,8 +256,10 @@ int rsa_sparse_attn_rectified_static(const rsa_shape* shape, const void* Q, cons
  * up to values below 2^-6 of a block's scale that were rounded twice. (Values from 1.9375 * 2^127 on round to 2^128, which
  * bf16 does not hold: they are read back as infinity.)
  *
- * A page of the codes is opaque but for its size; `scales` is {2^eK, 2^eV, 2^em, 0}. The library reads nothing of a page
- * that was not written; codes, scales and means need no initial values.
+ * A page of the codes is opaque but for its size; `scales` is {2^eK, 2^eV, 2^em, 0}. Codes, scales and means need no initial
+ * values, but a page is to be written before it is used: those that the table gives for the first kv_len[b] tokens by selection and
+ * attention, those of a range by reading it, and by a write that begins inside a block the block's earlier tokens. Of a page
+ * that was not, calls read whatever it holds: their results say nothing then, but stay within their buffers.
  */
 typedef struct rsa_cache {
   int32_t batch;       /* sequences, >= 1 */

@@ -30,7 +30,7 @@ __device__ __forceinline__ double finite_or_zero(uint32_t bits16) {
 }
 constexpr uint32_t kUnseen = 0u;                   // below every score
 constexpr float kLargest = 3.4028234663852886e38f;
-constexpr uint32_t kLowest = 0x00800000u;          // key of -kLargest, also of what is no number (a page that was never written)
+constexpr uint32_t kLowest = 0x00800000u;          // key of -kLargest, also of what is no number
 constexpr int kRunBlocks = 1024;                   // blocks that a workgroup of the scoring launch takes
 
 struct Row {
@@ -171,8 +171,8 @@ __device__ __forceinline__ void score_blocks(const CacheDims& c, const RowDims& 
   for (int i = 0; i < NI; ++i) {
     const int m = tid + 64 * W * i, page = from + m < to && early.page[i] >= 0 && early.page[i] < c.pages ? early.page[i] : -1;
     if (from + m < to) keys[m] = (uint32_t)page;
-    scale[i] = -1.f;                               // there is no page
-    if (page >= 0) scale[i] = c.scales[((int64_t)page * c.heads_kv + w.hk) * 4 + 2];
+    scale[i] = -1.f;                               // there is no page; of one that there is the scale has no sign, whatever stands in memory
+    if (page >= 0) scale[i] = fabsf(c.scales[((int64_t)page * c.heads_kv + w.hk) * 4 + 2]);
   }
   __syncthreads();
   int page[kRound];

@@ -268,6 +268,26 @@ def test_select_where_pages_are_missing(ws):
     select(p, p.rng.normal(size=(2, 4, 2, 128)), [0, 1], [2, 2], 1, 6, 1, 2, True, ws=ws)       # a sequence without tokens; positions before the first
 
 
+@pytest.mark.parametrize("stray", [-1.0, 0.0, 1e-45, float("nan"), float("inf"), -3e38])
+def test_select_whatever_a_page_holds(stray):
+    """Scales of means as they may stand in memory that was never written: a block counts by its entry in the table, and as many as asked
+    for are listed."""
+    table = np.random.default_rng(2).permutation(90).reshape(1, 90)
+    table[0, 11] = -1
+    p = Pair(1, 2, 128, 64, 90, table=table, pages=90)
+    p.fill([90 * 64])
+    p.gpu.scales[torch.as_tensor(table[0, ::3].copy()).long().to(DEV), :, 2] = stray
+    Q = bf16(p.rng.normal(size=(1, 2, 1, 128)))
+    for keep in (30, 89, 90):
+        buf = torch.full((2 * 90 + 100,), 12345, dtype=torch.int32, device=DEV)
+        idx, kept = buf[:180].view(1, 2, 1, 90), torch.zeros(1, 2, 1, dtype=torch.int32, device=DEV)
+        rb.rsa_cache_select(p.gpu, rb.make_rows(Q), Q, i32([90 * 64]), None, 1, keep, 0, 0, 0, idx, kept)
+        assert kept.flatten().tolist() == [min(keep, 89)] * 2 and (buf[180:] == 12345).all()
+        for row in idx.view(2, 90).tolist():
+            own = row[:min(keep, 89)]
+            assert own == sorted(set(own)) and 0 <= own[0] and own[-1] < 90 and 11 not in own and row[len(own):] == [-1] * (90 - len(own))
+
+
 @pytest.mark.parametrize("ws", [True, False])
 @pytest.mark.parametrize("blocks,keep", [(1000, 100), (16384, 700)])
 def test_select_long(blocks, keep, ws):
