@@ -590,6 +590,61 @@ def test_offsets_past_32_bits():
     assert torch.equal(O[0], O[1]) and O.abs().max() > 0 and torch.equal(idx[0], idx[1])
 
 
+def pool(batch, hk, d, block, max_blocks, pages, seed=0):
+    """A Pair whose sequences take their blocks from the same few written pages (nothing is written through it afterwards)."""
+    p = Pair(batch, hk, d, block, max_blocks, seed, np.random.default_rng(seed + 1).integers(0, pages, size=(batch, max_blocks)), pages)
+    one = Pair(1, hk, d, block, pages, seed + 2, np.arange(pages).reshape(1, pages), pages)
+    one.gpu = rb.cache_of(p.gpu.k_codes, p.gpu.v_codes, p.gpu.scales, p.gpu.k_mean, one.gpu.table, block)
+    one.fill([pages * block], spread=0.5)
+    p.ref.held = one.ref.held
+    return p
+
+
+# ---- many rows, long tables ----------------------------------------------------------------------
+@pytest.mark.parametrize("ws", [True, False])
+@pytest.mark.parametrize("d,batch,hk,G,t,blocks,keep", [
+    (128, 3, 2, 2, 1, 1025, 100), (64, 3, 1, 1, 2, 2000, 150), (128, 2, 2, 1, 26, 1500, 40), (64, 2, 3, 2, 20, 4096, 64), (64, 3, 1, 4, 1, 4097, 300),
+    (128, 1, 1, 1, 3, 9000, 2000), (64, 2, 1, 1, 2, 16384, 64)])
+def test_select_from_long_tables(d, batch, hk, G, t, blocks, keep, ws):
+    """Every form of the choice, several sequences of different length, means and scales drawn directly."""
+    p = Pair(batch, hk, d, 64, blocks, table=np.random.default_rng(5).integers(-3, 200, size=(batch, blocks)), pages=200)
+    for page in range(200):
+        for h in range(hk):
+            q = p.ref.held.setdefault((page, h), co.Page(64, d))
+            q.mean, q.em = p.rng.integers(-127, 128, size=d), int(p.rng.integers(-9, -5))
+    p.gpu.k_mean.copy_(torch.as_tensor(np.array([[p.ref.held[i, h].mean for h in range(hk)] for i in range(200)])))
+    p.gpu.scales.copy_(torch.as_tensor(np.array([[[1, 1, 2.0 ** p.ref.held[i, h].em, 0] for h in range(hk)] for i in range(200)])))
+    lens = [blocks * 64 - i * (blocks * 64 // 3) for i in range(batch)]
+    select(p, p.rng.normal(size=(batch, hk * G, t, d)), lens, [max(1, t - i) for i in range(batch)], 1, keep, 1, 2, True, ws=ws)
+
+
+def test_attention_in_several_rounds_of_workgroups():
+    """76 rows on up to 6400 keys, each in parts, more workgroups than the chip takes at once."""
+    p = pool(19, 4, 128, 64, 100, 30)
+    lens = [6400 - 300 * i for i in range(19)]
+    compare(*attend(p, p.rng.normal(size=(19, 8, 1, 128)), lens, causal=True), 128)
+
+
+@pytest.mark.parametrize("d,t,G", [(64, 140, 1), (128, 75, 2)])
+def test_prompts_of_many_tiles(d, t, G):
+    """528 tiles of causal prompts, so that those of a sequence's last tokens go first: the same bits as a few sequences at a time."""
+    batch = 33
+    p = pool(batch, 8, d, 64, 3, 20)
+    lens, q_len = [t + i for i in range(batch)], [t - i % 5 for i in range(batch)]
+    Q = bf16(p.rng.normal(size=(batch, 8 * G, t, d)))
+    O, lse = torch.full_like(Q, 7.0), torch.full(Q.shape[:3], 7.0, device=DEV)
+    rb.rsa_cache_attn(p.gpu, rb.make_rows(Q), Q, i32(lens), i32(q_len), 0.0, rb.RSA_CACHE_CAUSAL, None, None, 0, O, lse)
+    for at in range(0, batch, 11):
+        part = Pair(11, 8, d, 64, 3, table=p.ref.table[at:at + 11], pages=20)
+        part.gpu = rb.cache_of(p.gpu.k_codes, p.gpu.v_codes, p.gpu.scales, p.gpu.k_mean, part.gpu.table, 64)
+        q, o, own = Q[at:at + 11], torch.full_like(Q[at:at + 11], 7.0), torch.full((11, 8 * G, t), 7.0, device=DEV)
+        rb.rsa_cache_attn(part.gpu, rb.make_rows(q), q, i32(lens[at:at + 11]), i32(q_len[at:at + 11]), 0.0, rb.RSA_CACHE_CAUSAL, None, None, 0, o, own)
+        assert torch.equal(O[at:at + 11].view(torch.int16), o.view(torch.int16)) and torch.equal(lse[at:at + 11], own)
+    few = slice(16, 18)
+    p.ref.table = p.ref.table[few]
+    compare(f64(O[few]), lse[few].cpu().double().numpy(), p.ref.attend(f64(Q[few]), lens[few], q_len[few], 0.0, True), d)
+
+
 # ---- together ------------------------------------------------------------------------------------
 @pytest.mark.parametrize("d,block,G,steps", [(128, 64, 2, [100, 1, 1, 5, 70, 1]), (64, 128, 1, [130, 128, 3, 1])])
 def test_a_sequence_step_by_step(d, block, G, steps):
