@@ -365,8 +365,12 @@ def _call(cache: KVCache, stream, where: str, fn, *args) -> None:
         raise RsaError(status, where)
 
 
-def _scratch(ws: Optional[torch.Tensor]):
-    return (None, 0) if ws is None else (_ptr(ws), ws.numel() * ws.element_size())
+def _scratch(cache: KVCache, ws: Optional[torch.Tensor]):
+    if ws is None:
+        return None, 0
+    if not ws.is_contiguous() or ws.device != cache.device:
+        raise ValueError(f"expect a contiguous workspace on {cache.device}, got strides {ws.stride()} on {ws.device}")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def rsa_cache_bytes(desc: rsa_cache):
@@ -395,7 +399,7 @@ def rsa_cache_read(cache: KVCache, rows, start, count, K, V, stream=None):
 def rsa_cache_select(cache: KVCache, rows, Q, kv_len, q_len, group, keep, first, last, flags, block_idx, kept, ws=None, stream=None):
     _lists(cache, rows, group, block_idx, kept)
     _call(cache, stream, "rsa_cache_select", _lib().rsa_cache_select, rows.ref, _row_tensor(cache, rows, Q), _lengths(cache, kv_len),
-          _lengths(cache, q_len), group, keep, first, last, flags, block_idx.data_ptr(), kept.data_ptr(), block_idx.shape[3], *_scratch(ws))
+          _lengths(cache, q_len), group, keep, first, last, flags, block_idx.data_ptr(), kept.data_ptr(), block_idx.shape[3], *_scratch(cache, ws))
 
 
 def rsa_cache_attn(cache: KVCache, rows, Q, kv_len, q_len, scale, flags, block_idx, kept, group, O, lse=None, ws=None, stream=None):
@@ -405,7 +409,7 @@ def rsa_cache_attn(cache: KVCache, rows, Q, kv_len, q_len, scale, flags, block_i
         _lists(cache, rows, group, block_idx, kept)
     _call(cache, stream, "rsa_cache_attn", _lib().rsa_cache_attn, rows.ref, _row_tensor(cache, rows, Q), _lengths(cache, kv_len),
           _lengths(cache, q_len), scale, flags, _ptr(block_idx), _ptr(kept), group, block_idx.shape[3] if block_idx is not None else 0,
-          _row_tensor(cache, rows, O), _ptr(lse), *_scratch(ws))
+          _row_tensor(cache, rows, O), _ptr(lse), *_scratch(cache, ws))
 
 
 def cached_sparse_attention(cache: KVCache, K, V, Q, O, kv_len, q_len, group: int, keep: int, block_idx, kept, first: int = 1,

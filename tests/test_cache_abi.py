@@ -173,3 +173,18 @@ def test_binding_refuses_cpu_tensors_and_wrong_buffers(lib):
         rb.make_rows(torch.zeros(1, 2, 3, 64))
     r = rb.make_rows(torch.zeros(1, 3, 2, 64, dtype=torch.bfloat16).transpose(1, 2))
     assert (r.heads, r.t, r.stride_h, r.stride_t) == (2, 3, 64, 128)
+
+
+def test_binding_refuses_a_workspace_elsewhere(lib):
+    """On another device than the cache, or a view that says more bytes than it has."""
+    on = lambda device: type("Tensor", (), dict(device=torch.device(device), is_cuda=True, is_contiguous=lambda self: True, stride=lambda self: (1,),
+                                                numel=lambda self: 1024, element_size=lambda self: 1, data_ptr=lambda self: 256))()
+    cache = type("Cache", (), dict(device=torch.device("cuda:0")))()
+    assert rb._scratch(cache, on("cuda:0")) == (256, 1024) and rb._scratch(cache, None) == (None, 0)
+    with pytest.raises(ValueError, match="workspace"):
+        rb._scratch(cache, on("cuda:1"))
+    with pytest.raises(ValueError, match="workspace"):
+        rb._scratch(cache, torch.zeros(1024, dtype=torch.uint8))
+    cache.device = torch.device("cpu")
+    with pytest.raises(ValueError, match="workspace"):
+        rb._scratch(cache, torch.zeros(1, dtype=torch.uint8).expand(1 << 20))
