@@ -334,7 +334,7 @@ int rsa_cache_select(const rsa_cache* cache, const rsa_rows* rows, const void* Q
  * O = softmax(scale * Q K^T) V over the cached tokens that a query sees: the first kv_len[b], with RSA_CACHE_CAUSAL
  * those up to its own position; with lists (block_idx and kept not NULL, as rsa_cache_select leaves them, `group`
  * as there) of the listed blocks only. Entries of a list that are negative or behind the last visible block are passed over; a block
- * listed twice counts twice. scale 0 selects 1/sqrt(head_dim). A query that sees no key gets 0 and a log-sum-exp of -inf. A NaN among
+ * listed twice counts twice. scale 0 selects 1/sqrt(head_dim); scale * log2(e) is to be finite in fp32 (RSA_E_RANGE). A query that sees no key gets 0 and a log-sum-exp of -inf. A NaN among
  * the stored keys or values reaches the queries that see its token and no others.
  * Without lists both pointers are NULL and `group` and `list_len` are ignored.
  *   O    as Q (may be Q). Rows behind q_len[b] are left as they were

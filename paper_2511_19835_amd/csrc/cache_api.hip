@@ -168,7 +168,8 @@ int rsa_cache_attn(const rsa_cache* cache, const rsa_rows* rows, const void* Q, 
   if (!Q || !kv_len || !O || !block_idx != !kept) return RSA_E_NULL;
   if (misaligned(Q, 16) || misaligned(O, 16)) return RSA_E_SHAPE;
   if (flags & ~RSA_CACHE_CAUSAL) return RSA_E_RANGE;
-  if (!(scale >= 0.f) || !isfinite(scale)) return RSA_E_RANGE;
+  const float scale_log2e = (scale > 0.f ? scale : 1.0f / sqrtf((float)c.d)) * 1.4426950408889634f;
+  if (!(scale >= 0.f) || !isfinite(scale_log2e)) return RSA_E_RANGE;
   if (block_idx && (group < 1 || list_len < 1)) return RSA_E_RANGE;
   rsa::CacheAttnArgs a = {};
   a.Q = (const uint16_t*)Q;
@@ -180,7 +181,7 @@ int rsa_cache_attn(const rsa_cache* cache, const rsa_rows* rows, const void* Q, 
   a.groups = (int)(((int64_t)r.t + a.group - 1) / a.group);
   a.list_len = block_idx ? list_len : 0;
   a.causal = flags & RSA_CACHE_CAUSAL;
-  a.scale_log2e = (scale > 0.f ? scale : 1.0f / sqrtf((float)c.d)) * 1.4426950408889634f;
+  a.scale_log2e = scale_log2e;
   a.O = (uint16_t*)O;
   a.lse = lse;
   if (rsa::cache_attn_workgroups(c, r, block_idx ? a.group : 0, a.list_len) > kMostWorkgroups) return RSA_E_UNSUPPORTED;

@@ -188,3 +188,10 @@ def test_binding_refuses_a_workspace_elsewhere(lib):
     cache.device = torch.device("cpu")
     with pytest.raises(ValueError, match="workspace"):
         rb._scratch(cache, torch.zeros(1, dtype=torch.uint8).expand(1 << 20))
+
+
+@pytest.mark.parametrize("scale", [3e38, 2.4e38, -1e-45, math.inf, -math.inf, math.nan])
+def test_scales_beyond_32_bits_are_refused(lib, scale):
+    """Scores are powers of two inside: 2.4e38 * log2(e) is none that fp32 holds."""
+    by = ctypes.byref
+    assert lib.rsa_cache_attn(by(_cache()), by(_rows(heads=4)), ONE, ONE, None, scale, 0, None, None, 0, 0, ONE, None, None, 0, None) == -5
