@@ -17,8 +17,8 @@
 //
 // The four waves of a workgroup take every fourth step of 64 keys and are joined in LDS; where there are few tiles the key
 // axis is also split over workgroups, whose normalised parts (fp32) cache_join_kernel adds in a fixed order.
-// Bound by memory: one token of 32 sequences of up to 32 768 tokens (8 heads of 128) 240 us at 5.7 TB/s, of one of 237 600 (24 heads)
-// 250 us at 5.8, from lists of 64 blocks (268 MB) 52 us at 5.1; a copy of 1 GiB makes 5.2.
+// Bound by memory: one token of 32 sequences of up to 32 768 tokens (8 heads of 128) 241 us at 5.7 TB/s, of one of 237 600 (24 heads)
+// 246 us at 5.9, from lists of 64 blocks (268 MB) 52 us at 5.1; reading 1.46 GB in long pieces makes 6.1, a copy of 1 GiB 5.2.
 #include "cache_common.hpp"
 
 namespace rsa {
@@ -128,6 +128,15 @@ __device__ __forceinline__ floatx4 scaled(const floatx4& o, float f, int e) {
   for (int i = 0; i < 4; ++i) z[i] = ldexpf(o[i] * f, e);
   return z;
 }
+// No block was seen yet: the first decides, there is nothing to move.
+constexpr int kNoScale = -512;
+template <int QT>
+__device__ __forceinline__ void begin_values(int ev, int (&eo)[QT], int& lo, int& hi) {
+  if (lo != kNoScale) return;
+  lo = hi = ev - kAbove;
+#pragma unroll
+  for (int x = 0; x < QT; ++x) eo[x] = lo;
+}
 // A block with values over 2^ev is outside some column's window: each column's eo goes to ev - kAbove, but only so far that its largest |o| stays
 // within 2^-90 .. 2^60 (no bit of it is lost, and what the keys still add is at most 2^55), and then as far up as the block's own
 // weights, the largest of them 2^(most - m), ask for. The columns' lowest and highest eo are left in lo and hi, the same in every lane.
@@ -224,9 +233,9 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void cache_attn_kernel(CacheD
 #pragma unroll
     for (int v = 0; v < VC; ++v) o[x][v] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
-  int eo[QT], lo = -512, hi = -512;                // o is held over 2^eo; the lowest and the highest of the wave's columns
+  int eo[QT], lo = kNoScale, hi = kNoScale;                // o is held over 2^eo; the lowest and the highest of the wave's columns
 #pragma unroll
-  for (int x = 0; x < QT; ++x) eo[x] = -512;
+  for (int x = 0; x < QT; ++x) eo[x] = kNoScale;
 
   const int u0 = (int)((int64_t)t.units * split / tg.splits), u1 = (int)((int64_t)t.units * (split + 1) / tg.splits);
   const int steps = (u1 - u0) * SPB;
@@ -260,7 +269,11 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void cache_attn_kernel(CacheD
       for (int x = 0; x < VC; ++x) vc[x] = *reinterpret_cast<const uint4*>(p + x * 1024);
     };
     int i = todo ? __builtin_ctzll(todo) : -1;
-    if (i >= 0) { load_k(i); load_v(i); }
+    if (i >= 0) {
+      load_k(i);
+      load_v(i);
+      begin_values<QT>(exponent_of(__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, my_v), i))), eo, lo, hi);
+    }
     while (i >= 0) {
       todo &= todo - 1;
       const int next = todo ? __builtin_ctzll(todo) : -1;
@@ -447,8 +460,8 @@ __global__ __launch_bounds__(256, QT == 1 ? 2 : 1) void cache_attn_kernel(CacheD
 // barrier a step of 64 keys: while a step is computed the codes of the next are widened and those of the one after are on
 // their way. 64 KB of LDS at d = 128, so that two workgroups share a compute unit and the softmax of one can run beside the
 // products of the other. 1560 queries of 24 heads over 20 280 keys: 382 us, 1020 TFLOP/s; the matrix pipe is busy 45 % of the time, the
-// vector ALU 51 and LDS 42. Codes are widened and written between the softmax and the values' products: 393 us, in front of the
-// scores 427, behind the values' products 411. Operands are read four ahead of their products (eight 396).
+// vector ALU 53 and LDS 42. Codes are widened and written between the softmax and the values' products, and operands read four ahead of their
+// products (when that was chosen, on a slower box: 393 us; widened in front of the scores 427, behind the values' products 411; eight ahead 396).
 constexpr int kAhead = 256;                        // steps that are looked up together
 template <int D, int BLK, int QT>
 __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims r, CacheAttnArgs a, TileGrid tg) {
@@ -500,9 +513,9 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
 #pragma unroll
     for (int v = 0; v < VC; ++v) o[x][v] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
-  int eo[QT], lo = -512, hi = -512;
+  int eo[QT], lo = kNoScale, hi = kNoScale;
 #pragma unroll
-  for (int x = 0; x < QT; ++x) eo[x] = -512;
+  for (int x = 0; x < QT; ++x) eo[x] = kNoScale;
 
   const int u0 = (int)((int64_t)t.units * split / tg.splits), u1 = (int)((int64_t)t.units * (split + 1) / tg.splits);
   const int steps = (u1 - u0) * SPB;
@@ -598,6 +611,7 @@ __global__ __launch_bounds__(256, 2) void cache_tile_kernel(CacheDims c, RowDims
     };
 
     Step now = step_of(entry(0)), next = step_of(entry(1));
+    begin_values<QT>(now.ev, eo, lo, hi);
     request(now, raw_k, c.k, KC);
     request(now, raw_v, c.v, VW);
     if (now.key + 64 > t.lo_seen) clear_nan(0);
@@ -870,7 +884,7 @@ Plan plan_of(const CacheDims& c, const RowDims& r, int group, int list_len) {
   if (p.tiled) {
     // Rounds of workgroups over the slots (two to a compute unit, three at d = 64), the last one between what it fills and whole; what one
     // takes is its steps and, in steps, its start, its end and the parts that it leaves. 312 tiles of 317 steps in 1, 2, 3, 4, 5,
-    // 6, 8 parts: 613, 502, 427, 417, 453, 440, 430 us; 696 tiles of 186: 577, 572, 582, 571, 589, 609, 638.
+    // 6, 8 parts: 512, 501, 382, 409, 442, 406, 406 us; 696 tiles of 186: 572, 531, 559, 550, 559, 583, 609.
     // Three slots at d = 64 and two: 1000 tokens of 12 heads on 30 000 keys 137 and 148 us, 64 of 16 x 8 heads on 8192 46 and 49.
     const int64_t slots = (c.d == 64 ? 3 : 2) * kCus;
     int64_t cost = -1;
