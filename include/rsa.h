@@ -242,8 +242,8 @@ int rsa_sparse_attn_rectified_static(const rsa_shape* shape, const void* Q, cons
  *
  * A page holds one block of `block` tokens of all key/value heads; `table` says which page each block of
  * a sequence is. Entries that are no page (negative, or >= pages) hold no tokens: what is written there
- * is dropped, attention and selection pass over them, reading leaves those rows as they were. A page may stand in several rows of the
- * table (a shared prefix) as long as no write reaches it through two of them at once.
+ * is dropped, attention and selection pass over them, reading leaves those rows as they were. A page may stand in several places of
+ * the table (a shared prefix) as long as no call writes it through two of them.
  *
  * Codes are e4m3 with one power-of-two scale for each (page, key/value head) of K and of V:
  *   value = code * 2^e,  e the least >= -126 with max |value| <= 448 * 2^e,  rounded to nearest even.
@@ -334,8 +334,12 @@ int rsa_cache_select(const rsa_cache* cache, const rsa_rows* rows, const void* Q
  * O = softmax(scale * Q K^T) V over the cached tokens that a query sees: the first kv_len[b], with RSA_CACHE_CAUSAL
  * those up to its own position; with lists (block_idx and kept not NULL, as rsa_cache_select leaves them, `group`
  * as there) of the listed blocks only. Entries of a list that are negative or behind the last visible block are passed over; a block
- * listed twice counts twice. scale 0 selects 1/sqrt(head_dim); scale * log2(e) is to be finite in fp32 (RSA_E_RANGE). A query that sees no key gets 0 and a log-sum-exp of -inf. A NaN among
- * the stored keys or values reaches the queries that see its token and no others.
+ * listed twice counts twice. scale 0 selects 1/sqrt(head_dim); scale * log2(e) is to be finite in fp32 (RSA_E_RANGE). A query
+ * that sees no key gets 0 and a log-sum-exp of -inf. A NaN among the stored keys or values reaches the queries that see its token
+ * and no others. Scores and sums are fp32 (queries times codes, that times 2^eK * scale, have to stay in its range), weights
+ * are rounded to fp16: beside the rounding of O to bf16 and those of the fp32 steps an output is off by at most 2^-11 of
+ * sum p |v|, and for every key by 2^-24 of half the largest value of its block's codes (448 * 2^eV), but no more than p |v|, both over sum p with
+ * the largest p 1: weights below 2^-24 may vanish, however large their values.
  * Without lists both pointers are NULL and `group` and `list_len` are ignored.
  *   O    as Q (may be Q). Rows behind q_len[b] are left as they were
  *   lse  (nullable) [batch][heads][t] fp32, natural log of the softmax denominator including the maximum

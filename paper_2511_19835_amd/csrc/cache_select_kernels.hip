@@ -7,7 +7,7 @@
 // One workgroup per row = (sequence, key/value head, group): the sum of the queries (fp64: exact for bf16 terms within 40
 // binades of each other), the scores of all blocks as order-preserving keys, the threshold key by a histogram (keys in
 // registers, each wave owning a run of blocks), and the kept blocks in ascending order. What bounds it is latency and the
-// address unit: 256 rows of 512 blocks 7.9 us (its 17 MB of means would take 3.3), 696 rows of 929 18.6; the longest rows
+// address unit: 256 rows of 512 blocks 8.3 us (its 17 MB of means would take 2.8), 696 rows of 929 19.2; the longest rows
 // take sixteen waves. Where there are few rows and many blocks the scores are a launch of their own, in runs of blocks over
 // many workgroups.
 #include "cache_common.hpp"
@@ -138,7 +138,7 @@ __device__ __forceinline__ void sum_queries(const RowDims& r, const CacheSelectA
 }
 
 // What a row's scores need and no length decides, requested before the lengths are here (256 rows of 512 blocks 8.3 us without and 7.9
-// so, 696 of 929 19.0 and 18.6).
+// so, 696 of 929 19.0 and 18.6, both on one box).
 template <int NI>
 struct Early {
   int page[NI];
