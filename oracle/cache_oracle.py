@@ -93,11 +93,6 @@ class Cache:
                 K[t - lo], V[t - lo], there[t - lo] = p.k[t % self.block], p.v[t % self.block], True
         return K, V, there
 
-    def units(self, b, h, lo, hi):
-        """2^e of the codes of the values of tokens lo..hi-1 (0 without a page)."""
-        pages = [self.held.get((self.page_of(b, t // self.block), h)) for t in range(lo, hi)]
-        return np.array([0.0 if p is None else 2.0 ** p.ev for p in pages])
-
     def select(self, Q, kv_len, q_len, group, keep, first, last, causal):
         """Q [batch, heads, t, d] fp64 -> {(b, head, group): ascending list}."""
         B, H, t, d = Q.shape
@@ -126,10 +121,10 @@ class Cache:
         return out
 
     def attend(self, Q, kv_len, q_len, scale, causal, lists=None, group=0):
-        """Outputs, log-sum-exps and the parts of the error bound of every row: A = sum p |v| and S = the largest sum |q||k| * scale; n
-        keys; and `vmax`, 2^24 times what one of them costs whose weight is below fp16's normal range: half a step, 2^-25 of the
-        largest value 448 * 2^e of its block's codes, but no more than the weight itself, p |v|; the mean over the keys, over the sum of the
-        weights. NaN where a row is not a query."""
+        """Outputs, log-sum-exps and the parts of the error bound of every row. 2^-11 A is what the weights' rounding to fp16 costs an
+        output: half a step is 2^-11 p, from 2^-14 on down 2^-25, and never more than the weight itself, so A = sum min(max(p, 2^-14), 2^11 p) |v|
+        over sum p, the largest p being 1. S is the largest sum |q||k| * scale, n the number of keys; nothing is left for `vmax`, which is 0. NaN where a
+        row is not a query."""
         B, H, t, d = Q.shape
         G = H // self.hk
         scale = scale or d ** -0.5
@@ -141,8 +136,6 @@ class Cache:
             kv, ql = max(int(kv_len[b]), 0), t if q_len is None else min(int(q_len[b]), t)
             for hk in range(self.hk):
                 K, V, there = self.rows(b, hk, 0, kv)
-                unit = self.units(b, hk, 0, kv)
-                most = np.nanmax(np.where(np.isnan(V), 0, np.abs(V)), axis=1, initial=0) if kv else unit
                 for i in range(max(ql, 0)):
                     end = min(max(kv - ql + i + 1, 0), kv) if causal else kv
                     if lists is None:
@@ -161,9 +154,8 @@ class Cache:
                             m = s.max()
                             p = np.exp(s - m)
                             O[b, h, i] = p @ V[keys] / p.sum()
-                            A[b, h, i] = p @ np.abs(V[keys]) / p.sum()
+                            A[b, h, i] = np.minimum(np.maximum(p, 2.0 ** -14), 2.0 ** 11 * p) @ np.abs(V[keys]) / p.sum()
                             lse[b, h, i] = np.log(p.sum()) + m
                             S[b, h, i] = (np.abs(K[keys]) @ np.abs(Q[b, h, i])).max() * scale
-                            vmax[b, h, i] = np.fmin(LARGEST / 2 * unit[keys], 2.0 ** 24 * p * most[keys]).mean() / p.sum()
                         n[b, h, i] = len(keys)
         return dict(O=O, A=A, lse=lse, S=S, n=n, vmax=vmax, isq=isq)

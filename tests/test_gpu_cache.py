@@ -4,13 +4,12 @@ What a write leaves, what is read back, the means behind the scores and the list
 the attention are held to a bound made of its roundings, for each element:
 
   |O - O64| <= 2^-8 |O64|                         the output in bf16: half a step
-             + (2^-11 + 2 e_s + 4 n 2^-24) A      P in fp16: half a step of 2^-11 of each p; scores off by e_s change p by e_s of
-                                                  itself, above and below the division; sums of n terms in 32 bits, each way
-             + n 2^-24 max|v|                     P below fp16's normal range: half a step of 2^-24, over a scale of up to twice max|v|
+             + (2^-11 + 2 e_s + 4 n 2^-24) A      P in fp16: half a step of 2^-11 of each p, of 2^-25 below 2^-14; scores off by e_s change
+                                                  p by e_s of itself, above and below the division; sums of n terms in 32 bits, each way
   e_s = (d + 16) 2^-24 max_j sum|q||k_j| * scale  the dot product in 32 bits and the few operations behind it
   |lse - lse64| <= 2 e_s + 4 n 2^-24 + 2^-21 max(1, |lse|)
 
-with A = sum p |v| over the same keys.
+with A = sum min(max(p, 2^-14), 2^11 p) |v| over the same keys and over sum p, the largest p being 1 (oracle: vmax is 0).
 """
 import numpy as np
 import pytest
