@@ -337,9 +337,9 @@ int rsa_cache_select(const rsa_cache* cache, const rsa_rows* rows, const void* Q
  * listed twice counts twice. scale 0 selects 1/sqrt(head_dim); scale * log2(e) is to be finite in fp32 (RSA_E_RANGE). A query
  * that sees no key gets 0 and a log-sum-exp of -inf. A NaN among the stored keys or values reaches the queries that see its token
  * and no others. Scores and sums are fp32 (queries times codes, that times 2^eK * scale, have to stay in its range), weights
- * are rounded to fp16: beside the rounding of O to bf16 and those of the fp32 steps an output is off by at most 2^-11 of
- * sum p |v|, and for every key by 2^-24 of half the largest value of its block's codes (448 * 2^eV), but no more than p |v|, both over sum p with
- * the largest p 1: weights below 2^-24 may vanish, however large their values.
+ * are rounded to fp16: beside the rounding of O to bf16 and those of the fp32 steps an output is off by at most
+ * sum max(2^-11 p, 2^-25) |v| / sum p, the largest p being 1, where the blocks that a row gives weight to are over scales within 2^60 of each other
+ * (weights below 2^-25 may vanish, however large their values).
  * Without lists both pointers are NULL and `group` and `list_len` are ignored.
  *   O    as Q (may be Q). Rows behind q_len[b] are left as they were
  *   lse  (nullable) [batch][heads][t] fp32, natural log of the softmax denominator including the maximum

@@ -138,7 +138,7 @@ __device__ __forceinline__ void begin_values(int ev, int (&eo)[QT], int& lo, int
   for (int x = 0; x < QT; ++x) eo[x] = lo;
 }
 // A block with values over 2^ev is outside some column's window: each column's eo goes to ev - kAbove, but only so far that its largest |o| stays
-// within 2^-90 .. 2^60 (no bit of it is lost, and what the keys still add is at most 2^55), and then as far up as the block's own
+// within 2^-90 .. 2^100 (no bit of it is lost, and what the keys still add is at most 2^55), and then as far up as the block's own
 // weights, the largest of them 2^(most - m), ask for. The columns' lowest and highest eo are left in lo and hi, the same in every lane.
 template <int QT, int VC>
 __device__ __forceinline__ void follow_values(int ev, const float (&most)[QT], const float (&m)[QT], int (&eo)[QT], floatx4 (&o)[QT][VC], int& lo, int& hi) {
@@ -156,7 +156,7 @@ __device__ __forceinline__ void follow_values(int ev, const float (&most)[QT], c
     int to = aim;
     if (big > 0.f) {
       const int at = exponent_of(big), weight = fabsf(m[x]) < kWhole ? (int)ceilf(fminf(fmaxf(top - m[x], -1000.f), 0.f)) : 0;
-      to = max(min(max(aim, eo[x] - max(60 - at, 0)), eo[x] + max(at + 90, 0)), aim + weight);
+      to = max(min(max(aim, eo[x] - max(100 - at, 0)), eo[x] + max(at + 90, 0)), aim + weight);
     }
 #pragma unroll
     for (int v = 0; v < VC; ++v)

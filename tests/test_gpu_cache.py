@@ -567,6 +567,25 @@ def test_scores_of_many_millions(size, d, t, G):
         assert O.min() >= 1 and O.max() <= 256
 
 
+@pytest.mark.parametrize("by", [20, 60, 76])
+@pytest.mark.parametrize("d,t,G", KINDS)
+def test_channels_that_only_the_small_blocks_fill(d, t, G, by):
+    """Every block has weight; values 2^by times larger stand in every fourth one and leave the first half of the channels zero, which the
+    others make up alone."""
+    for shift in (0, 3):
+        p = Pair(1, 1, d, 64, 16)
+        n = 16 * 64
+        s = p.rng.integers(-8, 9, size=n) / 8.0
+        v = p.rng.uniform(1, 2, size=(n, d))
+        far = (np.arange(n) // 64 + shift) % 4 == 0
+        v[far] *= 2.0 ** by
+        v[far, :d // 2] = 0
+        Q = one_channel(p, s, v, 1.0, d, G, t)
+        for ws in (True, False):
+            compare(*attend(p, Q, [n], scale=1.0, ws=ws), d)
+
+
+
 def test_offsets_past_32_bits():
     """The same tokens in the first and in the last pages of a pool of more than 4 GiB of codes for K alone."""
     pages, hk, d, block = 33000, 8, 128, 128
