@@ -140,6 +140,7 @@ __device__ __forceinline__ void begin_values(int ev, int (&eo)[QT], int& lo, int
 // A block with values over 2^ev is outside some column's window: each column's eo goes to ev - kAbove, but only so far that its largest |o| stays
 // within 2^-90 .. 2^100 (no bit of it is lost, and what the keys still add is at most 2^55), and then as far up as the block's own
 // weights, the largest of them 2^(most - m), ask for. The columns' lowest and highest eo are left in lo and hi, the same in every lane.
+// Rare: scales of 2^3 apart cost nothing; a frame on 20 280 keys with every second block 2^10 times larger takes 490 us instead of 383.
 template <int QT, int VC>
 __device__ __forceinline__ void follow_values(int ev, const float (&most)[QT], const float (&m)[QT], int (&eo)[QT], floatx4 (&o)[QT][VC], int& lo, int& hi) {
   uint32_t low = 0, high = 0;                      // eo < 512
