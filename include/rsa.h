@@ -350,6 +350,123 @@ int rsa_cache_attn(const rsa_cache* cache, const rsa_rows* rows, const void* Q, 
                    const int32_t* q_len, float scale, int flags, const int32_t* block_idx, const int32_t* kept, int group,
                    int list_len, void* O, float* lse, void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * The same cache in 4 bits: half the memory and half the bytes that an attention over it reads. The record is rsa_cache, with
+ * code buffers of the sizes that rsa_fourbit_bytes says; rsa_cache_select works on either cache (it reads the means, their scales
+ * and the table). The other calls of one cache must not be given the other's buffers.
+ *
+ * Codes are e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign) over a power of two: one for each 32 channels of a key, one for each value row
+ *   value = code * 2^e,  e the least >= -124 with max |value| <= 6 * 2^e over those channels,  rounded to nearest even.
+ * A token's codes depend on its own rows alone, so pages are the same bits however calls are cut, and nothing is rounded twice.
+ * Channels that share a scale with an infinity or NaN are all stored as NaN (and count neither for e nor for the mean). (Values
+ * from 1.75 * 2^127 on round to 2^128, which is read back as infinity.) The mean of a page's keys is what it is in 8 bits, over
+ * the stored values, summed in 64 bits; scales[..][2] is its 2^em, the rest of `scales` is 0.
+ */
+
+/* Host only. Bytes of k_codes, v_codes, scales and k_mean; the pointers in `cache` may be NULL here. */
+int rsa_fourbit_bytes(const rsa_cache* cache, size_t* k_bytes, size_t* v_bytes, size_t* scale_bytes, size_t* mean_bytes);
+
+/* Host only. Bytes of device scratch of rsa_fourbit_attn for queries `rows` in groups of `group` (0: no lists), whatever list_len. */
+int rsa_fourbit_workspace_bytes(const rsa_cache* cache, const rsa_rows* rows, int group, size_t* attn_ws_bytes);
+
+/* As rsa_cache_write. Tokens behind start[b] + count[b] keep their codes too; the mean of a block that is touched is that of its first
+ * tokens up to the last new one. */
+int rsa_fourbit_write(const rsa_cache* cache, const rsa_rows* rows, const void* K, const void* V, const int32_t* start,
+                      const int32_t* count, void* stream);
+
+/* As rsa_cache_read (exact: a code has 2 significant bits). */
+int rsa_fourbit_read(const rsa_cache* cache, const rsa_rows* rows, const int32_t* start, const int32_t* count, void* K,
+                     void* V, void* stream);
+
+/*
+ * As rsa_cache_attn, arguments and rules alike, but for the roundings: scores are those of the stored keys, summed in fp32; a weight times
+ * its token's scale is rounded to bf16, so that beside the rounding of O to bf16 and those of the fp32 steps an output is off by at
+ * most 2^-8 sum p |v| / sum p, however far apart the tokens' scales are. Values are to be below 2^100, and those below 2^-100 may
+ * vanish (2^8 of them times their number has to stay in the range of fp32, and their products with weights are taken in it). A NaN among the stored
+ * keys or values reaches the queries that see its token and no others.
+ */
+int rsa_fourbit_attn(const rsa_cache* cache, const rsa_rows* rows, const void* Q, const int32_t* kv_len,
+                     const int32_t* q_len, float scale, int flags, const int32_t* block_idx, const int32_t* kept, int group,
+                     int list_len, void* O, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Tables of a cache (of either kind) from request lengths, on the device: pages for new tokens are taken from a free list, pages of
+ * sequences that get shorter go back to it, and what the cache's calls need of the new lengths is written. A captured step
+ * advances its own tables with it.
+ */
+typedef struct rsa_pages {
+  int32_t batch;       /* sequences, 1 .. 65535 */
+  int32_t max_blocks;  /* entries of a row of the table, >= 1 */
+  int32_t block;       /* tokens of a page, >= 1 (the cache's) */
+  int64_t pages;       /* entries that the free list has room for: 1 .. 2^31 - 1 (the cache's pages) */
+  int32_t* table;      /* device, [batch][max_blocks]: the cache's table */
+  int32_t* free_pages; /* device, [pages]: pages that no sequence holds; the first free_count entries are valid, the last is taken first */
+} rsa_pages;
+
+/*
+ * Sequence b holds kv_len[b] tokens (less than 0 as 0, more than the table as the table) and is to get add[b] more (more than t counts
+ * as t), or to lose -add[b] (all of them, if it has fewer).
+ *   given back  where it gets shorter: its entries from ceil(new length / block) on become -1, and the pages that stood there go to the end of the
+ *               free list, in the order of the sequences and their entries; not those of the first shared[b] entries (a prefix that others
+ *               read too: device int32 [batch], NULL: none), and not entries that are no page. All of this comes before the first page is taken.
+ *   taken       entries from ceil(kv_len / block) to ceil(new length / block) get pages from the end of the free list, in the same order. A
+ *               sequence is served if its new length fits the table and the list holds what all sequences up to it ask for (those that do
+ *               not fit their table ask for none); one that needs no new page always is, if it fits. One that is not served stays as it is.
+ * Outputs, all device int32 unless said:
+ *   kv_new [batch]        the new lengths                   (may be kv_len)
+ *   free_left [1]         entries of the list that are left  (may be free_count)
+ *   start, count [batch]  the new tokens: position of the first, how many (0 where the sequence was not served or got shorter), as
+ *                         the write calls and rsa_rotary_apply take them; count is the q_len of the attention
+ *   positions [batch][t]  start + i for i < count, -1 behind     (NULL: not wanted)
+ *   slots [batch][t]      int64, page * block + offset of each new token, -1 behind and where the entry is no page (NULL: not wanted)
+ * table, free_pages, kv_new, free_left, start and count must not overlap each other or other arguments except as said (RSA_E_RANGE where two are
+ * the same). batch * t < 2^28. Allocates nothing and needs no workspace; calls on the same buffers must not overlap in time.
+ */
+int rsa_cache_assign(const rsa_pages* pages, int t, const int32_t* kv_len, const int32_t* add, const int32_t* shared,
+                     const int32_t* free_count, int32_t* kv_new, int32_t* free_left, int32_t* start, int32_t* count,
+                     int32_t* positions, int64_t* slots, void* stream);
+
+/*
+ * Rotary positions. Pair j < pairs of a head's channels (2 j and 2 j + 1 if interleaved, j and pairs + j if not; channels from 2 pairs on
+ * are left out) is turned by the angle position * freq[j]:
+ *   y1 = factor (x1 cos - x2 sin),  y2 = factor (x1 sin + x2 cos)
+ * in fp32, rounded once to bf16; the angle is reduced in fp64. With several axes (time, height, width) the first axis_pairs[0]
+ * pairs turn by the position along axis 0, and so on.
+ */
+typedef struct rsa_rotary {
+  int32_t head_dim;      /* a multiple of 8, <= 1024 */
+  int32_t pairs;         /* 1 .. head_dim / 2 */
+  int32_t interleaved;   /* 0 or not */
+  int32_t axes;          /* 1 .. 3 */
+  int32_t axis_pairs[3]; /* >= 0, those of the axes add up to pairs */
+  float factor;          /* >= 0; 0 selects 1 */
+  const double* freq;    /* device, [pairs]: radians a position */
+} rsa_rotary;
+
+/* scaling of rsa_rotary_frequencies */
+#define RSA_ROTARY_PLAIN 0  /* base^(-j / pairs) */
+#define RSA_ROTARY_LINEAR 1 /* the same over `stretch`: positions are interpolated */
+#define RSA_ROTARY_BASE 2   /* base * stretch^(pairs / (pairs - 1)) in place of base: the slowest pair is stretched, the fastest is not */
+#define RSA_ROTARY_PARTS 3  /* by parts: pairs with turns_many turns and more in old_len positions stay, those with turns_few and less are
+                               stretched, between them linearly; factor = 0.1 ln(stretch) + 1 */
+
+/* Host only: frequencies of one axis (freq [pairs], pairs <= 512, HOST) and the factor that goes with them. base > 1; stretch >= 1; old_len,
+ * turns_few < turns_many are read by RSA_ROTARY_PARTS alone. */
+int rsa_rotary_frequencies(int pairs, double base, int scaling, double stretch, double old_len, double turns_few,
+                           double turns_many, double* freq, float* factor);
+
+#define RSA_ROTARY_INVERSE 1 /* turn back: the gradient of the call without it, from that of its outputs */
+
+/*
+ * Rows of Q and, in the same launch, of K (rows_k NULL: Q alone; other heads and strides, the same t): row i < count[b] of sequence b (NULL: all; rows
+ * behind are left as they were) stands at positions[axis][b][i] (device int32 [axes][batch][t], any sign), or, where that is NULL and there
+ * is one axis, at start[b] + i (start NULL: i). Qr and Kr have the strides of Q and K and may be Q and K; otherwise inputs and outputs must not
+ * overlap. Channels that do not turn are copied. batch * heads * t < 2^28. Needs no workspace.
+ */
+int rsa_rotary_apply(const rsa_rotary* rotary, int batch, const rsa_rows* rows_q, const void* Q, void* Qr, const rsa_rows* rows_k,
+                     const void* K, void* Kr, const int32_t* positions, const int32_t* start, const int32_t* count, int flags,
+                     void* stream);
+
 /* Static string for a return code. */
 const char* rsa_status_string(int status);
 

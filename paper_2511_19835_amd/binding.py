@@ -24,11 +24,15 @@ RSA_MAX_BLOCKS = 4096
 RSA_STATIC_SCRATCH_BYTES = 16 << 20
 RSA_CACHE_CAUSAL = 1
 RSA_CACHE_MAX_SELECT = 16384
+RSA_ROTARY_PLAIN, RSA_ROTARY_LINEAR, RSA_ROTARY_BASE, RSA_ROTARY_PARTS = 0, 1, 2, 3
+RSA_ROTARY_INVERSE = 1
 
 EXPORTS = (
     "rsa_block_counts", "rsa_workspace_bytes", "rsa_pool", "rsa_pool_values", "rsa_implicit_attention", "rsa_adjacency_mask", "rsa_reorder_tokens", "rsa_select_blocks",
     "rsa_sparse_attn_rectified", "rsa_sparse_attn_rectified_static", "rsa_status_string",
     "rsa_cache_bytes", "rsa_cache_workspace_bytes", "rsa_cache_write", "rsa_cache_read", "rsa_cache_select", "rsa_cache_attn",
+    "rsa_fourbit_bytes", "rsa_fourbit_workspace_bytes", "rsa_fourbit_write", "rsa_fourbit_read", "rsa_fourbit_attn",
+    "rsa_cache_assign", "rsa_rotary_frequencies", "rsa_rotary_apply",
 )
 
 
@@ -62,6 +66,20 @@ class rsa_rows(ctypes.Structure):
     _fields_ = [
         ("heads", ctypes.c_int32), ("t", ctypes.c_int32),
         ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64), ("stride_t", ctypes.c_int64),
+    ]
+
+
+class rsa_pages(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("max_blocks", ctypes.c_int32), ("block", ctypes.c_int32), ("pages", ctypes.c_int64),
+        ("table", ctypes.c_void_p), ("free_pages", ctypes.c_void_p),
+    ]
+
+
+class rsa_rotary(ctypes.Structure):
+    _fields_ = [
+        ("head_dim", ctypes.c_int32), ("pairs", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("axes", ctypes.c_int32),
+        ("axis_pairs", ctypes.c_int32 * 3), ("factor", ctypes.c_float), ("freq", ctypes.c_void_p),
     ]
 
 
@@ -112,6 +130,17 @@ def _lib() -> ctypes.CDLL:
         lib.rsa_cache_select.restype = i
         lib.rsa_cache_attn.argtypes = [cap, rwp] + [vp] * 3 + [ctypes.c_float, i, vp, vp, i, i, vp, vp, vp, ctypes.c_size_t, vp]
         lib.rsa_cache_attn.restype = i
+        lib.rsa_fourbit_bytes.argtypes = [cap, szp, szp, szp, szp]
+        lib.rsa_fourbit_workspace_bytes.argtypes = [cap, rwp, i, szp]
+        lib.rsa_fourbit_write.argtypes = lib.rsa_cache_write.argtypes
+        lib.rsa_fourbit_read.argtypes = lib.rsa_cache_read.argtypes
+        lib.rsa_fourbit_attn.argtypes = lib.rsa_cache_attn.argtypes
+        lib.rsa_cache_assign.argtypes = [ctypes.POINTER(rsa_pages), i] + [vp] * 11
+        dbl = ctypes.c_double
+        lib.rsa_rotary_frequencies.argtypes = [i, dbl, i, dbl, dbl, dbl, dbl, ctypes.POINTER(dbl), ctypes.POINTER(ctypes.c_float)]
+        lib.rsa_rotary_apply.argtypes = [ctypes.POINTER(rsa_rotary), i, rwp, vp, vp, rwp, vp, vp, vp, vp, vp, i, vp]
+        for name in EXPORTS[17:]:
+            getattr(lib, name).restype = i
         lib.rsa_status_string.argtypes = [ctypes.c_int]
         lib.rsa_status_string.restype = ctypes.c_char_p
         _LIB = lib
@@ -272,16 +301,17 @@ def rectified_sparse_attention(Q, K, V, O, buf: LayerBuffers, sparsity: float, p
     return O
 
 
-# ---- the 8-bit key/value cache ---------------------------------------------------------
+# ---- the key/value cache in 8 and in 4 bits ----------------------------------------------
 @dataclass
 class KVCache:
-    """Caller-owned device buffers of an 8-bit key/value cache and the record of them that the calls take."""
+    """Caller-owned device buffers of a key/value cache and the record of them that the calls take."""
     desc: rsa_cache
-    k_codes: torch.Tensor      # uint8 [pages, heads_kv, block * head_dim], opaque
-    v_codes: torch.Tensor
+    k_codes: torch.Tensor      # uint8 [pages, heads_kv, block * head_dim], opaque (4 bits: block * (head_dim / 2 + head_dim / 32))
+    v_codes: torch.Tensor      # the same (4 bits: block * (head_dim / 2 + 2))
     scales: torch.Tensor       # fp32  [pages, heads_kv, 4]
     k_mean: torch.Tensor       # int8  [pages, heads_kv, head_dim]
     table: torch.Tensor        # int32 [batch, max_blocks]: page of each block of a sequence, -1 where there is none
+    bits: int = 8
 
     def __post_init__(self):
         # what every call needs of the record, at hand
@@ -306,9 +336,31 @@ def cache_of(k_codes, v_codes, scales, k_mean, table, block: int) -> KVCache:
     return KVCache(desc, k_codes, v_codes, scales, k_mean, table)
 
 
-def allocate_cache(batch: int, heads_kv: int, head_dim: int, block: int, pages: int, max_blocks: int, device="cuda:0") -> KVCache:
-    """An empty cache: no page is in the table yet."""
+def fourbit_of(k_codes, v_codes, scales, k_mean, table, block: int) -> KVCache:
+    """Record of a cache in 4 bits whose buffers exist."""
+    pages, heads_kv, head_dim = k_mean.shape
+    want = ((k_codes, torch.uint8, (pages, heads_kv, block * (head_dim // 2 + head_dim // 32))),
+            (v_codes, torch.uint8, (pages, heads_kv, block * (head_dim // 2 + 2))), (scales, torch.float32, (pages, heads_kv, 4)),
+            (k_mean, torch.int8, (pages, heads_kv, head_dim)), (table, torch.int32, (table.shape[0], table.shape[-1])))
+    for x, dtype, shape in want:
+        if x.dtype != dtype or tuple(x.shape) != shape or not x.is_contiguous() or x.device != k_codes.device:
+            raise ValueError(f"expect a contiguous {dtype} tensor of shape {shape} on {k_codes.device}, got {x.dtype} {tuple(x.shape)} on {x.device}")
+    desc = rsa_cache(table.shape[0], heads_kv, head_dim, block, table.shape[1], pages, _ptr(k_codes), _ptr(v_codes), _ptr(scales),
+                     _ptr(k_mean), _ptr(table))
+    return KVCache(desc, k_codes, v_codes, scales, k_mean, table, 4)
+
+
+def allocate_cache(batch: int, heads_kv: int, head_dim: int, block: int, pages: int, max_blocks: int, device="cuda:0", bits: int = 8) -> KVCache:
+    """An empty cache of 8 or 4 bits: no page is in the table yet."""
+    if bits not in (4, 8):
+        raise ValueError(f"a cache holds 8 or 4 bits, not {bits}")
     probe = rsa_cache(batch, heads_kv, head_dim, block, max_blocks, pages)
+    if bits == 4:
+        sizes = rsa_fourbit_bytes(probe)
+        k, v = (torch.empty(n, dtype=torch.uint8, device=device).view(pages, heads_kv, -1) for n in sizes[:2])
+        return fourbit_of(k, v, torch.empty(pages, heads_kv, 4, dtype=torch.float32, device=device),
+                          torch.empty(pages, heads_kv, head_dim, dtype=torch.int8, device=device),
+                          torch.full((batch, max_blocks), -1, dtype=torch.int32, device=device), block)
     code, scale, mean = rsa_cache_bytes(probe)
     u8 = dict(dtype=torch.uint8, device=device)
     return cache_of(torch.empty(code, **u8).view(pages, heads_kv, block * head_dim),
@@ -352,17 +404,24 @@ def _lists(cache: KVCache, rows: rsa_rows, group: int, block_idx: torch.Tensor, 
         raise ValueError(f"expect contiguous int32 lists {shape} + [list_len] and counts {shape} on the cache's device")
 
 
-def _call(cache: KVCache, stream, where: str, fn, *args) -> None:
-    """One call on the cache's device: on `stream`, or on that device's current stream."""
-    dev = cache.device.index
+def _launch(device: torch.device, stream, where: str, fn, *args) -> None:
+    """One call on a device: on `stream`, or on that device's current stream."""
+    dev = device.index
     raw = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
     if torch.cuda.current_device() == dev:
-        status = fn(cache.ref, *args, raw)
+        status = fn(*args, raw)
     else:
         with torch.cuda.device(dev):
-            status = fn(cache.ref, *args, raw)
+            status = fn(*args, raw)
     if status != 0:
         raise RsaError(status, where)
+
+
+def _call(cache: KVCache, stream, where: str, fn, *args, bits: int = 0) -> None:
+    """One call on the cache's device; `bits`: only caches of so many are taken."""
+    if bits and cache.bits != bits:
+        raise ValueError(f"{where} takes a cache of {bits} bits, not of {cache.bits}")
+    _launch(cache.device, stream, where, fn, cache.ref, *args)
 
 
 def _scratch(cache: KVCache, ws: Optional[torch.Tensor]):
@@ -388,12 +447,12 @@ def rsa_cache_workspace_bytes(cache: KVCache, rows: rsa_rows, group: int = 0):
 
 def rsa_cache_write(cache: KVCache, rows, K, V, start, count=None, stream=None):
     _call(cache, stream, "rsa_cache_write", _lib().rsa_cache_write, rows.ref, _row_tensor(cache, rows, K), _row_tensor(cache, rows, V),
-          _lengths(cache, start), _lengths(cache, count))
+          _lengths(cache, start), _lengths(cache, count), bits=8)
 
 
 def rsa_cache_read(cache: KVCache, rows, start, count, K, V, stream=None):
     _call(cache, stream, "rsa_cache_read", _lib().rsa_cache_read, rows.ref, _lengths(cache, start), _lengths(cache, count),
-          _row_tensor(cache, rows, K), _row_tensor(cache, rows, V))
+          _row_tensor(cache, rows, K), _row_tensor(cache, rows, V), bits=8)
 
 
 def rsa_cache_select(cache: KVCache, rows, Q, kv_len, q_len, group, keep, first, last, flags, block_idx, kept, ws=None, stream=None):
@@ -402,14 +461,44 @@ def rsa_cache_select(cache: KVCache, rows, Q, kv_len, q_len, group, keep, first,
           _lengths(cache, q_len), group, keep, first, last, flags, block_idx.data_ptr(), kept.data_ptr(), block_idx.shape[3], *_scratch(cache, ws))
 
 
-def rsa_cache_attn(cache: KVCache, rows, Q, kv_len, q_len, scale, flags, block_idx, kept, group, O, lse=None, ws=None, stream=None):
+def _attn_call(cache: KVCache, where: str, fn, bits: int, rows, Q, kv_len, q_len, scale, flags, block_idx, kept, group, O, lse, ws, stream):
     if lse is not None and (lse.dtype is not torch.float32 or lse.shape != rows.shape[:3] or not lse.is_contiguous() or lse.device != cache.device):
         raise ValueError("expect a contiguous fp32 lse [batch, heads, t] on the cache's device")
     if block_idx is not None and kept is not None:
         _lists(cache, rows, group, block_idx, kept)
-    _call(cache, stream, "rsa_cache_attn", _lib().rsa_cache_attn, rows.ref, _row_tensor(cache, rows, Q), _lengths(cache, kv_len),
+    _call(cache, stream, where, fn, rows.ref, _row_tensor(cache, rows, Q), _lengths(cache, kv_len),
           _lengths(cache, q_len), scale, flags, _ptr(block_idx), _ptr(kept), group, block_idx.shape[3] if block_idx is not None else 0,
-          _row_tensor(cache, rows, O), _ptr(lse), *_scratch(cache, ws))
+          _row_tensor(cache, rows, O), _ptr(lse), *_scratch(cache, ws), bits=bits)
+
+
+def rsa_cache_attn(cache: KVCache, rows, Q, kv_len, q_len, scale, flags, block_idx, kept, group, O, lse=None, ws=None, stream=None):
+    _attn_call(cache, "rsa_cache_attn", _lib().rsa_cache_attn, 8, rows, Q, kv_len, q_len, scale, flags, block_idx, kept, group, O, lse, ws, stream)
+
+
+def rsa_fourbit_bytes(desc: rsa_cache):
+    out = [ctypes.c_size_t() for _ in range(4)]
+    _check(_lib().rsa_fourbit_bytes(ctypes.byref(desc), *(ctypes.byref(x) for x in out)), "rsa_fourbit_bytes")
+    return tuple(x.value for x in out)
+
+
+def rsa_fourbit_workspace_bytes(cache: KVCache, rows: rsa_rows, group: int = 0):
+    a = ctypes.c_size_t()
+    _check(_lib().rsa_fourbit_workspace_bytes(cache.ref, rows.ref, int(group), ctypes.byref(a)), "rsa_fourbit_workspace_bytes")
+    return a.value
+
+
+def rsa_fourbit_write(cache: KVCache, rows, K, V, start, count=None, stream=None):
+    _call(cache, stream, "rsa_fourbit_write", _lib().rsa_fourbit_write, rows.ref, _row_tensor(cache, rows, K), _row_tensor(cache, rows, V),
+          _lengths(cache, start), _lengths(cache, count), bits=4)
+
+
+def rsa_fourbit_read(cache: KVCache, rows, start, count, K, V, stream=None):
+    _call(cache, stream, "rsa_fourbit_read", _lib().rsa_fourbit_read, rows.ref, _lengths(cache, start), _lengths(cache, count),
+          _row_tensor(cache, rows, K), _row_tensor(cache, rows, V), bits=4)
+
+
+def rsa_fourbit_attn(cache: KVCache, rows, Q, kv_len, q_len, scale, flags, block_idx, kept, group, O, lse=None, ws=None, stream=None):
+    _attn_call(cache, "rsa_fourbit_attn", _lib().rsa_fourbit_attn, 4, rows, Q, kv_len, q_len, scale, flags, block_idx, kept, group, O, lse, ws, stream)
 
 
 def cached_sparse_attention(cache: KVCache, K, V, Q, O, kv_len, q_len, group: int, keep: int, block_idx, kept, first: int = 1,
@@ -424,7 +513,119 @@ def cached_sparse_attention(cache: KVCache, K, V, Q, O, kv_len, q_len, group: in
         with torch.cuda.stream(stream):                # (None: the current stream)
             start = kv_len - (q_len.clamp(max=Q.shape[2]) if q_len is not None else Q.shape[2])
     rows_kv, rows = make_rows(K), make_rows(Q)
-    rsa_cache_write(cache, rows_kv, K, V, start, q_len, stream)
+    write, attn = (rsa_fourbit_write, rsa_fourbit_attn) if cache.bits == 4 else (rsa_cache_write, rsa_cache_attn)
+    write(cache, rows_kv, K, V, start, q_len, stream)
     rsa_cache_select(cache, rows, Q, kv_len, q_len, group, keep, first, last, flags, block_idx, kept, ws, stream)
-    rsa_cache_attn(cache, rows, Q, kv_len, q_len, 0.0, flags, block_idx, kept, group, O, lse, ws, stream)
+    attn(cache, rows, Q, kv_len, q_len, 0.0, flags, block_idx, kept, group, O, lse, ws, stream)
+    return O
+
+
+# ---- pages, positions and a step of many requests ----------------------------------------
+@dataclass
+class Pages:
+    """A cache's table and the list of pages that no sequence holds, and the record of them."""
+    desc: rsa_pages
+    table: torch.Tensor        # int32 [batch, max_blocks]
+    free_pages: torch.Tensor   # int32 [pages]
+
+    def __post_init__(self):
+        self.ref, self.device, self.batch = ctypes.byref(self.desc), self.table.device, self.desc.batch
+
+
+def pages_of(table: torch.Tensor, free_pages: torch.Tensor, block: int) -> Pages:
+    """Record of a table and a free list; free_pages has room for every page of the cache."""
+    for x, dims in ((table, 2), (free_pages, 1)):
+        if x.dtype is not torch.int32 or x.dim() != dims or not x.is_contiguous() or x.device != table.device:
+            raise ValueError(f"expect a contiguous int32 tensor of {dims} dimensions on {table.device}, got {x.dtype} {tuple(x.shape)} on {x.device}")
+    return Pages(rsa_pages(table.shape[0], table.shape[1], block, free_pages.shape[0], _ptr(table), _ptr(free_pages)), table, free_pages)
+
+
+def _ints(x: Optional[torch.Tensor], shape, device, dtype=torch.int32) -> Optional[int]:
+    if x is None:
+        return None
+    if x.dtype is not dtype or tuple(x.shape) != tuple(shape) or not x.is_contiguous() or x.device != device:
+        raise ValueError(f"expect a contiguous {dtype} tensor {tuple(shape)} on {device}, got {x.dtype} {tuple(x.shape)} on {x.device}")
+    return x.data_ptr()
+
+
+def rsa_cache_assign(pages: Pages, t, kv_len, add, free_count, kv_new, free_left, start, count, positions=None, slots=None, shared=None, stream=None):
+    b, dev = (pages.batch,), pages.device
+    _launch(dev, stream, "rsa_cache_assign", _lib().rsa_cache_assign, pages.ref, t, _ints(kv_len, b, dev), _ints(add, b, dev), _ints(shared, b, dev),
+            _ints(free_count, (1,), dev), _ints(kv_new, b, dev), _ints(free_left, (1,), dev), _ints(start, b, dev), _ints(count, b, dev),
+            _ints(positions, (pages.batch, t), dev), _ints(slots, (pages.batch, t), dev, torch.int64))
+
+
+@dataclass
+class Rotary:
+    """Frequencies of rotary positions on the device and the record of them."""
+    desc: rsa_rotary
+    freq: torch.Tensor         # fp64 [pairs], radians a position
+
+    def __post_init__(self):
+        self.device, self.axes, self.refs = self.freq.device, self.desc.axes, {}
+
+    def ref(self, head_dim: int):
+        """The record for heads of `head_dim` channels."""
+        if head_dim not in self.refs:
+            d = rsa_rotary.from_buffer_copy(self.desc)
+            d.head_dim = head_dim
+            self.refs[head_dim] = ctypes.byref(d)
+        return self.refs[head_dim]
+
+
+def make_rotary(freq: torch.Tensor, pairing: str = "half", axis_pairs=None, factor: float = 1.0) -> Rotary:
+    """Record of fp64 frequencies on the device, one for each pair of channels that turns. pairing: "half" (channels j and pairs + j) or
+    "interleaved" (2 j and 2 j + 1); axis_pairs: how many of the pairs turn along each of up to three axes."""
+    if pairing not in ("half", "interleaved"):
+        raise ValueError(f"pairs are 'half' or 'interleaved', not {pairing!r}")
+    if freq.dtype is not torch.float64 or freq.dim() != 1 or not freq.is_contiguous():
+        raise ValueError(f"expect contiguous fp64 frequencies of one dimension, got {freq.dtype} {tuple(freq.shape)}")
+    axis = list(axis_pairs) if axis_pairs is not None else [freq.shape[0]]
+    if not 1 <= len(axis) <= 3 or sum(axis) != freq.shape[0] or min(axis) < 0:
+        raise ValueError(f"pairs of up to three axes add up to {freq.shape[0]}: got {axis}")
+    return Rotary(rsa_rotary(0, freq.shape[0], int(pairing == "interleaved"), len(axis), (ctypes.c_int32 * 3)(*axis), float(factor), _ptr(freq)), freq)
+
+
+def rsa_rotary_frequencies(pairs: int, base: float = 10000.0, scaling: int = RSA_ROTARY_PLAIN, stretch: float = 1.0, old_len: float = 0.0,
+                           turns_few: float = 1.0, turns_many: float = 32.0):
+    """(frequencies as a list, factor) of one axis."""
+    freq, factor = (ctypes.c_double * max(1, pairs))(), ctypes.c_float()
+    _check(_lib().rsa_rotary_frequencies(pairs, base, scaling, stretch, old_len, turns_few, turns_many, freq, ctypes.byref(factor)), "rsa_rotary_frequencies")
+    return list(freq), factor.value
+
+
+def _turned(rows: rsa_rows, batch: int, device, *tensors):
+    for x in tensors:
+        if (x.dtype is not torch.bfloat16 or x.shape != rows.shape or x.shape[0] != batch or x.device != device
+                or x.stride() != rows.strides and any(n > 1 and p != q for n, p, q in zip(x.shape, x.stride(), rows.strides))):
+            raise ValueError(f"tensor {x.dtype} {tuple(x.shape)} strides {x.stride()} on {x.device} is not what the row record says")
+    return (x.data_ptr() for x in tensors)
+
+
+def rsa_rotary_apply(rotary: Rotary, rows_q, Q, Qr, rows_k=None, K=None, Kr=None, positions=None, start=None, count=None, flags=0, stream=None):
+    b, t, d, dev = Q.shape[0], Q.shape[2], Q.shape[3], rotary.device
+    q, qr = _turned(rows_q, b, dev, Q, Qr)
+    k, kr = _turned(rows_k, b, dev, K, Kr) if rows_k is not None else (None, None)
+    if rows_k is not None and K.shape[3] != d:
+        raise ValueError(f"queries and keys have heads of the same size: got {d} and {K.shape[3]}")
+    if positions is not None and positions.dim() == 2:
+        positions = positions[None]
+    _launch(dev, stream, "rsa_rotary_apply", _lib().rsa_rotary_apply, rotary.ref(d), b, rows_q.ref, q, qr, rows_k.ref if rows_k is not None else None, k, kr,
+            _ints(positions, (rotary.axes, b, t), dev), _ints(start, (b,), dev), _ints(count, (b,), dev), flags)
+
+
+def serve_step(cache: KVCache, pages: Pages, rotary: Rotary, Q, K, V, O, kv_len, add, free_count, start, count, positions=None, slots=None, shared=None,
+               lse=None, ws=None, stream=None):
+    """One step of a batch of requests on one stream, with no host sync, so that it can be captured and replayed: sequence b brings add[b] new
+    tokens (rows 0 .. add[b] - 1 of Q, K and V; less than 0: it is cut). Pages for them (rsa_cache_assign; kv_len and free_count move on in place,
+    start and count say what was served), Q and K turned in place by their positions, keys and values into the cache, and the causal
+    attention of the new queries over their sequences. Rows of sequences that were not served are left as they were."""
+    if pages.table.data_ptr() != cache.table.data_ptr():
+        raise ValueError("the pages are not those of the cache's table")
+    rows, rows_kv = make_rows(Q), make_rows(K)
+    write, attn = (rsa_fourbit_write, rsa_fourbit_attn) if cache.bits == 4 else (rsa_cache_write, rsa_cache_attn)
+    rsa_cache_assign(pages, Q.shape[2], kv_len, add, free_count, kv_len, free_count, start, count, positions, slots, shared, stream)
+    rsa_rotary_apply(rotary, rows, Q, Q, rows_kv, K, K, None, start, count, 0, stream)
+    write(cache, rows_kv, K, V, start, count, stream)
+    attn(cache, rows, Q, kv_len, count, 0.0, RSA_CACHE_CAUSAL, None, None, 0, O, lse, ws, stream)
     return O

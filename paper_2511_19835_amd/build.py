@@ -31,6 +31,11 @@ SOURCES = [
     "cache_page_kernels.hip",
     "cache_select_kernels.hip",
     "cache_attn_kernels.hip",
+    "serve_api.hip",
+    "assign_kernels.hip",
+    "rotary_kernels.hip",
+    "fourbit_page_kernels.hip",
+    "fourbit_attn_kernels.hip",
 ]
 
 # Packed-fp32 VALU forms (v_pk_*_f32) are switched off for every device translation unit.

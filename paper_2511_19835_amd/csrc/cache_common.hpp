@@ -49,6 +49,27 @@ __device__ __forceinline__ int v_code_offset(int t, int ch) {
   return ((((t >> 6) * (D / 16) + (ch >> 4)) * 4 + ((t & 15) >> 2)) * 16 + (ch & 15)) * 16 + ((t & 63) >> 4) * 4 + (t & 3);
 }
 
+struct BlockSpan {
+  int64_t first;   // token (in the new rows) of the block's slot 0; negative where older tokens precede
+  int lo, hi;      // slots that get a new token
+  int page;        // -1: none
+};
+// The jth block that tokens [start, start + count) of sequence b touch; false: there is none.
+template <int BLK>
+__device__ __forceinline__ bool touched_block(const CacheDims& c, int t, const int32_t* start, const int32_t* count, int b, int j, BlockSpan* out) {
+  const int64_t s = start[b];
+  int64_t n = count ? count[b] : t;
+  if (n > t) n = t;
+  if (s < 0 || n <= 0) return false;
+  const int64_t blk = s / BLK + j, at = blk * BLK;
+  if (at >= s + n || blk >= c.max_blocks) return false;
+  out->page = cache_page(c, b, (int)blk);
+  out->first = at - s;
+  out->lo = s > at ? (int)(s - at) : 0;
+  out->hi = s + n - at < BLK ? (int)(s + n - at) : BLK;
+  return true;
+}
+
 // Workgroups go round the eight XCDs in turn; numbered like this, those of an XCD take numbers that follow one another, so
 // that what neighbours share (a sequence's heads the lines of scales, a head's groups means and codes) is in one L2.
 __device__ __forceinline__ int xcd_run(int id, int all) {

@@ -54,27 +54,6 @@ __device__ __forceinline__ bool code_is_nan(uint32_t byte) { return (byte & 127u
 // The value of a code in units of 2^-9; NaN counts as 0. At most 448 * 512 < 2^18: sums over a block are exact in 32 bits.
 __device__ __forceinline__ int code_units(float x) { return x == x ? (int)(x * 512.f) : 0; }
 
-struct BlockSpan {
-  int64_t first;   // token (in the new rows) of the block's slot 0; negative where older tokens precede
-  int lo, hi;      // slots that get a new token
-  int page;        // -1: none
-};
-// The jth block that tokens [start, start + count) of sequence b touch; false: there is none.
-template <int BLK>
-__device__ __forceinline__ bool touched_block(const CacheDims& c, int t, const int32_t* start, const int32_t* count, int b, int j, BlockSpan* out) {
-  const int64_t s = start[b];
-  int64_t n = count ? count[b] : t;
-  if (n > t) n = t;
-  if (s < 0 || n <= 0) return false;
-  const int64_t blk = s / BLK + j, at = blk * BLK;
-  if (at >= s + n || blk >= c.max_blocks) return false;
-  out->page = cache_page(c, b, (int)blk);
-  out->first = at - s;
-  out->lo = s > at ? (int)(s - at) : 0;
-  out->hi = s + n - at < BLK ? (int)(s + n - at) : BLK;
-  return true;
-}
-
 template <int D, int BLK>
 __global__ __launch_bounds__(256) void cache_write_kernel(CacheDims c, RowDims r, CacheWriteArgs a, int blocks) {
   constexpr int CPR = D / 8;                       // chunks of eight channels

@@ -1,0 +1,602 @@
+// Attention of new queries over the 4-bit key/value cache, over all blocks or over listed ones.
+//
+// Tiles, splits and joins are those of the 8-bit cache (cache_attn_common.hpp): a tile is 16 QT rows of one (sequence, key/value
+// head), and each wave computes, with 16x16x32 products of bf16,
+//     S^T = K Q^T      (M = key, N = query, k = channel)
+//     O^T += V^T P^T   (M = channel, N = query, k = key)
+// with the softmax between them lane-local. A code times its key's scale is exact in bf16, so the scores are those of the stored
+// keys, summed in fp32; a value's code is widened alone, and its token's scale goes into P.
+//
+// P times that scale is rounded to bf16: half a step is 2^-8 of it, whatever the scales of the tokens are to each other, so no
+// running scale of the outputs is needed. The sum of the weights is taken before that rounding, in fp32. The running reference m of
+// a row follows its maximum lazily (only when a score passes it by more than 8 in log2), so p <= 2^8.
+#include "fourbit_common.hpp"
+
+#include "cache_attn_common.hpp"
+
+namespace rsa {
+namespace {
+
+// Eight codes as bf16, times `scale` (a power of two: exact).
+__device__ __forceinline__ bf16x8 widen8(uint32_t w, float scale) {
+  bf16x8 o;
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
+  o[0] = a[0]; o[1] = a[1]; o[2] = b[0]; o[3] = b[1];
+  o[4] = c[0]; o[5] = c[1]; o[6] = d[0]; o[7] = d[1];
+  return o;
+}
+// Byte t of a lane's exponents as a scale: 2^(byte - 127), NaN for 255 (whose bits are infinity: times 0 that is NaN).
+__device__ __forceinline__ float key_scale(uint32_t w, int t) {
+  const float s = __builtin_bit_cast(float, (w >> (8 * t) & 255u) << 23);
+  return __builtin_fmaf(s, 0.f, s);
+}
+// Scales of keys 16 t + 4 g + i of 64 from a lane's 32 bytes.
+__device__ __forceinline__ void value_scales(const uint4 (&w)[2], float (&s)[4][4]) {
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const uint32_t lo = t % 2 ? w[t / 2].z : w[t / 2].x, hi = t % 2 ? w[t / 2].w : w[t / 2].y;
+    s[t][0] = bf16_bits_to_float(lo & 0xffffu);
+    s[t][1] = __builtin_bit_cast(float, lo & 0xffff0000u);
+    s[t][2] = bf16_bits_to_float(hi & 0xffffu);
+    s[t][3] = __builtin_bit_cast(float, hi & 0xffff0000u);
+  }
+}
+
+// What a lane loads for a step of 64 keys.
+template <int D>
+struct Step64 {
+  uint32_t k[4][D / 32];       // codes of 16 keys: D / 4 channels of one key
+  uint32_t ks;                 // exponents of this lane's run of channels, key n of each tile
+  uint4 v[D / 32];
+  uint4 vs[2];
+};
+
+template <int D, int BLK, int QT>
+__global__ __launch_bounds__(256, 2) void fourbit_attn_kernel(CacheDims c, RowDims r, CacheAttnArgs a, TileGrid tg) {
+  constexpr int KM = D / 32, VC = D / 16;          // products of a tile of 16 keys / channel tiles
+  constexpr int SPB = BLK / 64;                    // steps of 64 keys in a block
+  constexpr int KR = fourbit_k_record(D), VR = fourbit_v_record(D);
+  constexpr int PITCH = D + 4;                     // floats of a row in the joining buffer
+  __shared__ __align__(16) float join[4][16][PITCH];
+  __shared__ float join_m[4][16], join_l[4][16];
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const int g = lane / 16, n = lane % 16;
+  const int split = blockIdx.x % tg.splits;
+  const int64_t id = blockIdx.x / tg.splits;
+  const Tile t = tile_of(c, r, a, tg, id);
+  const int G = r.heads / c.heads_kv;
+
+  // queries of this lane's columns, as operands (channels (D / 4) g + 8 m ..), and how many keys each sees
+  bf16x8 q[QT][KM];
+  int seen[QT];
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    const int row = t.row0 + 16 * x + n, tok = t.t0 + row / G;
+    const bool is = row < t.rows && tok < t.ql;
+    seen[x] = !is ? 0 : visible_keys(c, a, t, tok);
+    const uint16_t* src = a.Q + (int64_t)t.b * r.sb + (int64_t)(t.hk * G + row % G) * r.sh + (int64_t)tok * r.st + g * (D / 4);
+#pragma unroll
+    for (int k = 0; k < KM; ++k) {
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (is) v = *reinterpret_cast<const uint4*>(src + k * 8);
+      q[x][k] = __builtin_bit_cast(bf16x8, v);
+    }
+  }
+  floatx4 o[QT][VC];
+  float m[QT], l[QT], lazy = kLazy;
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    m[x] = kNoReference;
+    l[x] = 0.f;
+#pragma unroll
+    for (int v = 0; v < VC; ++v) o[x][v] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const int u0 = (int)((int64_t)t.units * split / tg.splits), u1 = (int)((int64_t)t.units * (split + 1) / tg.splits);
+  const int steps = (u1 - u0) * SPB;
+  // this wave's steps are wave, wave + 4, ...; lane i looks up the i-th of the next 64
+  for (int base = wave; base < steps; base += 256) {
+    int my_blk = -1, my_page = -1;
+    const int my_step = base + lane * 4;
+    if (my_step < steps) {
+      my_blk = u0 + my_step / SPB;
+      if (a.block_idx) my_blk = a.block_idx[(int64_t)t.lrow * a.list_len + my_blk];
+      if (my_blk < t.blocks) my_page = cache_page(c, t.b, my_blk);
+    }
+    unsigned long long todo = __ballot(my_page >= 0);
+    Step64<D> at[2];
+    auto load = [&](Step64<D>& z, int i) __attribute__((always_inline)) {
+      const int64_t rec = ((int64_t)__builtin_amdgcn_readlane(my_page, i) * c.heads_kv + t.hk) * SPB + (base + i * 4) % SPB;
+      const uint8_t *pk = c.k + rec * KR, *pv = c.v + rec * VR;
+      z.ks = *reinterpret_cast<const uint32_t*>(pk + 32 * D + (D == 128 ? lane : (g / 2) * 16 + n) * 4);
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        if constexpr (D == 128) {
+          const uint4 w = *reinterpret_cast<const uint4*>(pk + y * 1024 + lane * 16);
+          z.k[y][0] = w.x; z.k[y][1] = w.y; z.k[y][2] = w.z; z.k[y][3] = w.w;
+        } else {
+          const uint2 w = *reinterpret_cast<const uint2*>(pk + y * 512 + ((g / 2) * 16 + n) * 16 + (g % 2) * 8);
+          z.k[y][0] = w.x; z.k[y][1] = w.y;
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) z.vs[x] = *reinterpret_cast<const uint4*>(pv + 32 * D + g * 32 + x * 16);
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x) z.v[x] = *reinterpret_cast<const uint4*>(pv + x * 1024 + lane * 16);
+    };
+    auto compute = [&](const Step64<D>& z, int i) __attribute__((always_inline)) {
+      const int key0 = __builtin_amdgcn_readlane(my_blk, i) * BLK + ((base + i * 4) % SPB) * 64;
+      floatx4 s[QT][4];
+#pragma unroll
+      for (int x = 0; x < QT; ++x)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) s[x][y] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const float sc = key_scale(z.ks, y);
+#pragma unroll
+        for (int k = 0; k < KM; ++k) {
+          const bf16x8 op = widen8(z.k[y][k], sc);
+#pragma unroll
+          for (int x = 0; x < QT; ++x) s[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op, q[x][k], s[x][y], 0, 0, 0);
+        }
+      }
+      // scores; keys that a row does not see leave its softmax
+      const bool partly = key0 + 64 > t.lo_seen;
+      bool over = false;
+#pragma unroll
+      for (int x = 0; x < QT; ++x) {
+        const int left = seen[x] - key0;             // of the 64
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float w = s[x][y][e] * a.scale_log2e;
+            if (partly) w = 16 * y + 4 * g + e < left ? w : -INFINITY;
+            s[x][y][e] = w;
+            over |= w > m[x] + lazy;
+          }
+      }
+      if (__any(over)) {
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          float mx = kNoReference;
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[x][y][e]);
+          mx = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, mx), MaxF32()), MaxF32()));
+          if (mx > m[x] + lazy) {                  // the same in the four lanes of a column
+            mx = floorf(mx);                       // (whole, so that what is taken from it and what it rescales stays exact)
+            const float down = exp2f(m[x] - mx);
+            m[x] = mx;
+            l[x] *= down;
+#pragma unroll
+            for (int v = 0; v < VC; ++v) o[x][v] *= down;
+          }
+        }
+        if (far_from_zero<QT>(m)) lazy = 0.f;
+      }
+      float vs[4][4];
+      value_scales(z.vs, vs);
+      bf16x8 p[QT][2];
+#pragma unroll
+      for (int x = 0; x < QT; ++x) {
+        float sum = 0.f;
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) {
+            floatx2 w;
+#pragma unroll
+            for (int f = 0; f < 2; ++f) {
+              const float one = __builtin_amdgcn_exp2f(s[x][y][e + f] - m[x]);
+              sum += one;
+              w[f] = one * vs[y][e + f];
+              // a value that is NaN under a key that a row does not see must not reach it through 0 * NaN
+              if (partly) w[f] = s[x][y][e + f] == -INFINITY ? 0.f : w[f];
+            }
+            const bf16x2 b = __builtin_convertvector(w, bf16x2);
+            p[x][y / 2][y % 2 * 4 + e] = b[0];
+            p[x][y / 2][y % 2 * 4 + e + 1] = b[1];
+          }
+        l[x] += sum;
+      }
+#pragma unroll
+      for (int v = 0; v < VC; ++v) {
+        const uint4 w = z.v[v / 2];
+        const bf16x8 lo = widen8(v % 2 ? w.z : w.x, 1.f), hi = widen8(v % 2 ? w.w : w.y, 1.f);
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          o[x][v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, p[x][0], o[x][v], 0, 0, 0);
+          o[x][v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, p[x][1], o[x][v], 0, 0, 0);
+        }
+      }
+    };
+    auto take = [&]() __attribute__((always_inline)) {
+      const int i = todo ? __builtin_ctzll(todo) : -1;
+      todo &= todo - 1;
+      return i;
+    };
+    int i = take();
+    if (i >= 0) load(at[0], i);
+    while (i >= 0) {
+      const int j = take();
+      if (j >= 0) load(at[1], j);
+      compute(at[0], i);
+      if (j < 0) break;
+      i = take();
+      if (i >= 0) load(at[0], i);
+      compute(at[1], j);
+    }
+  }
+
+  // join the four waves, 16 rows at a time
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    const float sum = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, l[x]), AddF32()), AddF32()));
+    if (x > 0) __syncthreads();
+    if (g == 0) {
+      join_m[wave][n] = m[x];
+      join_l[wave][n] = sum;
+    }
+    __syncthreads();
+    float most = join_m[0][n];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) most = fmaxf(most, join_m[w][n]);
+    float total = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) total += join_l[w][n] * exp2f(join_m[w][n] - most);
+    const float f = total == 0.f ? 0.f : exp2f(m[x] - most) / total;
+#pragma unroll
+    for (int v = 0; v < VC; ++v) *reinterpret_cast<floatx4*>(&join[wave][n][16 * v + 4 * g]) = o[x][v] * f;
+    __syncthreads();
+    constexpr int CPR = D / 8;
+    for (int u = tid; u < 16 * CPR; u += 256) {
+      const int rr = u / CPR, ch = u % CPR * 8, row = t.row0 + 16 * x + rr, tok = t.t0 + row / G;
+      if (row >= t.rows || tok >= t.ql) continue;
+      float z[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] = (join[0][rr][ch + e] + join[1][rr][ch + e]) + (join[2][rr][ch + e] + join[3][rr][ch + e]);
+      if (tg.splits == 1) {
+        uint4 v = make_uint4(pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]), pack_bf16x2(z[4], z[5]), pack_bf16x2(z[6], z[7]));
+        *reinterpret_cast<uint4*>(a.O + (int64_t)t.b * r.sb + (int64_t)(t.hk * G + row % G) * r.sh + (int64_t)tok * r.st + ch) = v;
+      } else {
+        float* dst = a.parts + ((int64_t)blockIdx.x * tg.stored + 16 * x + rr) * D + ch;
+        *reinterpret_cast<float4*>(dst) = make_float4(z[0], z[1], z[2], z[3]);
+        *reinterpret_cast<float4*>(dst + 4) = make_float4(z[4], z[5], z[6], z[7]);
+      }
+    }
+    const int row = t.row0 + 16 * x + n, tok = t.t0 + row / G;
+    if (tid < 16 && row < t.rows && tok < t.ql) {
+      const float lse2 = total == 0.f ? -INFINITY : most + log2f(total);
+      if (tg.splits > 1) (a.parts + (int64_t)gridDim.x * tg.stored * D)[(int64_t)blockIdx.x * tg.stored + 16 * x + n] = lse2;
+      else if (a.lse) a.lse[((int64_t)t.b * r.heads + t.hk * G + row % G) * r.t + tok] = lse2 * kLn2;
+    }
+  }
+}
+
+// The same for many query rows. 64 QT rows to a workgroup, 16 QT to a wave: every wave needs all codes, so they are widened once for
+// the workgroup, a quarter by each wave, into LDS in the order of the operands. Two buffers, one barrier a step of 64 keys.
+constexpr int kAhead = 256;                        // steps that are looked up together
+template <int D, int BLK, int QT>
+__global__ __launch_bounds__(256, 2) void fourbit_tile_kernel(CacheDims c, RowDims r, CacheAttnArgs a, TileGrid tg) {
+  constexpr int KM = D / 32, VC = D / 16, VW = VC / 4;   // VW: channel tiles that a wave widens
+  constexpr int SPB = BLK / 64;
+  constexpr int KR = fourbit_k_record(D), VR = fourbit_v_record(D);
+  constexpr int KBYTES = 4 * KM * 1024, VBYTES = VC * 2048;
+  __shared__ __align__(16) uint8_t lds_k[2][KBYTES], lds_v[2][VBYTES];
+  __shared__ __align__(16) uint32_t lds_s[2][32];  // scales of the values
+  __shared__ int2 look[kAhead];                    // page, first key
+  __shared__ int n_valid[4];
+  const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int g = lane / 16, n = lane % 16;
+  // tiles of one key/value head that walk the same part of the keys follow one another on an XCD
+  const int inner = tg.per_group * a.groups;
+  const int id = xcd_run(blockIdx.x, gridDim.x);
+  const int split = id / inner % tg.splits;
+  const int64_t tile = (int64_t)(id / inner / tg.splits) * inner + (tg.last_first ? inner - 1 - id % inner : id % inner);
+  const Tile t = tile_of(c, r, a, tg, tile);
+  const int G = r.heads / c.heads_kv;
+
+  bf16x8 q[QT][KM];
+  int seen[QT];
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    const int row = t.row0 + (wave * QT + x) * 16 + n, tok = t.t0 + row / G;
+    const bool is = row < t.rows && tok < t.ql;
+    seen[x] = !is ? 0 : visible_keys(c, a, t, tok);
+    const uint16_t* src = a.Q + (int64_t)t.b * r.sb + (int64_t)(t.hk * G + row % G) * r.sh + (int64_t)tok * r.st + g * (D / 4);
+#pragma unroll
+    for (int k = 0; k < KM; ++k) {
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (is) v = *reinterpret_cast<const uint4*>(src + k * 8);
+      q[x][k] = __builtin_bit_cast(bf16x8, v);
+    }
+  }
+  // the queries are here before the loop: a wait for them inside it would be one for every load in flight
+#pragma unroll
+  for (int x = 0; x < QT; ++x)
+#pragma unroll
+    for (int k = 0; k < KM; ++k) asm volatile("" : "+v"(q[x][k]));
+  floatx4 o[QT][VC];
+  float m[QT], l[QT], lazy = kLazy;
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    m[x] = kNoReference;
+    l[x] = 0.f;
+#pragma unroll
+    for (int v = 0; v < VC; ++v) o[x][v] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float all_ks = fmaxf(a.scale_log2e, 0x1p-149f);      // (above 0, so that a masked score stays -inf)
+
+  const int u0 = (int)((int64_t)t.units * split / tg.splits), u1 = (int)((int64_t)t.units * (split + 1) / tg.splits);
+  const int steps = (u1 - u0) * SPB;
+  for (int base = 0; base < steps; base += kAhead) {
+    // the next steps: those with a page, put together in order (one look-up for the workgroup, so that its waves walk the
+    // same steps whatever happens to the table meanwhile)
+    __syncthreads();
+    {
+      const int s = base + tid;
+      int blk = -1, page = -1;
+      if (s < steps) {
+        blk = u0 + s / SPB;
+        if (a.block_idx) blk = a.block_idx[(int64_t)t.lrow * a.list_len + blk];
+        if (blk < t.blocks) page = cache_page(c, t.b, blk);
+      }
+      const unsigned long long all = __ballot(page >= 0);
+      if (lane == 0) n_valid[wave] = __popcll(all);
+      __syncthreads();
+      int at = __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
+      for (int w = 0; w < wave; ++w) at += n_valid[w];
+      if (page >= 0) look[at] = make_int2(page, blk * BLK + s % SPB * 64);
+      __syncthreads();
+    }
+    const int count = __builtin_amdgcn_readfirstlane(n_valid[0] + n_valid[1] + n_valid[2] + n_valid[3]);
+    if (count == 0) continue;
+    struct Step { int page, key; };                // the same in every lane
+    auto entry = [&](int i) __attribute__((always_inline)) { return look[min(i, count - 1)]; };
+    auto step_of = [&](const int2& v) __attribute__((always_inline)) {
+      return Step{__builtin_amdgcn_readfirstlane(v.x), __builtin_amdgcn_readfirstlane(v.y)};
+    };
+    uint32_t raw_k[KM], raw_v[2 * VW], raw_ks, raw_vs;
+    auto request = [&](const Step& z) __attribute__((always_inline)) {
+      const int64_t rec = ((int64_t)z.page * c.heads_kv + t.hk) * SPB + z.key % BLK / 64;
+      const uint8_t *pk = c.k + rec * KR, *pv = c.v + rec * VR;
+      raw_ks = *reinterpret_cast<const uint32_t*>(pk + 32 * D + (D == 128 ? lane : (g / 2) * 16 + n) * 4);
+      raw_vs = *reinterpret_cast<const uint32_t*>(pv + 32 * D + (lane % 32) * 4);
+      if constexpr (D == 128) {
+        const uint4 k = *reinterpret_cast<const uint4*>(pk + wave * 1024 + lane * 16);
+        raw_k[0] = k.x; raw_k[1] = k.y; raw_k[2] = k.z; raw_k[3] = k.w;
+        const uint4 v = *reinterpret_cast<const uint4*>(pv + wave * 1024 + lane * 16);
+        raw_v[0] = v.x; raw_v[1] = v.y; raw_v[2] = v.z; raw_v[3] = v.w;
+      } else {
+        const uint2 k = *reinterpret_cast<const uint2*>(pk + wave * 512 + ((g / 2) * 16 + n) * 16 + (g % 2) * 8);
+        raw_k[0] = k.x; raw_k[1] = k.y;
+        const uint2 v = *reinterpret_cast<const uint2*>(pv + wave / 2 * 1024 + lane * 16 + wave % 2 * 8);
+        raw_v[0] = v.x; raw_v[1] = v.y;
+      }
+    };
+    auto store = [&](int buf) __attribute__((always_inline)) {
+      const float sc = key_scale(raw_ks, wave);
+#pragma unroll
+      for (int k = 0; k < KM; ++k) *reinterpret_cast<bf16x8*>(lds_k[buf] + (wave * KM + k) * 1024 + lane * 16) = widen8(raw_k[k], sc);
+#pragma unroll
+      for (int x = 0; x < 2 * VW; ++x) *reinterpret_cast<bf16x8*>(lds_v[buf] + (wave * 2 * VW + x) * 1024 + lane * 16) = widen8(raw_v[x], 1.f);
+      if (tid < 32) lds_s[buf][tid] = raw_vs;
+    };
+
+    Step now = step_of(entry(0)), next = step_of(entry(1));
+    request(now);
+    store(0);
+    request(next);
+    for (int i = 0; i < count; ++i) {
+      __syncthreads();
+      const int2 ahead = entry(i + 2);
+      const bool partly = now.key + 64 > t.lo_seen;
+      uint4 vw[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) vw[x] = *reinterpret_cast<const uint4*>(&lds_s[i & 1][g * 8 + x * 4]);
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
+      floatx4 s[QT][4];
+#pragma unroll
+      for (int x = 0; x < QT; ++x)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) s[x][y] = floatx4{0.f, 0.f, 0.f, 0.f};
+      {
+        const uint8_t* buf = lds_k[i & 1] + lane * 16;
+#pragma unroll
+        for (int k = 0; k < KM; ++k)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {            // (a sum is touched again 4 QT products later)
+            const bf16x8 op = *reinterpret_cast<const bf16x8*>(buf + (y * KM + k) * 1024);
+#pragma unroll
+            for (int x = 0; x < QT; ++x) s[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op, q[x][k], s[x][y], 0, 0, 0);
+          }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+#pragma unroll
+      for (int u = 0; u < 4 * KM - 4; ++u) {
+        __builtin_amdgcn_sched_group_barrier(0x008, QT, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, QT * 4, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(0);
+      if (partly) {
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          const int left = seen[x] - now.key;
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[x][y][e] = 16 * y + 4 * g + e < left ? s[x][y][e] : -INFINITY;
+        }
+      }
+      float most[QT];
+      bool over = false;
+#pragma unroll
+      for (int x = 0; x < QT; ++x) {
+        most[x] = -INFINITY;
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) most[x] = fmaxf(fmaxf(most[x], s[x][y][e]), s[x][y][e + 1]);
+        most[x] *= all_ks;
+        over |= most[x] > m[x] + lazy;
+      }
+      if (__any(over)) {
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          const float mx = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, most[x]), MaxF32()), MaxF32()));
+          const float to = mx > m[x] + lazy ? floorf(mx) : m[x];    // the same in the four lanes of a column; whole, as above
+          const float down = __builtin_amdgcn_exp2f(m[x] - to);
+          m[x] = to;
+          l[x] *= down;
+#pragma unroll
+          for (int v = 0; v < VC; ++v) o[x][v] *= down;
+        }
+        if (far_from_zero<QT>(m)) lazy = 0.f;
+      }
+      // Far from zero the multiply-add below would leave a product's own rounding, which may be 2^8 and more: rounded products, as m is one
+      float ks = all_ks;
+      if (__builtin_expect(lazy == 0.f, 0)) {
+        ks = 1.f;
+#pragma unroll
+        for (int x = 0; x < QT; ++x)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) s[x][y] *= all_ks;
+      }
+      float vs[4][4];
+      value_scales(vw, vs);
+      bf16x8 p[QT][2];
+#pragma unroll
+      for (int x = 0; x < QT; ++x) {
+        float sum = 0.f;
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) {
+            floatx2 w;
+#pragma unroll
+            for (int f = 0; f < 2; ++f) {
+              const float one = __builtin_amdgcn_exp2f(fmaf(s[x][y][e + f], ks, -m[x]));
+              sum += one;
+              w[f] = one * vs[y][e + f];
+            }
+            if (partly) {                          // no NaN of a token that a row does not see into 0 * NaN
+#pragma unroll
+              for (int f = 0; f < 2; ++f) w[f] = s[x][y][e + f] == -INFINITY ? 0.f : w[f];
+            }
+            const bf16x2 b = __builtin_convertvector(w, bf16x2);
+            p[x][y / 2][y % 2 * 4 + e] = b[0];
+            p[x][y / 2][y % 2 * 4 + e + 1] = b[1];
+          }
+        l[x] += sum;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      store((i + 1) & 1);
+      const Step later = step_of(ahead);
+      request(later);
+      __builtin_amdgcn_s_setprio(1);
+      const uint8_t* buf = lds_v[i & 1] + lane * 16;
+#pragma unroll
+      for (int v = 0; v < VC; v += 2)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+          for (int vv = v; vv < v + 2; ++vv) {
+            const bf16x8 op = *reinterpret_cast<const bf16x8*>(buf + (vv * 2 + hf) * 1024);
+#pragma unroll
+            for (int x = 0; x < QT; ++x) o[x][vv] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op, p[x][hf], o[x][vv], 0, 0, 0);
+          }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+#pragma unroll
+      for (int u = 0; u < 2 * VC - 4; ++u) {
+        __builtin_amdgcn_sched_group_barrier(0x008, QT, 1);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, QT * 4, 1);
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(0);
+      now = next;
+      next = later;
+    }
+  }
+
+  // rows out: normalised, turned through the wave's share of a buffer
+  constexpr int PITCH = D + 8;                     // bf16 of a row
+  static_assert(4 * 16 * PITCH * 2 <= 2 * KBYTES, "rows of a wave do not fit");
+  uint16_t* turn = reinterpret_cast<uint16_t*>(&lds_k[0][0]) + wave * 16 * PITCH;
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    const float total = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, l[x]), AddF32()), AddF32()));
+    const float f = total == 0.f ? 0.f : 1.f / total;
+    const int first = (wave * QT + x) * 16, row = t.row0 + first + n, tok = t.t0 + row / G;
+    const float lse2 = total == 0.f ? -INFINITY : m[x] + log2f(total);
+    const bool is = row < t.rows && tok < t.ql;
+    if (tg.splits > 1) {
+      const int64_t at = (tile * tg.splits + split) * tg.stored + first + n;
+      if (is) {
+#pragma unroll
+        for (int v = 0; v < VC; ++v) *reinterpret_cast<floatx4*>(a.parts + at * D + 16 * v + 4 * g) = o[x][v] * f;
+        if (g == 0) (a.parts + (int64_t)gridDim.x * tg.stored * D)[at] = lse2;
+      }
+      continue;
+    }
+    if (is && g == 0 && a.lse) a.lse[((int64_t)t.b * r.heads + t.hk * G + row % G) * r.t + tok] = lse2 * kLn2;
+#pragma unroll
+    for (int v = 0; v < VC; ++v) {
+      const floatx4 z = o[x][v] * f;
+      *reinterpret_cast<uint2*>(turn + n * PITCH + 16 * v + 4 * g) = make_uint2(pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]));
+    }
+    __builtin_amdgcn_wave_barrier();               // (the wave's own rows: LDS keeps a wave's order)
+#pragma unroll
+    for (int u = lane; u < 16 * (D / 8); u += 64) {
+      const int rr = u / (D / 8), ch = u % (D / 8) * 8, orow = t.row0 + first + rr, otok = t.t0 + orow / G;
+      if (orow < t.rows && otok < t.ql)
+        *reinterpret_cast<uint4*>(a.O + (int64_t)t.b * r.sb + (int64_t)(t.hk * G + orow % G) * r.sh + (int64_t)otok * r.st + ch) =
+            *reinterpret_cast<const uint4*>(turn + rr * PITCH + ch);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+template <int D, int BLK>
+hipError_t launch_t(const CacheDims& c, const RowDims& r, const CacheAttnArgs& a, Plan p, hipStream_t s) {
+  const dim3 grid((uint32_t)(p.tiles * p.grid.splits)), block(256);
+  // Where there are several rounds of tiles and the last tokens see the most keys, these go first, so that the launch ends with short tiles.
+  p.grid.last_first = a.causal && p.tiles * p.grid.splits > 2 * kCus;
+  if (p.tiled && p.qt == 1) hipLaunchKernelGGL((fourbit_tile_kernel<D, BLK, 1>), grid, block, 0, s, c, r, a, p.grid);
+  else if (p.tiled) hipLaunchKernelGGL((fourbit_tile_kernel<D, BLK, 2>), grid, block, 0, s, c, r, a, p.grid);
+  else if (p.qt == 1) hipLaunchKernelGGL((fourbit_attn_kernel<D, BLK, 1>), grid, block, 0, s, c, r, a, p.grid);
+  else hipLaunchKernelGGL((fourbit_attn_kernel<D, BLK, 2>), grid, block, 0, s, c, r, a, p.grid);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess ? e : launch_join<D>(c, r, a, p, s);
+}
+
+}  // namespace
+
+int64_t fourbit_attn_workgroups(const CacheDims& c, const RowDims& r, int group, int list_len) {
+  const Plan p = plan_of(c, r, group, list_len);
+  return p.tiles * p.grid.splits;
+}
+
+size_t fourbit_attn_parts_bytes(const CacheDims& c, const RowDims& r, int group, int list_len) {
+  const Plan p = plan_of(c, r, group, list_len);
+  return p.grid.splits == 1 ? 0 : (size_t)p.tiles * p.grid.splits * p.grid.stored * (c.d + 1) * sizeof(float);
+}
+
+hipError_t launch_fourbit_attn(const CacheDims& c, const RowDims& r, const CacheAttnArgs& a, hipStream_t s) {
+  Plan p = plan_of(c, r, a.block_idx ? a.group : 0, a.block_idx ? a.list_len : 0);
+  if (!a.parts) p.grid.splits = 1;
+  if (c.d == 128) return c.blk == 128 ? launch_t<128, 128>(c, r, a, p, s) : launch_t<128, 64>(c, r, a, p, s);
+  return c.blk == 128 ? launch_t<64, 128>(c, r, a, p, s) : launch_t<64, 64>(c, r, a, p, s);
+}
+
+}  // namespace rsa
