@@ -321,7 +321,8 @@ __global__ __launch_bounds__(256, 2) void fourbit_tile_kernel(CacheDims c, RowDi
 #pragma unroll
     for (int k = 0; k < KM; ++k) asm volatile("" : "+v"(q[x][k]));
   floatx4 o[QT][VC];
-  float m[QT], l[QT], lazy = kLazy;
+  float m[QT], l[QT];
+  bool far = false;                                // a reference is 2^23 and more
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
     m[x] = kNoReference;
@@ -436,34 +437,10 @@ __global__ __launch_bounds__(256, 2) void fourbit_tile_kernel(CacheDims c, RowDi
             for (int e = 0; e < 4; ++e) s[x][y][e] = 16 * y + 4 * g + e < left ? s[x][y][e] : -INFINITY;
         }
       }
-      float most[QT];
-      bool over = false;
-#pragma unroll
-      for (int x = 0; x < QT; ++x) {
-        most[x] = -INFINITY;
-#pragma unroll
-        for (int y = 0; y < 4; ++y)
-#pragma unroll
-          for (int e = 0; e < 4; e += 2) most[x] = fmaxf(fmaxf(most[x], s[x][y][e]), s[x][y][e + 1]);
-        most[x] *= all_ks;
-        over |= most[x] > m[x] + lazy;
-      }
-      if (__any(over)) {
-#pragma unroll
-        for (int x = 0; x < QT; ++x) {
-          const float mx = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, most[x]), MaxF32()), MaxF32()));
-          const float to = mx > m[x] + lazy ? floorf(mx) : m[x];    // the same in the four lanes of a column; whole, as above
-          const float down = __builtin_amdgcn_exp2f(m[x] - to);
-          m[x] = to;
-          l[x] *= down;
-#pragma unroll
-          for (int v = 0; v < VC; ++v) o[x][v] *= down;
-        }
-        if (far_from_zero<QT>(m)) lazy = 0.f;
-      }
-      // Far from zero the multiply-add below would leave a product's own rounding, which may be 2^8 and more: rounded products, as m is one
+      // Weights over the running reference. It is moved only when a lane's weights add up to more than 2^8 (bf16 and fp32 have the range), so
+      // that no maximum is taken otherwise; then they are made once more, over the new one at most 2^1.25.
       float ks = all_ks;
-      if (__builtin_expect(lazy == 0.f, 0)) {
+      if (far) {
         ks = 1.f;
 #pragma unroll
         for (int x = 0; x < QT; ++x)
@@ -473,29 +450,69 @@ __global__ __launch_bounds__(256, 2) void fourbit_tile_kernel(CacheDims c, RowDi
       float vs[4][4];
       value_scales(vw, vs);
       bf16x8 p[QT][2];
+      float sum[QT];
+      auto weigh = [&]() __attribute__((always_inline)) {
+        bool over = false;
 #pragma unroll
-      for (int x = 0; x < QT; ++x) {
-        float sum = 0.f;
+        for (int x = 0; x < QT; ++x) {
+          sum[x] = 0.f;
 #pragma unroll
-        for (int y = 0; y < 4; ++y)
+          for (int y = 0; y < 4; ++y)
 #pragma unroll
-          for (int e = 0; e < 4; e += 2) {
-            floatx2 w;
+            for (int e = 0; e < 4; e += 2) {
+              floatx2 w;
 #pragma unroll
-            for (int f = 0; f < 2; ++f) {
-              const float one = __builtin_amdgcn_exp2f(fmaf(s[x][y][e + f], ks, -m[x]));
-              sum += one;
-              w[f] = one * vs[y][e + f];
+              for (int f = 0; f < 2; ++f) {
+                const float one = __builtin_amdgcn_exp2f(fmaf(s[x][y][e + f], ks, -m[x]));
+                sum[x] += one;
+                w[f] = one * vs[y][e + f];
+              }
+              const bf16x2 b = __builtin_convertvector(w, bf16x2);
+              p[x][y / 2][y % 2 * 4 + e] = b[0];
+              p[x][y / 2][y % 2 * 4 + e + 1] = b[1];
             }
-            if (partly) {                          // no NaN of a token that a row does not see into 0 * NaN
+          over |= sum[x] > 256.f;
+        }
+        return over;
+      };
+      if (__any(weigh())) {
 #pragma unroll
-              for (int f = 0; f < 2; ++f) w[f] = s[x][y][e + f] == -INFINITY ? 0.f : w[f];
-            }
-            const bf16x2 b = __builtin_convertvector(w, bf16x2);
-            p[x][y / 2][y % 2 * 4 + e] = b[0];
-            p[x][y / 2][y % 2 * 4 + e + 1] = b[1];
-          }
-        l[x] += sum;
+        for (int x = 0; x < QT; ++x) {
+          float mx = -INFINITY;
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[x][y][e]);
+          mx = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, mx), MaxF32()), MaxF32())) * ks;
+          const float to = mx > m[x] ? floorf(mx) : m[x];           // the same in the four lanes of a column; whole, so that what is taken from it stays exact
+          const float down = __builtin_amdgcn_exp2f(m[x] - to);
+          m[x] = to;
+          l[x] *= down;
+#pragma unroll
+          for (int v = 0; v < VC; ++v) o[x][v] *= down;
+        }
+        // Far from zero a multiply-add would leave a product's own rounding, which may be 2^8 and more: rounded products from here on, as m is one
+        if (!far && far_from_zero<QT>(m)) {
+          far = true;
+          ks = 1.f;
+#pragma unroll
+          for (int x = 0; x < QT; ++x)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) s[x][y] *= all_ks;
+        }
+        weigh();
+      }
+#pragma unroll
+      for (int x = 0; x < QT; ++x) l[x] += sum[x];
+      if (partly) {                                // no NaN of a token that a row does not see into 0 * NaN
+        asm volatile("");                          // (a branch, not selects in every step)
+#pragma unroll
+        for (int x = 0; x < QT; ++x)
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (s[x][y][e] == -INFINITY) p[x][y / 2][y % 2 * 4 + e] = (__bf16)0.f;
       }
       __builtin_amdgcn_sched_barrier(0);
       store((i + 1) & 1);
