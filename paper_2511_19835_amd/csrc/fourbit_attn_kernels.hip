@@ -277,6 +277,20 @@ __global__ __launch_bounds__(256, 2) void fourbit_attn_kernel(CacheDims c, RowDi
   }
 }
 
+// Weights are made 2^kBias too large, as large as a sum over 2^31 keys allows, so that a token's scale comes in by a subtraction of exponents
+// (16 bits, two at once; below 0 it stays 0): bits of the scale taken from those of 2^kBias say by how much. Scales above 2^kBias and NaN
+// go the long way.
+constexpr float kBias = 90.f;
+constexpr uint32_t kMostScale = 0x6c806c80u;     // 2^90 in bf16, twice
+typedef uint16_t ushortx2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t less_than_most(uint32_t w) {      // (its own inverse)
+  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(ushortx2, kMostScale) - __builtin_bit_cast(ushortx2, w));
+}
+__device__ __forceinline__ bf16x2 scaled2(float a, float b, uint32_t less) {
+  const uint32_t w = pack_bf16x2(a, b);
+  return __builtin_bit_cast(bf16x2, __builtin_elementwise_sub_sat(__builtin_bit_cast(ushortx2, w), __builtin_bit_cast(ushortx2, less)));
+}
+
 // The same for many query rows. 64 QT rows to a workgroup, 16 QT to a wave: every wave needs all codes, so they are widened once for
 // the workgroup, a quarter by each wave, into LDS in the order of the operands. Two buffers, one barrier a step of 64 keys.
 constexpr int kAhead = 256;                        // steps that are looked up together
@@ -361,44 +375,46 @@ __global__ __launch_bounds__(256, 2) void fourbit_tile_kernel(CacheDims c, RowDi
     auto step_of = [&](const int2& v) __attribute__((always_inline)) {
       return Step{__builtin_amdgcn_readfirstlane(v.x), __builtin_amdgcn_readfirstlane(v.y)};
     };
-    uint32_t raw_k[KM], raw_v[2 * VW], raw_ks, raw_vs;
-    auto request = [&](const Step& z) __attribute__((always_inline)) {
+    struct Raw { uint32_t k[KM], v[2 * VW], ks, vs; } ra, rb;      // of the next step and of the one behind it
+    auto request = [&](const Step& z, Raw& raw) __attribute__((always_inline)) {
       const int64_t rec = ((int64_t)z.page * c.heads_kv + t.hk) * SPB + z.key % BLK / 64;
       const uint8_t *pk = c.k + rec * KR, *pv = c.v + rec * VR;
-      raw_ks = *reinterpret_cast<const uint32_t*>(pk + 32 * D + (D == 128 ? lane : (g / 2) * 16 + n) * 4);
-      raw_vs = *reinterpret_cast<const uint32_t*>(pv + 32 * D + (lane % 32) * 4);
+      raw.ks = *reinterpret_cast<const uint32_t*>(pk + 32 * D + (D == 128 ? lane : (g / 2) * 16 + n) * 4);
+      raw.vs = *reinterpret_cast<const uint32_t*>(pv + 32 * D + (lane % 32) * 4);
       if constexpr (D == 128) {
         const uint4 k = *reinterpret_cast<const uint4*>(pk + wave * 1024 + lane * 16);
-        raw_k[0] = k.x; raw_k[1] = k.y; raw_k[2] = k.z; raw_k[3] = k.w;
+        raw.k[0] = k.x; raw.k[1] = k.y; raw.k[2] = k.z; raw.k[3] = k.w;
         const uint4 v = *reinterpret_cast<const uint4*>(pv + wave * 1024 + lane * 16);
-        raw_v[0] = v.x; raw_v[1] = v.y; raw_v[2] = v.z; raw_v[3] = v.w;
+        raw.v[0] = v.x; raw.v[1] = v.y; raw.v[2] = v.z; raw.v[3] = v.w;
       } else {
         const uint2 k = *reinterpret_cast<const uint2*>(pk + wave * 512 + ((g / 2) * 16 + n) * 16 + (g % 2) * 8);
-        raw_k[0] = k.x; raw_k[1] = k.y;
+        raw.k[0] = k.x; raw.k[1] = k.y;
         const uint2 v = *reinterpret_cast<const uint2*>(pv + wave / 2 * 1024 + lane * 16 + wave % 2 * 8);
-        raw_v[0] = v.x; raw_v[1] = v.y;
+        raw.v[0] = v.x; raw.v[1] = v.y;
       }
     };
-    auto store = [&](int buf) __attribute__((always_inline)) {
-      const float sc = key_scale(raw_ks, wave);
+    auto store = [&](int buf, const Raw& raw) __attribute__((always_inline)) {
+      const float sc = key_scale(raw.ks, wave);
 #pragma unroll
-      for (int k = 0; k < KM; ++k) *reinterpret_cast<bf16x8*>(lds_k[buf] + (wave * KM + k) * 1024 + lane * 16) = widen8(raw_k[k], sc);
+      for (int k = 0; k < KM; ++k) *reinterpret_cast<bf16x8*>(lds_k[buf] + (wave * KM + k) * 1024 + lane * 16) = widen8(raw.k[k], sc);
 #pragma unroll
-      for (int x = 0; x < 2 * VW; ++x) *reinterpret_cast<bf16x8*>(lds_v[buf] + (wave * 2 * VW + x) * 1024 + lane * 16) = widen8(raw_v[x], 1.f);
-      if (tid < 32) lds_s[buf][tid] = raw_vs;
+      for (int x = 0; x < 2 * VW; ++x) *reinterpret_cast<bf16x8*>(lds_v[buf] + (wave * 2 * VW + x) * 1024 + lane * 16) = widen8(raw.v[x], 1.f);
+      if (tid < 32) lds_s[buf][tid] = less_than_most(raw.vs);
+      return __any((raw.vs & 0x7fffu) > (kMostScale & 0xffffu) || (raw.vs >> 16 & 0x7fffu) > (kMostScale & 0xffffu)) != 0;
     };
 
-    Step now = step_of(entry(0)), next = step_of(entry(1));
-    request(now);
-    store(0);
-    request(next);
-    for (int i = 0; i < count; ++i) {
+    Step now = step_of(entry(0)), next = step_of(entry(1)), third = step_of(entry(2));
+    request(now, rb);
+    request(next, ra);
+    bool odd = store(0, rb);                       // of the step `now`
+    request(third, rb);
+    auto step = [&](int i, Raw& raw) __attribute__((always_inline)) {
       __syncthreads();
-      const int2 ahead = entry(i + 2);
+      const int2 ahead = entry(i + 3);
       const bool partly = now.key + 64 > t.lo_seen;
-      uint4 vw[2];
+      uint4 less[2];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) vw[x] = *reinterpret_cast<const uint4*>(&lds_s[i & 1][g * 8 + x * 4]);
+      for (int x = 0; x < 2; ++x) less[x] = *reinterpret_cast<const uint4*>(&lds_s[i & 1][g * 8 + x * 4]);
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_s_setprio(1);
       floatx4 s[QT][4];
@@ -441,37 +457,37 @@ __global__ __launch_bounds__(256, 2) void fourbit_tile_kernel(CacheDims c, RowDi
       // that no maximum is taken otherwise; then they are made once more, over the new one at most 2^1.25.
       float ks = all_ks;
       if (far) {
+        asm volatile("");
         ks = 1.f;
 #pragma unroll
         for (int x = 0; x < QT; ++x)
 #pragma unroll
           for (int y = 0; y < 4; ++y) s[x][y] *= all_ks;
       }
-      float vs[4][4];
-      value_scales(vw, vs);
       bf16x8 p[QT][2];
       float sum[QT];
+      // Weights times 2^kBias over the running reference, and their sums; in P their tokens' scales are taken in.
       auto weigh = [&]() __attribute__((always_inline)) {
         bool over = false;
 #pragma unroll
         for (int x = 0; x < QT; ++x) {
+          const float ref = m[x] - kBias;
           sum[x] = 0.f;
 #pragma unroll
-          for (int y = 0; y < 4; ++y)
+          for (int y = 0; y < 4; ++y) {
+            float w[4];
 #pragma unroll
-            for (int e = 0; e < 4; e += 2) {
-              floatx2 w;
-#pragma unroll
-              for (int f = 0; f < 2; ++f) {
-                const float one = __builtin_amdgcn_exp2f(fmaf(s[x][y][e + f], ks, -m[x]));
-                sum[x] += one;
-                w[f] = one * vs[y][e + f];
-              }
-              const bf16x2 b = __builtin_convertvector(w, bf16x2);
-              p[x][y / 2][y % 2 * 4 + e] = b[0];
-              p[x][y / 2][y % 2 * 4 + e + 1] = b[1];
+            for (int e = 0; e < 4; ++e) {
+              w[e] = __builtin_amdgcn_exp2f(fmaf(s[x][y][e], ks, -ref));
+              sum[x] += w[e];
             }
-          over |= sum[x] > 256.f;
+            const uint32_t d0 = y % 2 ? less[y / 2].z : less[y / 2].x, d1 = y % 2 ? less[y / 2].w : less[y / 2].y;
+            const bf16x2 lo = scaled2(w[0], w[1], d0), hi = scaled2(w[2], w[3], d1);
+            p[x][y / 2][y % 2 * 4 + 0] = lo[0]; p[x][y / 2][y % 2 * 4 + 1] = lo[1];
+            p[x][y / 2][y % 2 * 4 + 2] = hi[0]; p[x][y / 2][y % 2 * 4 + 3] = hi[1];
+          }
+          over |= sum[x] > 0x1p98f;
+          asm volatile("" : "+v"(p[x][0]), "+v"(p[x][1]));     // (made here, not behind the branches)
         }
         return over;
       };
@@ -504,20 +520,30 @@ __global__ __launch_bounds__(256, 2) void fourbit_tile_kernel(CacheDims c, RowDi
       }
 #pragma unroll
       for (int x = 0; x < QT; ++x) l[x] += sum[x];
-      if (partly) {                                // no NaN of a token that a row does not see into 0 * NaN
-        asm volatile("");                          // (a branch, not selects in every step)
+      if (odd) {                                   // rare: P by products, and no NaN of a token that a row does not see into 0 * NaN
+        asm volatile("");
+        uint4 vw[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const uint32_t* z = &lds_s[i & 1][g * 8 + x * 4];
+          vw[x] = make_uint4(less_than_most(z[0]), less_than_most(z[1]), less_than_most(z[2]), less_than_most(z[3]));
+        }
+        float vs[4][4];
+        value_scales(vw, vs);
 #pragma unroll
         for (int x = 0; x < QT; ++x)
 #pragma unroll
           for (int y = 0; y < 4; ++y)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (s[x][y][e] == -INFINITY) p[x][y / 2][y % 2 * 4 + e] = (__bf16)0.f;
+            for (int e = 0; e < 4; ++e) {
+              const float w = __builtin_amdgcn_exp2f(fmaf(s[x][y][e], ks, -m[x])) * vs[y][e];
+              p[x][y / 2][y % 2 * 4 + e] = (__bf16)(s[x][y][e] == -INFINITY ? 0.f : w);
+            }
       }
       __builtin_amdgcn_sched_barrier(0);
-      store((i + 1) & 1);
+      odd = store((i + 1) & 1, raw);
       const Step later = step_of(ahead);
-      request(later);
+      request(later, raw);
       __builtin_amdgcn_s_setprio(1);
       const uint8_t* buf = lds_v[i & 1] + lane * 16;
 #pragma unroll
@@ -541,7 +567,13 @@ __global__ __launch_bounds__(256, 2) void fourbit_tile_kernel(CacheDims c, RowDi
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_s_setprio(0);
       now = next;
-      next = later;
+      next = third;
+      third = later;
+    };
+    for (int i = 0; i < count; i += 2) {
+      step(i, ra);
+      if (i + 1 >= count) break;
+      step(i + 1, rb);
     }
   }
 
@@ -552,7 +584,7 @@ __global__ __launch_bounds__(256, 2) void fourbit_tile_kernel(CacheDims c, RowDi
   __syncthreads();
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
-    const float total = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, l[x]), AddF32()), AddF32()));
+    const float total = ldexpf(__builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, l[x]), AddF32()), AddF32())), -(int)kBias);
     const float f = total == 0.f ? 0.f : 1.f / total;
     const int first = (wave * QT + x) * 16, row = t.row0 + first + n, tok = t.t0 + row / G;
     const float lse2 = total == 0.f ? -INFINITY : m[x] + log2f(total);
