@@ -59,7 +59,7 @@ __global__ __launch_bounds__(256, 2) void fourbit_attn_kernel(CacheDims c, RowDi
   constexpr int KR = fourbit_k_record(D), VR = fourbit_v_record(D);
   constexpr int PITCH = D + 4;                     // floats of a row in the joining buffer
   __shared__ __align__(16) float join[4][16][PITCH];
-  __shared__ float join_m[4][16], join_l[4][16];
+  __shared__ float join_m[4][16], join_l[4][16], join_r[4][16];
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
   const int g = lane / 16, n = lane % 16;
   const int split = blockIdx.x % tg.splits;
@@ -84,11 +84,11 @@ __global__ __launch_bounds__(256, 2) void fourbit_attn_kernel(CacheDims c, RowDi
     }
   }
   floatx4 o[QT][VC];
-  float m[QT], l[QT], lazy = kLazy;
+  float m[QT], l[QT], lr[QT], lazy = kLazy;         // sums of the weights, and of what they are in P
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
     m[x] = kNoReference;
-    l[x] = 0.f;
+    l[x] = lr[x] = 0.f;
 #pragma unroll
     for (int v = 0; v < VC; ++v) o[x][v] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
@@ -105,10 +105,12 @@ __global__ __launch_bounds__(256, 2) void fourbit_attn_kernel(CacheDims c, RowDi
       if (my_blk < t.blocks) my_page = cache_page(c, t.b, my_blk);
     }
     unsigned long long todo = __ballot(my_page >= 0);
-    Step64<D> at[2];
-    auto load = [&](Step64<D>& z, int i) __attribute__((always_inline)) {
+    // Two steps are in registers, one used and one on its way; where two tiles of rows leave no room, one, loaded again as it is used up.
+    constexpr int SETS = QT == 1 ? 2 : 1;
+    Step64<D> at[SETS];
+    auto load_k = [&](Step64<D>& z, int i) __attribute__((always_inline)) {
       const int64_t rec = ((int64_t)__builtin_amdgcn_readlane(my_page, i) * c.heads_kv + t.hk) * SPB + (base + i * 4) % SPB;
-      const uint8_t *pk = c.k + rec * KR, *pv = c.v + rec * VR;
+      const uint8_t* pk = c.k + rec * KR;
       z.ks = *reinterpret_cast<const uint32_t*>(pk + 32 * D + (D == 128 ? lane : (g / 2) * 16 + n) * 4);
 #pragma unroll
       for (int y = 0; y < 4; ++y) {
@@ -120,12 +122,16 @@ __global__ __launch_bounds__(256, 2) void fourbit_attn_kernel(CacheDims c, RowDi
           z.k[y][0] = w.x; z.k[y][1] = w.y;
         }
       }
+    };
+    auto load_v = [&](Step64<D>& z, int i) __attribute__((always_inline)) {
+      const int64_t rec = ((int64_t)__builtin_amdgcn_readlane(my_page, i) * c.heads_kv + t.hk) * SPB + (base + i * 4) % SPB;
+      const uint8_t* pv = c.v + rec * VR;
 #pragma unroll
       for (int x = 0; x < 2; ++x) z.vs[x] = *reinterpret_cast<const uint4*>(pv + 32 * D + g * 32 + x * 16);
 #pragma unroll
       for (int x = 0; x < D / 32; ++x) z.v[x] = *reinterpret_cast<const uint4*>(pv + x * 1024 + lane * 16);
     };
-    auto compute = [&](const Step64<D>& z, int i) __attribute__((always_inline)) {
+    auto compute = [&](Step64<D>& z, int i, int again) __attribute__((always_inline)) {
       const int key0 = __builtin_amdgcn_readlane(my_blk, i) * BLK + ((base + i * 4) % SPB) * 64;
       floatx4 s[QT][4];
 #pragma unroll
@@ -142,6 +148,7 @@ __global__ __launch_bounds__(256, 2) void fourbit_attn_kernel(CacheDims c, RowDi
           for (int x = 0; x < QT; ++x) s[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op, q[x][k], s[x][y], 0, 0, 0);
         }
       }
+      if (SETS == 1) load_k(z, again);
       // scores; keys that a row does not see leave its softmax
       const bool partly = key0 + 64 > t.lo_seen;
       bool over = false;
@@ -172,6 +179,7 @@ __global__ __launch_bounds__(256, 2) void fourbit_attn_kernel(CacheDims c, RowDi
             const float down = exp2f(m[x] - mx);
             m[x] = mx;
             l[x] *= down;
+            lr[x] *= down;
 #pragma unroll
             for (int v = 0; v < VC; ++v) o[x][v] *= down;
           }
@@ -183,25 +191,28 @@ __global__ __launch_bounds__(256, 2) void fourbit_attn_kernel(CacheDims c, RowDi
       bf16x8 p[QT][2];
 #pragma unroll
       for (int x = 0; x < QT; ++x) {
-        float sum = 0.f;
+        float sum = 0.f, rounded = 0.f;
 #pragma unroll
         for (int y = 0; y < 4; ++y)
 #pragma unroll
           for (int e = 0; e < 4; e += 2) {
-            floatx2 w;
-#pragma unroll
-            for (int f = 0; f < 2; ++f) {
-              const float one = __builtin_amdgcn_exp2f(s[x][y][e + f] - m[x]);
-              sum += one;
-              w[f] = one * vs[y][e + f];
-              // a value that is NaN under a key that a row does not see must not reach it through 0 * NaN
-              if (partly) w[f] = s[x][y][e + f] == -INFINITY ? 0.f : w[f];
-            }
+            const floatx2 w = {__builtin_amdgcn_exp2f(s[x][y][e] - m[x]), __builtin_amdgcn_exp2f(s[x][y][e + 1] - m[x])};
+            sum += w[0] + w[1];
             const bf16x2 b = __builtin_convertvector(w, bf16x2);
-            p[x][y / 2][y % 2 * 4 + e] = b[0];
-            p[x][y / 2][y % 2 * 4 + e + 1] = b[1];
+            const float w0 = (float)b[0], w1 = (float)b[1];
+            rounded += w0 + w1;
+            floatx2 z = {w0 * vs[y][e], w1 * vs[y][e + 1]};          // (exact)
+            // a value that is NaN under a key that a row does not see must not reach it through 0 * NaN
+            if (partly) {
+              if (s[x][y][e] == -INFINITY) z[0] = 0.f;
+              if (s[x][y][e + 1] == -INFINITY) z[1] = 0.f;
+            }
+            const bf16x2 p2 = __builtin_convertvector(z, bf16x2);
+            p[x][y / 2][y % 2 * 4 + e] = p2[0];
+            p[x][y / 2][y % 2 * 4 + e + 1] = p2[1];
           }
         l[x] += sum;
+        lr[x] += rounded;
       }
 #pragma unroll
       for (int v = 0; v < VC; ++v) {
@@ -213,6 +224,7 @@ __global__ __launch_bounds__(256, 2) void fourbit_attn_kernel(CacheDims c, RowDi
           o[x][v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, p[x][1], o[x][v], 0, 0, 0);
         }
       }
+      if (SETS == 1) load_v(z, again);
     };
     auto take = [&]() __attribute__((always_inline)) {
       const int i = todo ? __builtin_ctzll(todo) : -1;
@@ -220,15 +232,29 @@ __global__ __launch_bounds__(256, 2) void fourbit_attn_kernel(CacheDims c, RowDi
       return i;
     };
     int i = take();
-    if (i >= 0) load(at[0], i);
+    if (i >= 0) {
+      load_k(at[0], i);
+      load_v(at[0], i);
+    }
     while (i >= 0) {
       const int j = take();
-      if (j >= 0) load(at[1], j);
-      compute(at[0], i);
-      if (j < 0) break;
-      i = take();
-      if (i >= 0) load(at[0], i);
-      compute(at[1], j);
+      if constexpr (SETS == 1) {
+        compute(at[0], i, j < 0 ? i : j);
+        i = j;
+      } else {
+        if (j >= 0) {
+          load_k(at[1], j);
+          load_v(at[1], j);
+        }
+        compute(at[0], i, i);
+        if (j < 0) break;
+        i = take();
+        if (i >= 0) {
+          load_k(at[0], i);
+          load_v(at[0], i);
+        }
+        compute(at[1], j, j);
+      }
     }
   }
 
@@ -236,19 +262,25 @@ __global__ __launch_bounds__(256, 2) void fourbit_attn_kernel(CacheDims c, RowDi
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
     const float sum = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, l[x]), AddF32()), AddF32()));
+    const float rounded = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, lr[x]), AddF32()), AddF32()));
     if (x > 0) __syncthreads();
     if (g == 0) {
       join_m[wave][n] = m[x];
       join_l[wave][n] = sum;
+      join_r[wave][n] = rounded;
     }
     __syncthreads();
     float most = join_m[0][n];
 #pragma unroll
     for (int w = 1; w < 4; ++w) most = fmaxf(most, join_m[w][n]);
-    float total = 0.f;
+    float total = 0.f, divisor = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) total += join_l[w][n] * exp2f(join_m[w][n] - most);
-    const float f = total == 0.f ? 0.f : exp2f(m[x] - most) / total;
+    for (int w = 0; w < 4; ++w) {
+      const float down = exp2f(join_m[w][n] - most);
+      total += join_l[w][n] * down;
+      divisor += join_r[w][n] * down;
+    }
+    const float f = divisor == 0.f ? 0.f : exp2f(m[x] - most) / divisor;
 #pragma unroll
     for (int v = 0; v < VC; ++v) *reinterpret_cast<floatx4*>(&join[wave][n][16 * v + 4 * g]) = o[x][v] * f;
     __syncthreads();
