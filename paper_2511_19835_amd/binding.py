@@ -317,6 +317,7 @@ class KVCache:
         # what every call needs of the record, at hand
         self.ref = ctypes.byref(self.desc)
         self.device = self.k_codes.device
+        self.dev = self.device.index
         self.batch, self.heads_kv, self.head_dim = self.desc.batch, self.desc.heads_kv, self.desc.head_dim
 
 
@@ -380,21 +381,39 @@ def make_rows(x: torch.Tensor) -> rsa_rows:
     return rows
 
 
-def _row_tensor(cache: KVCache, rows: rsa_rows, x: torch.Tensor) -> int:
-    """Address of a tensor that goes with a row record: bf16, of its sizes and strides, on the cache's device."""
-    shape = x.shape
-    if (x.dtype is not torch.bfloat16 or shape != rows.shape or shape[0] != cache.batch or shape[3] != cache.head_dim or x.device != cache.device
-            or x.stride() != rows.strides and any(n > 1 and p != q for n, p, q in zip(shape, x.stride(), rows.strides))):
-        raise ValueError(f"tensor {x.dtype} {tuple(shape)} strides {x.stride()} on {x.device} is not what the row record says")
-    return x.data_ptr()
+# (The checks of a call cost more than its launch where it is small: each asks a tensor as little as will do.)
+_I32, _I64, _BF16 = torch.int32, torch.int64, torch.bfloat16
 
 
-def _lengths(cache: KVCache, x: Optional[torch.Tensor]) -> Optional[int]:
-    if x is None:
-        return None
-    if x.dtype is not torch.int32 or x.numel() != cache.batch or not x.is_contiguous() or x.device != cache.device:
-        raise ValueError("expect contiguous int32 lengths, one for each sequence, on the cache's device")
-    return x.data_ptr()
+def _row_addresses(cache, rows: rsa_rows, *xs) -> list:
+    """Addresses of tensors that go with a row record: bf16, of its sizes and strides, on the device of the cache (or of the frequencies)."""
+    shape, strides, dev = rows.shape, rows.strides, cache.dev
+    out = []
+    for x in xs:
+        if (x.dtype is not _BF16 or x.shape != shape or x.get_device() != dev
+                or x.stride() != strides and any(n > 1 and p != q for n, p, q in zip(shape, x.stride(), strides))):
+            raise ValueError(f"tensor {x.dtype} {tuple(x.shape)} strides {x.stride()} on {x.device} is not what the row record says")
+        out.append(x.data_ptr())
+    return out
+
+
+def _cache_rows(cache: KVCache, rows: rsa_rows, *xs) -> list:
+    if rows.shape[0] != cache.batch or rows.shape[3] != cache.head_dim:
+        raise ValueError(f"rows {tuple(rows.shape)} are not those of {cache.batch} sequences with heads of {cache.head_dim}")
+    return _row_addresses(cache, rows, *xs)
+
+
+def _vectors(dev: int, n: int, *xs) -> list:
+    """Addresses of contiguous int32 tensors of n elements on device `dev`; None for None."""
+    out = []
+    for x in xs:
+        if x is None:
+            out.append(None)
+            continue
+        if x.dtype is not _I32 or x.numel() != n or x.get_device() != dev or not x.is_contiguous():
+            raise ValueError(f"expect {n} contiguous int32 numbers on cuda:{dev}, got {x.dtype} {tuple(x.shape)} on {x.device}")
+        out.append(x.data_ptr())
+    return out
 
 
 def _lists(cache: KVCache, rows: rsa_rows, group: int, block_idx: torch.Tensor, kept: torch.Tensor) -> None:
@@ -404,11 +423,10 @@ def _lists(cache: KVCache, rows: rsa_rows, group: int, block_idx: torch.Tensor, 
         raise ValueError(f"expect contiguous int32 lists {shape} + [list_len] and counts {shape} on the cache's device")
 
 
-def _launch(device: torch.device, stream, where: str, fn, *args) -> None:
+def _launch(dev: int, stream, where: str, fn, *args) -> None:
     """One call on a device: on `stream`, or on that device's current stream."""
-    dev = device.index
     raw = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
-    if torch.cuda.current_device() == dev:
+    if torch._C._cuda_getDevice() == dev:
         status = fn(*args, raw)
     else:
         with torch.cuda.device(dev):
@@ -417,11 +435,9 @@ def _launch(device: torch.device, stream, where: str, fn, *args) -> None:
         raise RsaError(status, where)
 
 
-def _call(cache: KVCache, stream, where: str, fn, *args, bits: int = 0) -> None:
-    """One call on the cache's device; `bits`: only caches of so many are taken."""
-    if bits and cache.bits != bits:
+def _of_bits(cache: KVCache, bits: int, where: str) -> None:
+    if cache.bits != bits:
         raise ValueError(f"{where} takes a cache of {bits} bits, not of {cache.bits}")
-    _launch(cache.device, stream, where, fn, cache.ref, *args)
 
 
 def _scratch(cache: KVCache, ws: Optional[torch.Tensor]):
@@ -446,29 +462,33 @@ def rsa_cache_workspace_bytes(cache: KVCache, rows: rsa_rows, group: int = 0):
 
 
 def rsa_cache_write(cache: KVCache, rows, K, V, start, count=None, stream=None):
-    _call(cache, stream, "rsa_cache_write", _lib().rsa_cache_write, rows.ref, _row_tensor(cache, rows, K), _row_tensor(cache, rows, V),
-          _lengths(cache, start), _lengths(cache, count), bits=8)
+    _of_bits(cache, 8, "rsa_cache_write")
+    _launch(cache.dev, stream, "rsa_cache_write", _lib().rsa_cache_write, cache.ref, rows.ref, *_cache_rows(cache, rows, K, V),
+            *_vectors(cache.dev, cache.batch, start, count))
 
 
 def rsa_cache_read(cache: KVCache, rows, start, count, K, V, stream=None):
-    _call(cache, stream, "rsa_cache_read", _lib().rsa_cache_read, rows.ref, _lengths(cache, start), _lengths(cache, count),
-          _row_tensor(cache, rows, K), _row_tensor(cache, rows, V), bits=8)
+    _of_bits(cache, 8, "rsa_cache_read")
+    _launch(cache.dev, stream, "rsa_cache_read", _lib().rsa_cache_read, cache.ref, rows.ref, *_vectors(cache.dev, cache.batch, start, count),
+            *_cache_rows(cache, rows, K, V))
 
 
 def rsa_cache_select(cache: KVCache, rows, Q, kv_len, q_len, group, keep, first, last, flags, block_idx, kept, ws=None, stream=None):
     _lists(cache, rows, group, block_idx, kept)
-    _call(cache, stream, "rsa_cache_select", _lib().rsa_cache_select, rows.ref, _row_tensor(cache, rows, Q), _lengths(cache, kv_len),
-          _lengths(cache, q_len), group, keep, first, last, flags, block_idx.data_ptr(), kept.data_ptr(), block_idx.shape[3], *_scratch(cache, ws))
+    _launch(cache.dev, stream, "rsa_cache_select", _lib().rsa_cache_select, cache.ref, rows.ref, *_cache_rows(cache, rows, Q),
+            *_vectors(cache.dev, cache.batch, kv_len, q_len), group, keep, first, last, flags, block_idx.data_ptr(), kept.data_ptr(),
+            block_idx.shape[3], *_scratch(cache, ws))
 
 
 def _attn_call(cache: KVCache, where: str, fn, bits: int, rows, Q, kv_len, q_len, scale, flags, block_idx, kept, group, O, lse, ws, stream):
-    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != rows.shape[:3] or not lse.is_contiguous() or lse.device != cache.device):
+    _of_bits(cache, bits, where)
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != rows.shape[:3] or lse.get_device() != cache.dev or not lse.is_contiguous()):
         raise ValueError("expect a contiguous fp32 lse [batch, heads, t] on the cache's device")
     if block_idx is not None and kept is not None:
         _lists(cache, rows, group, block_idx, kept)
-    _call(cache, stream, where, fn, rows.ref, _row_tensor(cache, rows, Q), _lengths(cache, kv_len),
-          _lengths(cache, q_len), scale, flags, _ptr(block_idx), _ptr(kept), group, block_idx.shape[3] if block_idx is not None else 0,
-          _row_tensor(cache, rows, O), _ptr(lse), *_scratch(cache, ws), bits=bits)
+    q, o = _cache_rows(cache, rows, Q, O)
+    _launch(cache.dev, stream, where, fn, cache.ref, rows.ref, q, *_vectors(cache.dev, cache.batch, kv_len, q_len), scale, flags, _ptr(block_idx),
+            _ptr(kept), group, block_idx.shape[3] if block_idx is not None else 0, o, lse.data_ptr() if lse is not None else None, *_scratch(cache, ws))
 
 
 def rsa_cache_attn(cache: KVCache, rows, Q, kv_len, q_len, scale, flags, block_idx, kept, group, O, lse=None, ws=None, stream=None):
@@ -488,13 +508,15 @@ def rsa_fourbit_workspace_bytes(cache: KVCache, rows: rsa_rows, group: int = 0):
 
 
 def rsa_fourbit_write(cache: KVCache, rows, K, V, start, count=None, stream=None):
-    _call(cache, stream, "rsa_fourbit_write", _lib().rsa_fourbit_write, rows.ref, _row_tensor(cache, rows, K), _row_tensor(cache, rows, V),
-          _lengths(cache, start), _lengths(cache, count), bits=4)
+    _of_bits(cache, 4, "rsa_fourbit_write")
+    _launch(cache.dev, stream, "rsa_fourbit_write", _lib().rsa_fourbit_write, cache.ref, rows.ref, *_cache_rows(cache, rows, K, V),
+            *_vectors(cache.dev, cache.batch, start, count))
 
 
 def rsa_fourbit_read(cache: KVCache, rows, start, count, K, V, stream=None):
-    _call(cache, stream, "rsa_fourbit_read", _lib().rsa_fourbit_read, rows.ref, _lengths(cache, start), _lengths(cache, count),
-          _row_tensor(cache, rows, K), _row_tensor(cache, rows, V), bits=4)
+    _of_bits(cache, 4, "rsa_fourbit_read")
+    _launch(cache.dev, stream, "rsa_fourbit_read", _lib().rsa_fourbit_read, cache.ref, rows.ref, *_vectors(cache.dev, cache.batch, start, count),
+            *_cache_rows(cache, rows, K, V))
 
 
 def rsa_fourbit_attn(cache: KVCache, rows, Q, kv_len, q_len, scale, flags, block_idx, kept, group, O, lse=None, ws=None, stream=None):
@@ -529,7 +551,7 @@ class Pages:
     free_pages: torch.Tensor   # int32 [pages]
 
     def __post_init__(self):
-        self.ref, self.device, self.batch = ctypes.byref(self.desc), self.table.device, self.desc.batch
+        self.ref, self.device, self.dev, self.batch = ctypes.byref(self.desc), self.table.device, self.table.device.index, self.desc.batch
 
 
 def pages_of(table: torch.Tensor, free_pages: torch.Tensor, block: int) -> Pages:
@@ -540,19 +562,17 @@ def pages_of(table: torch.Tensor, free_pages: torch.Tensor, block: int) -> Pages
     return Pages(rsa_pages(table.shape[0], table.shape[1], block, free_pages.shape[0], _ptr(table), _ptr(free_pages)), table, free_pages)
 
 
-def _ints(x: Optional[torch.Tensor], shape, device, dtype=torch.int32) -> Optional[int]:
-    if x is None:
-        return None
-    if x.dtype is not dtype or tuple(x.shape) != tuple(shape) or not x.is_contiguous() or x.device != device:
-        raise ValueError(f"expect a contiguous {dtype} tensor {tuple(shape)} on {device}, got {x.dtype} {tuple(x.shape)} on {x.device}")
-    return x.data_ptr()
-
-
 def rsa_cache_assign(pages: Pages, t, kv_len, add, free_count, kv_new, free_left, start, count, positions=None, slots=None, shared=None, stream=None):
-    b, dev = (pages.batch,), pages.device
-    _launch(dev, stream, "rsa_cache_assign", _lib().rsa_cache_assign, pages.ref, t, _ints(kv_len, b, dev), _ints(add, b, dev), _ints(shared, b, dev),
-            _ints(free_count, (1,), dev), _ints(kv_new, b, dev), _ints(free_left, (1,), dev), _ints(start, b, dev), _ints(count, b, dev),
-            _ints(positions, (pages.batch, t), dev), _ints(slots, (pages.batch, t), dev, torch.int64))
+    n, dev = pages.batch, pages.dev
+    kv, more, own, new, first, many = _vectors(dev, n, kv_len, add, shared, kv_new, start, count)
+    free, left = _vectors(dev, 1, free_count, free_left)
+    pos, = _vectors(dev, n * t, positions)
+    slot = None
+    if slots is not None:
+        if slots.dtype is not _I64 or slots.numel() != n * t or slots.get_device() != dev or not slots.is_contiguous():
+            raise ValueError(f"expect {n * t} contiguous int64 slots on cuda:{dev}, got {slots.dtype} {tuple(slots.shape)} on {slots.device}")
+        slot = slots.data_ptr()
+    _launch(dev, stream, "rsa_cache_assign", _lib().rsa_cache_assign, pages.ref, t, kv, more, own, free, new, left, first, many, pos, slot)
 
 
 @dataclass
@@ -562,11 +582,11 @@ class Rotary:
     freq: torch.Tensor         # fp64 [pairs], radians a position
 
     def __post_init__(self):
-        self.device, self.axes, self.refs = self.freq.device, self.desc.axes, {}
+        self.device, self.dev, self.axes, self.refs = self.freq.device, self.freq.device.index, self.desc.axes, {}
 
     def ref(self, head_dim: int):
         """The record for heads of `head_dim` channels."""
-        if head_dim not in self.refs:
+        if head_dim not in self.refs:          # (one for each size of heads)
             d = rsa_rotary.from_buffer_copy(self.desc)
             d.head_dim = head_dim
             self.refs[head_dim] = ctypes.byref(d)
@@ -594,24 +614,20 @@ def rsa_rotary_frequencies(pairs: int, base: float = 10000.0, scaling: int = RSA
     return list(freq), factor.value
 
 
-def _turned(rows: rsa_rows, batch: int, device, *tensors):
-    for x in tensors:
-        if (x.dtype is not torch.bfloat16 or x.shape != rows.shape or x.shape[0] != batch or x.device != device
-                or x.stride() != rows.strides and any(n > 1 and p != q for n, p, q in zip(x.shape, x.stride(), rows.strides))):
-            raise ValueError(f"tensor {x.dtype} {tuple(x.shape)} strides {x.stride()} on {x.device} is not what the row record says")
-    return (x.data_ptr() for x in tensors)
-
-
 def rsa_rotary_apply(rotary: Rotary, rows_q, Q, Qr, rows_k=None, K=None, Kr=None, positions=None, start=None, count=None, flags=0, stream=None):
-    b, t, d, dev = Q.shape[0], Q.shape[2], Q.shape[3], rotary.device
-    q, qr = _turned(rows_q, b, dev, Q, Qr)
-    k, kr = _turned(rows_k, b, dev, K, Kr) if rows_k is not None else (None, None)
-    if rows_k is not None and K.shape[3] != d:
-        raise ValueError(f"queries and keys have heads of the same size: got {d} and {K.shape[3]}")
-    if positions is not None and positions.dim() == 2:
-        positions = positions[None]
-    _launch(dev, stream, "rsa_rotary_apply", _lib().rsa_rotary_apply, rotary.ref(d), b, rows_q.ref, q, qr, rows_k.ref if rows_k is not None else None, k, kr,
-            _ints(positions, (rotary.axes, b, t), dev), _ints(start, (b,), dev), _ints(count, (b,), dev), flags)
+    b, _, t, d = rows_q.shape
+    dev = rotary.dev
+    q, qr = _row_addresses(rotary, rows_q, Q, Qr)
+    ref = k = kr = None
+    if rows_k is not None:
+        if rows_k.shape[0] != b or rows_k.shape[3] != d:
+            raise ValueError(f"queries and keys are of the same sequences and head sizes: got {tuple(rows_q.shape)} and {tuple(rows_k.shape)}")
+        ref, (k, kr) = rows_k.ref, _row_addresses(rotary, rows_k, K, Kr)
+    if positions is not None and tuple(positions.shape) != (rotary.axes, b, t) and (rotary.axes, *positions.shape) != (1, b, t):
+        raise ValueError(f"expect positions {(rotary.axes, b, t)}, got {tuple(positions.shape)}")
+    pos, = _vectors(dev, rotary.axes * b * t, positions)
+    first, many = _vectors(dev, b, start, count)
+    _launch(dev, stream, "rsa_rotary_apply", _lib().rsa_rotary_apply, rotary.ref(d), b, rows_q.ref, q, qr, ref, k, kr, pos, first, many, flags)
 
 
 def serve_step(cache: KVCache, pages: Pages, rotary: Rotary, Q, K, V, O, kv_len, add, free_count, start, count, positions=None, slots=None, shared=None,
