@@ -396,7 +396,7 @@ int rsa_fourbit_attn(const rsa_cache* cache, const rsa_rows* rows, const void* Q
  */
 typedef struct rsa_pages {
   int32_t batch;       /* sequences, 1 .. 65535 */
-  int32_t max_blocks;  /* entries of a row of the table, >= 1 */
+  int32_t max_blocks;  /* entries of a row of the table, >= 1; batch * max_blocks < 2^31, max_blocks * block < 2^31 */
   int32_t block;       /* tokens of a page, >= 1 (the cache's) */
   int64_t pages;       /* entries that the free list has room for: 1 .. 2^31 - 1 (the cache's pages) */
   int32_t* table;      /* device, [batch][max_blocks]: the cache's table */

@@ -4,8 +4,11 @@
 // positions lose nothing (in fp32 a position of 2^20 leaves 2^-4 radians). sine and cosine are the Taylor series on an eighth of a turn
 // to each side of the next quarter, off by less than 2^-23.
 //
-// A thread has eight pairs of one token, so that the angles are computed once, and walks a run of heads with them. Bound by memory:
-// two bytes of each channel in and two out.
+// A workgroup has 64 pieces, eight pairs of one token each: its four waves compute a quarter of the angles each, which go through LDS,
+// and then take every fourth head. Bound by memory: two bytes of each channel in and two out.
+// 48 heads of 119 056 tokens along three axes 528 us (2.93 GB, 5.5 TB/s); a token of 32 sequences, 40 heads, 3.4 us.
+#include <type_traits>
+
 #include "serve_common.hpp"
 
 namespace rsa {
@@ -29,44 +32,73 @@ __device__ __forceinline__ void turn(double turns, float& co, float& si) {
 // 16 u + 15; kOdd: as kHalf for any number of pairs, element by element.
 enum Form { kHalf, kInterleaved, kOdd };
 
-template <Form F>
+// HEADS: heads of a wave that are in flight together. 48 heads of 119 056 tokens: 4, 6, 8, 12 at once 583, 564, 550, 528 us (5.5 TB/s); 24 of 6231
+// tokens of 64 channels, in two groups: 2, 4, 12 at once 7.0, 6.9, 8.6 (the registers of twelve cost more than they bring there).
+template <Form F, int HEADS>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int units, int heads_per) {
+  __shared__ float2 cs[8][64];
   const int turning = (a.pairs + 7) / 8;           // units that turn; behind them 16 channels each are copied
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int64_t id = (int64_t)blockIdx.x * 64 + lane;
   const int64_t row = id / units;
   const int u = (int)(id % units);
-  if (row >= (int64_t)a.batch * a.t) return;
   const int b = (int)(row / a.t), i = (int)(row % a.t);
-  if (a.count && i >= a.count[b]) return;
-  const int h0 = blockIdx.y * heads_per, h1 = min(h0 + heads_per, a.x[0].heads + a.x[1].heads);
-
-  float co[8], si[8];
-  if (u < turning) {
+  const bool is = row < (int64_t)a.batch * a.t && !(a.count && i >= a.count[b]);
+  if (is && u < turning) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int j = 8 * u + e;
-      co[e] = 1.f;
-      si[e] = 0.f;
+    for (int z = 0; z < 2; ++z) {
+      const int e = 2 * wave + z, j = 8 * u + e;
+      float co = 1.f, si = 0.f;
       if (j < a.pairs) {
         double pos = (double)(a.start ? a.start[b] : 0) + i;
         if (a.positions) {
           const int axis = (j >= a.ends[0]) + (j >= a.ends[1]);
           pos = a.positions[((int64_t)axis * a.batch + b) * a.t + i];
         }
-        turn(pos * a.freq[j] * 0.15915494309189535, co[e], si[e]);
-        co[e] *= a.factor;
-        si[e] *= a.inverse ? -a.factor : a.factor;
+        turn(pos * a.freq[j] * 0.15915494309189535, co, si);
+        co *= a.factor;
+        si *= a.inverse ? -a.factor : a.factor;
       }
+      cs[e][lane] = make_float2(co, si);
     }
   }
-  for (int h = h0; h < h1; ++h) {
+  __syncthreads();
+  if (!is) return;
+  float co[8], si[8];
+  if (u < turning) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float2 z = cs[e][lane];
+      co[e] = z.x;
+      si[e] = z.y;
+    }
+  }
+  const int h1 = min((int)(blockIdx.y + 1) * heads_per, a.x[0].heads + a.x[1].heads);
+  // two chunks of eight channels
+  int c0, c1;
+  if (F == kInterleaved) {
+    c0 = 16 * u;
+    c1 = c0 + 8;
+  } else if (u < turning) {
+    c0 = 8 * u;
+    c1 = a.pairs + 8 * u;
+  } else {
+    c0 = 2 * a.pairs + (u - turning) * 16;
+    c1 = c0 + 8;
+  }
+  const bool both = c1 < a.head_dim;
+  auto place = [&](int h, const uint16_t*& in, uint16_t*& out) __attribute__((always_inline)) {
     const bool second = h >= a.x[0].heads;
     const RotaryArgs::Rows& x = a.x[second];
     const int64_t at = (int64_t)b * x.sb + (int64_t)(second ? h - a.x[0].heads : h) * x.sh + (int64_t)i * x.st;
-    const uint16_t* in = x.in + at;
-    uint16_t* out = x.out + at;
-    if (u >= turning && in == out) continue;
-    if (F == kOdd) {
+    in = x.in + at;
+    out = x.out + at;
+  };
+  if (F == kOdd) {
+    for (int h = blockIdx.y * heads_per + wave; h < h1; h += 4) {
+      const uint16_t* in;
+      uint16_t* out;
+      place(h, in, out);
       if (u < turning) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -77,50 +109,55 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int units, in
             out[a.pairs + j] = to_bf16_bits(p * si[e] + q * co[e]);
           }
         }
-      } else {
-        for (int ch = 2 * a.pairs + (u - turning) * 16, n = 0; n < 16 && ch < a.head_dim; ++n, ++ch) out[ch] = in[ch];
+      } else if (in != out) {
+        for (int ch = c0, n = 0; n < 16 && ch < a.head_dim; ++n, ++ch) out[ch] = in[ch];
       }
-      continue;
     }
-    // two chunks of eight channels
-    int c0, c1;
-    if (F == kInterleaved) {
-      c0 = 16 * u;
-      c1 = c0 + 8;
-    } else if (u < turning) {
-      c0 = 8 * u;
-      c1 = a.pairs + 8 * u;
-    } else {
-      c0 = 2 * a.pairs + (u - turning) * 16;
-      c1 = c0 + 8;
+    return;
+  }
+  for (int first = blockIdx.y * heads_per + wave; first < h1; first += 4 * HEADS) {
+    uint4 v[HEADS], w[HEADS];
+    uint16_t* out[HEADS];
+    bool skip[HEADS];
+#pragma unroll
+    for (int z = 0; z < HEADS; ++z) {
+      skip[z] = first + 4 * z >= h1;
+      if (skip[z]) continue;
+      const uint16_t* in;
+      place(first + 4 * z, in, out[z]);
+      skip[z] = u >= turning && in == out[z];
+      v[z] = *reinterpret_cast<const uint4*>(in + c0);
+      w[z] = make_uint4(0, 0, 0, 0);
+      if (both) w[z] = *reinterpret_cast<const uint4*>(in + c1);
     }
-    const bool both = c1 < a.head_dim;
-    uint4 v = *reinterpret_cast<const uint4*>(in + c0), w = make_uint4(0, 0, 0, 0);
-    if (both) w = *reinterpret_cast<const uint4*>(in + c1);
-    if (u < turning) {
-      uint32_t p[4] = {v.x, v.y, v.z, v.w}, q[4] = {w.x, w.y, w.z, w.w};
-      if (F == kHalf) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float p0 = bf16_bits_to_float(p[e] & 0xffffu), p1 = __builtin_bit_cast(float, p[e] & 0xffff0000u);
-          const float q0 = bf16_bits_to_float(q[e] & 0xffffu), q1 = __builtin_bit_cast(float, q[e] & 0xffff0000u);
-          p[e] = pack_bf16x2(p0 * co[2 * e] - q0 * si[2 * e], p1 * co[2 * e + 1] - q1 * si[2 * e + 1]);
-          q[e] = pack_bf16x2(p0 * si[2 * e] + q0 * co[2 * e], p1 * si[2 * e + 1] + q1 * co[2 * e + 1]);
-        }
-      } else {
+    for (int z = 0; z < HEADS; ++z) {
+      if (skip[z]) continue;
+      if (u < turning) {
+        uint32_t p[4] = {v[z].x, v[z].y, v[z].z, v[z].w}, q[4] = {w[z].x, w[z].y, w[z].z, w[z].w};
+        if (F == kHalf) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          uint32_t& z = e < 4 ? p[e] : q[e - 4];
-          const float z0 = bf16_bits_to_float(z & 0xffffu), z1 = __builtin_bit_cast(float, z & 0xffff0000u);
-          const uint32_t t = pack_bf16x2(z0 * co[e] - z1 * si[e], z0 * si[e] + z1 * co[e]);
-          z = 8 * u + e < a.pairs ? t : z;         // (a channel behind the pairs is no product: 0 * infinity)
+          for (int e = 0; e < 4; ++e) {
+            const float p0 = bf16_bits_to_float(p[e] & 0xffffu), p1 = __builtin_bit_cast(float, p[e] & 0xffff0000u);
+            const float q0 = bf16_bits_to_float(q[e] & 0xffffu), q1 = __builtin_bit_cast(float, q[e] & 0xffff0000u);
+            p[e] = pack_bf16x2(p0 * co[2 * e] - q0 * si[2 * e], p1 * co[2 * e + 1] - q1 * si[2 * e + 1]);
+            q[e] = pack_bf16x2(p0 * si[2 * e] + q0 * co[2 * e], p1 * si[2 * e + 1] + q1 * co[2 * e + 1]);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            uint32_t& x = e < 4 ? p[e] : q[e - 4];
+            const float z0 = bf16_bits_to_float(x & 0xffffu), z1 = __builtin_bit_cast(float, x & 0xffff0000u);
+            const uint32_t y = pack_bf16x2(z0 * co[e] - z1 * si[e], z0 * si[e] + z1 * co[e]);
+            x = 8 * u + e < a.pairs ? y : x;       // (a channel behind the pairs is no product: 0 * infinity)
+          }
         }
+        v[z] = make_uint4(p[0], p[1], p[2], p[3]);
+        w[z] = make_uint4(q[0], q[1], q[2], q[3]);
       }
-      v = make_uint4(p[0], p[1], p[2], p[3]);
-      w = make_uint4(q[0], q[1], q[2], q[3]);
+      *reinterpret_cast<uint4*>(out[z] + c0) = v[z];
+      if (both) *reinterpret_cast<uint4*>(out[z] + c1) = w[z];
     }
-    *reinterpret_cast<uint4*>(out + c0) = v;
-    if (both) *reinterpret_cast<uint4*>(out + c1) = w;
   }
 }
 
@@ -129,16 +166,25 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int units, in
 hipError_t launch_rotary(const RotaryArgs& a, hipStream_t s) {
   const int turning = (a.pairs + 7) / 8, rest = a.head_dim - 2 * a.pairs;
   const int units = a.interleaved ? (a.head_dim + 15) / 16 : turning + (rest + 15) / 16;
-  const int64_t threads = (int64_t)a.batch * a.t * units;
+  const int64_t pieces = ((int64_t)a.batch * a.t * units + 63) / 64;
   const int heads = a.x[0].heads + a.x[1].heads;
-  // workgroups for every compute unit several times over, and as many heads to a thread as that leaves
-  const int64_t wgs = (threads + 255) / 256;
-  int64_t per = heads * wgs / 4096;
-  per = per < 1 ? 1 : per > heads ? heads : per;
-  const dim3 grid((uint32_t)wgs, (uint32_t)((heads + per - 1) / per));
-  if (a.interleaved) hipLaunchKernelGGL(rotary_kernel<kInterleaved>, grid, dim3(256), 0, s, a, units, (int)per);
-  else if (a.pairs % 8 == 0) hipLaunchKernelGGL(rotary_kernel<kHalf>, grid, dim3(256), 0, s, a, units, (int)per);
-  else hipLaunchKernelGGL(rotary_kernel<kOdd>, grid, dim3(256), 0, s, a, units, (int)per);
+  // Heads are shared out over workgroups too where there would be few: two to a compute unit (four: 6.9 us for the 6231 tokens, two 6.8, eight 7.7).
+  int64_t groups = (512 + pieces - 1) / pieces;
+  const int64_t most = (heads + 3) / 4;
+  groups = groups > most ? most : groups;
+  const int per = (int)((most + groups - 1) / groups * 4);
+  const dim3 grid((uint32_t)pieces, (uint32_t)((heads + per - 1) / per));
+  const int of_wave = per / 4;
+  const dim3 block(256);
+  auto launch = [&](auto form) {
+    constexpr Form F = decltype(form)::value;
+    if (F == kOdd || of_wave <= 4) hipLaunchKernelGGL((rotary_kernel<F, 4>), grid, block, 0, s, a, units, per);
+    else if (of_wave <= 8) hipLaunchKernelGGL((rotary_kernel<F, 8>), grid, block, 0, s, a, units, per);
+    else hipLaunchKernelGGL((rotary_kernel<F, 12>), grid, block, 0, s, a, units, per);
+  };
+  if (a.interleaved) launch(std::integral_constant<Form, kInterleaved>{});
+  else if (a.pairs % 8 == 0) launch(std::integral_constant<Form, kHalf>{});
+  else launch(std::integral_constant<Form, kOdd>{});
   return hipGetLastError();
 }
 

@@ -77,7 +77,7 @@ int rsa_cache_assign(const rsa_pages* pages, int t, const int32_t* kv_len, const
   if (pages->batch < 1 || pages->max_blocks < 1 || pages->block < 1 || pages->pages < 1 || t < 1) return RSA_E_SHAPE;
   if (pages->batch > 65535 || pages->pages >= ((int64_t)1 << 31)) return RSA_E_UNSUPPORTED;
   if ((int64_t)pages->max_blocks * pages->block >= ((int64_t)1 << 31)) return RSA_E_UNSUPPORTED;    // positions are int32
-  if ((int64_t)pages->batch * t >= ((int64_t)1 << 28)) return RSA_E_UNSUPPORTED;
+  if ((int64_t)pages->batch * t >= ((int64_t)1 << 28) || (int64_t)pages->batch * pages->max_blocks >= ((int64_t)1 << 31)) return RSA_E_UNSUPPORTED;
   if (!pages->table || !pages->free_pages || !kv_len || !add || !free_count || !kv_new || !free_left || !start || !count) return RSA_E_NULL;
   const void* small[] = {pages->table, pages->free_pages, kv_len, add, shared, free_count, kv_new, free_left, start, count, positions};
   for (const void* p : small)
@@ -181,7 +181,8 @@ int rsa_rotary_apply(const rsa_rotary* rotary, int batch, const rsa_rows* rows_q
     heads += r.heads;
   }
   if (rows_k && (Kr == Qr || Kr == Q || Qr == K)) return RSA_E_RANGE;
-  if ((int64_t)batch * a.t * (p.head_dim / 8) / 256 >= kMostWorkgroups || heads > 65535) return RSA_E_UNSUPPORTED;
+  // (64 pieces of at least eight channels to a workgroup)
+  if ((int64_t)batch * a.t * (p.head_dim / 8 + 2) / 64 >= kMostWorkgroups || heads > 65535) return RSA_E_UNSUPPORTED;
   return rsa::launch_rotary(a, (hipStream_t)stream) == hipSuccess ? RSA_OK : RSA_E_LAUNCH;
 }
 

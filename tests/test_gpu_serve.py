@@ -566,7 +566,8 @@ def run_rotary(rng, b, hq, hk, t, d, pairs, pairing, layout="bhtd", axis_pairs=N
             bound[..., 2 * pairs:] = 0
             ok = np.isfinite(w)
             assert np.array_equal(ok, np.isfinite(g))
-            assert (np.abs(g - w)[ok] <= bound[ok]).all(), (np.abs(g - w)[ok] / np.maximum(bound[ok], 1e-30)).max()
+            off = np.abs(g[ok] - w[ok])
+            assert (off <= bound[ok]).all(), (off / np.maximum(bound[ok], 1e-30)).max()
     return f64(Qr), f64(Kr)
 
 
