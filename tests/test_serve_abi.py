@@ -189,7 +189,7 @@ def test_bad_pages_are_refused(lib):
     assert lib.rsa_cache_assign(None, 1, *[ONE] * 10, None) == -1
     for kw in (dict(batch=0), dict(max_blocks=0), dict(block=0), dict(pages=0), dict(t=0)):
         assert call(**kw) == -2, kw
-    for kw in (dict(batch=65536), dict(pages=1 << 31), dict(max_blocks=1 << 26, block=64), dict(t=1 << 27), dict(batch=65535, t=1 << 13), dict(batch=65535, max_blocks=1 << 15, block=1)):
+    for kw in (dict(batch=65536), dict(pages=1 << 31), dict(max_blocks=1 << 26, block=64), dict(t=1 << 27), dict(batch=65535, t=1 << 13), dict(batch=65535, max_blocks=1 << 16, block=1)):
         assert call(**kw) == -3, kw
     for kw in (dict(table=None), dict(free_pages=None), dict(kv=None), dict(add=None), dict(fc=None), dict(new=None), dict(left=None), dict(start=None), dict(count=None)):
         assert call(**kw) == -1, kw
