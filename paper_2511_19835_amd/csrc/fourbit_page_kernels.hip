@@ -121,8 +121,9 @@ __global__ __launch_bounds__(256) void fourbit_write_kernel(CacheDims c, RowDims
   __shared__ __align__(16) uint16_t img_vs[SPB][64];
   __shared__ double sums[4][D];
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-  const int j = blockIdx.x % blocks, bh = blockIdx.x / blocks;
-  const int b = bh / c.heads_kv, h = bh % c.heads_kv;
+  // (the heads of a block follow one another: their rows are neighbours in [token, head] order, their pages in memory)
+  const int h = blockIdx.x % c.heads_kv, bj = blockIdx.x / c.heads_kv;
+  const int b = bj / blocks, j = bj % blocks;
   BlockSpan sp;
   if (!touched_block<BLK>(c, r.t, a.start, a.count, b, j, &sp)) return;   // the whole workgroup
 
