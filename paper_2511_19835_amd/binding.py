@@ -636,10 +636,24 @@ def serve_step(cache: KVCache, pages: Pages, rotary: Rotary, Q, K, V, O, kv_len,
     tokens (rows 0 .. add[b] - 1 of Q, K and V; less than 0: it is cut). Pages for them (rsa_cache_assign; kv_len and free_count move on in place,
     start and count say what was served), Q and K turned in place by their positions, keys and values into the cache, and the causal
     attention of the new queries over their sequences. Rows of sequences that were not served are left as they were."""
-    if pages.table.data_ptr() != cache.table.data_ptr():
+    # (all of it before the first call: that one moves the lengths on)
+    if pages.table.data_ptr() != cache.table.data_ptr() or pages.desc.block != cache.desc.block or pages.batch != cache.batch:
         raise ValueError("the pages are not those of the cache's table")
+    if K.shape[2] != Q.shape[2] or rotary.dev != cache.dev:
+        raise ValueError(f"a step brings keys and queries for the same rows, on one device: got {K.shape[2]} and {Q.shape[2]} rows")
     rows, rows_kv = make_rows(Q), make_rows(K)
+    _cache_rows(cache, rows, Q, O)
+    _cache_rows(cache, rows_kv, K, V)
+    if K.shape[1] != cache.heads_kv or Q.shape[1] % cache.heads_kv or 2 * rotary.desc.pairs > cache.head_dim:
+        raise ValueError(f"{Q.shape[1]} and {K.shape[1]} heads of {cache.head_dim} channels, {rotary.desc.pairs} pairs: not for a cache of {cache.heads_kv} heads")
+    if rotary.axes != 1:
+        raise ValueError("a step's tokens stand in a row: positions along one axis")
     write, attn = (rsa_fourbit_write, rsa_fourbit_attn) if cache.bits == 4 else (rsa_cache_write, rsa_cache_attn)
+    need = rsa_fourbit_workspace_bytes(cache, rows) if cache.bits == 4 else rsa_cache_workspace_bytes(cache, rows)[1]
+    if ws is not None and _scratch(cache, ws)[1] < need:
+        raise ValueError(f"the attention's workspace has {need} bytes")
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != rows.shape[:3] or lse.get_device() != cache.dev or not lse.is_contiguous()):
+        raise ValueError("expect a contiguous fp32 lse [batch, heads, t] on the cache's device")
     rsa_cache_assign(pages, Q.shape[2], kv_len, add, free_count, kv_len, free_count, start, count, positions, slots, shared, stream)
     rsa_rotary_apply(rotary, rows, Q, Q, rows_kv, K, K, None, start, count, 0, stream)
     write(cache, rows_kv, K, V, start, count, stream)

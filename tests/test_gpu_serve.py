@@ -435,6 +435,44 @@ def test_offsets_past_32_bits():
         assert torch.equal(O[0], O[1]) and O.abs().max() > 0
 
 
+@pytest.mark.parametrize("d,block,G,t", [(64, 64, 1, 1), (128, 128, 2, 2)])
+def test_more_short_sequences_than_compute_units(d, block, G, t):
+    """300 tiles of one launch: four waves to each, where fewer tiles have eight."""
+    p = Pair(60, 5, d, block, 5, table=np.random.default_rng(1).integers(0, 9, size=(60, 5)), pages=9)
+    one = Pair(1, 5, d, block, 9, 3, np.arange(9).reshape(1, 9), 9)
+    one.gpu = rb.fourbit_of(p.gpu.k_codes, p.gpu.v_codes, p.gpu.scales, p.gpu.k_mean, one.gpu.table, block)
+    one.fill([9 * block], spread=0.5)
+    p.ref.held = one.ref.held
+    lens = [int(n) for n in p.rng.integers(0, 5 * block + 1, size=60)]
+    Q = video_like(p.rng, 60, 5 * G, t, d)
+    compare(*attend(p, Q, lens, [min(t, n) for n in lens], causal=True), d)
+
+
+def test_rows_past_32_bits():
+    """Heads 2^32 elements apart: what is written, read, attended and turned there is what it is in a small tensor."""
+    if torch.cuda.mem_get_info()[0] < 120 << 30:
+        pytest.skip("needs 100 GB")
+    t, d, far = 70, 64, (1 << 32) + 64
+    rng = np.random.default_rng(0)
+    big = [torch.empty(far + t * d, dtype=torch.bfloat16, device=DEV).as_strided((1, 2, t, d), (8, far, d, 1)) for _ in range(5)]
+    small = [bf16(rng.normal(size=(1, 2, t, d))) for _ in range(3)]
+    for x, y in zip(big, small):
+        x.copy_(y)
+    outs = []
+    for K, V, Q, R, S in ((*big,), (*small, torch.zeros_like(small[0]), torch.zeros_like(small[0]))):
+        p = Pair(1, 2, d, 64, 2)
+        rows = rb.make_rows(K)
+        rb.rsa_fourbit_write(p.gpu, rows, K, V, i32([0]))
+        rb.rsa_fourbit_read(p.gpu, rows, i32([0]), None, R, S)
+        kept = R.clone(memory_format=torch.contiguous_format), S.clone(memory_format=torch.contiguous_format)
+        rb.rsa_fourbit_attn(p.gpu, rows, Q, i32([t]), None, 0.0, rb.RSA_CACHE_CAUSAL, None, None, 0, R)
+        rot = rb.make_rotary(torch.full((32,), 0.1, dtype=torch.float64, device=DEV))
+        rb.rsa_rotary_apply(rot, rows, Q, S)
+        outs.append([*kept, R.clone(memory_format=torch.contiguous_format), S.clone(memory_format=torch.contiguous_format)])
+    for x, y in zip(*outs):
+        assert torch.equal(x, y) and x.abs().max() > 0
+
+
 def test_prompts_of_many_tiles():
     """More workgroups than the chip takes at once, the last tokens first: against rows taken one at a time by the other kernel."""
     p = Pair(1, 8, 64, 64, 64)
@@ -750,3 +788,18 @@ def test_binding_refusals():
         rb.rsa_cache_assign(rec, 1, z, z.clone(), one, z, one, z, z.clone())        # start over the lengths
     with pytest.raises(ValueError, match="table"):
         rb.serve_step(four, rec, rot, x, x, x, x, z, z, one, z, z)
+    # nothing of a step that is refused has happened
+    rec = rb.pages_of(four.table, torch.arange(4, dtype=torch.int32, device=DEV), 64)
+    half = rb.make_rotary(torch.ones(32, dtype=torch.float64, device=DEV))
+    good = dict(cache=four, pages=rec, rotary=half, Q=x, K=x.clone(), V=x.clone(), O=x.clone(), kv_len=i32([0, 0]), add=i32([3, 3]), free_count=i32([4]), start=i32([0, 0]),
+                count=i32([0, 0]))
+    wide = torch.zeros(2, 2, 3, 128, dtype=torch.bfloat16, device=DEV)
+    for bad in (dict(K=x[:, :, :2].contiguous(), V=x[:, :, :2].contiguous()), dict(O=x[:, :, :2]), dict(V=x[:, :1]), dict(Q=wide, O=wide), dict(K=x[:, :1].contiguous(), V=x[:, :1].contiguous()),
+                dict(lse=torch.zeros(2, 2, 2, device=DEV)), dict(rotary=rb.make_rotary(torch.ones(33, dtype=torch.float64, device=DEV))),
+                dict(rotary=rb.make_rotary(torch.ones(32, dtype=torch.float64, device=DEV), axis_pairs=[16, 16])),
+                dict(pages=rb.pages_of(four.table, torch.arange(4, dtype=torch.int32, device=DEV), 128))):
+        with pytest.raises(ValueError):
+            rb.serve_step(**{**good, **bad})
+    assert int(good["free_count"]) == 4 and good["kv_len"].tolist() == [0, 0] and (four.table == -1).all()
+    rb.serve_step(**good)
+    assert int(good["free_count"]) == 2 and good["kv_len"].tolist() == [3, 3]
