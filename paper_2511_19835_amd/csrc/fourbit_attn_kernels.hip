@@ -329,9 +329,11 @@ __device__ __forceinline__ bf16x2 scaled2(float a, float b, uint32_t less) {
 
 // The same for many query rows. 64 QT rows to a workgroup, 16 QT to a wave: every wave needs all codes, so they are widened once for
 // the workgroup, a quarter by each wave, into LDS in the order of the operands. Two buffers, one barrier a step of 64 keys.
+// Three workgroups to a compute unit at d = 64, two at d = 128. us with two and
+// three: 128 rows of 16 x 8 heads on 8192 keys 63, 58; 1000 rows 343, 310; 1000 rows of 12 heads on 30 000 keys 137, 124.
 constexpr int kAhead = 256;                        // steps that are looked up together
 template <int D, int BLK, int QT>
-__global__ __launch_bounds__(256, 2) void fourbit_tile_kernel(CacheDims c, RowDims r, CacheAttnArgs a, TileGrid tg) {
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void fourbit_tile_kernel(CacheDims c, RowDims r, CacheAttnArgs a, TileGrid tg) {
   constexpr int KM = D / 32, VC = D / 16, VW = VC / 4;   // VW: channel tiles that a wave widens
   constexpr int SPB = BLK / 64;
   constexpr int KR = fourbit_k_record(D), VR = fourbit_v_record(D);
