@@ -7,9 +7,9 @@
 // with the softmax between them lane-local. A code times its key's scale is exact in bf16, so the scores are those of the stored
 // keys, summed in fp32; a value's code is widened alone, and its token's scale goes into P.
 //
-// P times that scale is rounded to bf16: half a step is 2^-8 of it, whatever the scales of the tokens are to each other, so no
-// running scale of the outputs is needed. The sum of the weights is taken before that rounding, in fp32. The running reference m of
-// a row follows its maximum lazily (only when a score passes it by more than 8 in log2), so p <= 2^8.
+// P in bf16: half a step is 2^-8 of a weight, and a scale only moves its exponent, whatever the scales of the tokens are to each other, so no
+// running scale of the outputs is needed. The log-sum-exp takes the weights as they are in fp32. The running reference m of a row is moved
+// only when the weights of a step have become large beside it, so most steps take no maximum.
 #include "fourbit_common.hpp"
 
 #include "cache_attn_common.hpp"
@@ -41,6 +41,85 @@ __device__ __forceinline__ void value_scales(const uint4 (&w)[2], float (&s)[4][
     s[t][2] = bf16_bits_to_float(hi & 0xffffu);
     s[t][3] = __builtin_bit_cast(float, hi & 0xffff0000u);
   }
+}
+
+// Weights are made 2^kBias too large, as large as a sum over 2^31 keys allows, so that a token's scale comes in by a subtraction of exponents
+// (16 bits, two at once; below 0 it stays 0): bits of the scale taken from those of 2^kBias say by how much. Scales above 2^kBias and NaN
+// go the long way.
+constexpr float kBias = 90.f;
+constexpr uint32_t kMostScale = 0x6c806c80u;     // 2^90 in bf16, twice
+typedef uint16_t ushortx2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t less_than_most(uint32_t w) {      // (its own inverse)
+  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(ushortx2, kMostScale) - __builtin_bit_cast(ushortx2, w));
+}
+__device__ __forceinline__ bf16x2 scaled2(uint32_t w, uint32_t less) {
+  return __builtin_bit_cast(bf16x2, __builtin_elementwise_sub_sat(__builtin_bit_cast(ushortx2, w), __builtin_bit_cast(ushortx2, less)));
+}
+
+// Weights of a lane's 16 scores of a row (times `ks`), 2^kBias too large, over the reference: their sum, the weights in bf16, and P, in which their
+// tokens' scales are taken in. -> whether the reference has to follow: it is moved only when the sum is more than 2^8 (bf16 and fp32 have the
+// range), so that no maximum is taken otherwise; then they are made once more, over the new one at most 2^1.25.
+__device__ __forceinline__ bool weigh_row(const floatx4 (&s)[4], float ks, float m, const uint4 (&less)[2], float& sum, bf16x8 (&u)[2], bf16x8 (&p)[2]) {
+  const float ref = m - kBias;
+  sum = 0.f;
+#pragma unroll
+  for (int y = 0; y < 4; ++y) {
+    float w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      w[e] = __builtin_amdgcn_exp2f(fmaf(s[y][e], ks, -ref));
+      sum += w[e];
+    }
+    const uint32_t d0 = y % 2 ? less[y / 2].z : less[y / 2].x, d1 = y % 2 ? less[y / 2].w : less[y / 2].y;
+    const uint32_t u0 = pack_bf16x2(w[0], w[1]), u1 = pack_bf16x2(w[2], w[3]);
+    const bf16x2 a = __builtin_bit_cast(bf16x2, u0), b = __builtin_bit_cast(bf16x2, u1), lo = scaled2(u0, d0), hi = scaled2(u1, d1);
+    const int at = y % 2 * 4;
+    u[y / 2][at] = a[0]; u[y / 2][at + 1] = a[1]; u[y / 2][at + 2] = b[0]; u[y / 2][at + 3] = b[1];
+    p[y / 2][at] = lo[0]; p[y / 2][at + 1] = lo[1]; p[y / 2][at + 2] = hi[0]; p[y / 2][at + 3] = hi[1];
+  }
+  asm volatile("" : "+v"(p[0]), "+v"(p[1]));       // (made here, not behind the branches)
+  return sum > 0x1p98f;
+}
+// The reference goes up to the row's largest score, where that is larger -> what is to be taken of what was summed over the old one. The same in
+// the four lanes of a column; whole, so that what is taken from it stays exact.
+__device__ __forceinline__ float move_row(const floatx4 (&s)[4], float ks, float& m) {
+  float mx = -INFINITY;
+#pragma unroll
+  for (int y = 0; y < 4; ++y)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[y][e]);
+  mx = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, mx), MaxF32()), MaxF32())) * ks;
+  const float to = mx > m ? floorf(mx) : m;
+  const float down = __builtin_amdgcn_exp2f(m - to);
+  m = to;
+  return down;
+}
+// Far from zero a multiply-add would leave a product's own rounding, which may be 2^8 and more, and the reference has no bits for kBias:
+// there it follows each step's largest score, and the scores become rounded products less the reference.
+__device__ __forceinline__ void from_reference(floatx4 (&s)[4], float ks, float m) {
+#pragma clang fp contract(off)
+#pragma unroll
+  for (int y = 0; y < 4; ++y)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float product = s[y][e] * ks;
+      s[y][e] = product - m;
+    }
+}
+// P of tokens with a scale above 2^kBias or NaN, by products; no NaN of a token that the row does not see into 0 * NaN.
+__device__ __forceinline__ void odd_row(const floatx4 (&s)[4], float ks, float m, const uint4 (&less)[2], bf16x8 (&p)[2]) {
+  uint4 w[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) w[x] = make_uint4(less_than_most(less[x].x), less_than_most(less[x].y), less_than_most(less[x].z), less_than_most(less[x].w));
+  float vs[4][4];
+  value_scales(w, vs);
+#pragma unroll
+  for (int y = 0; y < 4; ++y)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float z = __builtin_amdgcn_exp2f(fmaf(s[y][e], ks, -m)) * vs[y][e];
+      p[y / 2][y % 2 * 4 + e] = (__bf16)(s[y][e] == -INFINITY ? 0.f : z);
+    }
 }
 
 // What a lane loads for a step of 64 keys.
@@ -84,7 +163,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void fourbit_attn_kernel(
     }
   }
   floatx4 o[QT][VC];
-  float m[QT], l[QT], lr[QT], lazy = kLazy;         // sums of the weights, and of what they are in P
+  float m[QT], l[QT], lr[QT];                       // reference, sums of the weights and of what they are in P
+  bool far = false;                                // a reference is 2^23 and more
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
     m[x] = kNoReference;
@@ -92,6 +172,11 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void fourbit_attn_kernel(
 #pragma unroll
     for (int v = 0; v < VC; ++v) o[x][v] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
+
+  const float all_ks = fmaxf(a.scale_log2e, 0x1p-149f);      // (above 0, so that a masked score stays -inf)
+  bf16x8 ones;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.f;
 
   const int u0 = (int)((int64_t)t.units * split / tg.splits), u1 = (int)((int64_t)t.units * (split + 1) / tg.splits);
   const int steps = (u1 - u0) * SPB;
@@ -149,70 +234,68 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void fourbit_attn_kernel(
         }
       }
       if (SETS == 1) load_k(z, again);
-      // scores; keys that a row does not see leave its softmax
-      const bool partly = key0 + 64 > t.lo_seen;
-      bool over = false;
-#pragma unroll
-      for (int x = 0; x < QT; ++x) {
-        const int left = seen[x] - key0;             // of the 64
-#pragma unroll
-        for (int y = 0; y < 4; ++y)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float w = s[x][y][e] * a.scale_log2e;
-            if (partly) w = 16 * y + 4 * g + e < left ? w : -INFINITY;
-            s[x][y][e] = w;
-            over |= w > m[x] + lazy;
-          }
-      }
-      if (__any(over)) {
+      if (key0 + 64 > t.lo_seen) {                 // keys that a row does not see leave its softmax
+        asm volatile("");                          // (a branch, no selects)
 #pragma unroll
         for (int x = 0; x < QT; ++x) {
-          float mx = kNoReference;
+          const int left = seen[x] - key0;         // of the 64
 #pragma unroll
           for (int y = 0; y < 4; ++y)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[x][y][e]);
-          mx = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, mx), MaxF32()), MaxF32()));
-          if (mx > m[x] + lazy) {                  // the same in the four lanes of a column
-            mx = floorf(mx);                       // (whole, so that what is taken from it and what it rescales stays exact)
-            const float down = exp2f(m[x] - mx);
-            m[x] = mx;
-            l[x] *= down;
-            lr[x] *= down;
-#pragma unroll
-            for (int v = 0; v < VC; ++v) o[x][v] *= down;
-          }
+            for (int e = 0; e < 4; ++e) s[x][y][e] = 16 * y + 4 * g + e < left ? s[x][y][e] : -INFINITY;
         }
-        if (far_from_zero<QT>(m)) lazy = 0.f;
       }
-      float vs[4][4];
-      value_scales(z.vs, vs);
+      uint4 less[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) less[x] = make_uint4(less_than_most(z.vs[x].x), less_than_most(z.vs[x].y), less_than_most(z.vs[x].z), less_than_most(z.vs[x].w));
       bf16x8 p[QT][2];
+      float sum[QT], rounded[QT];
+      auto weigh = [&](float ks) __attribute__((always_inline)) {
+        bool over = false;
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          bf16x8 u[2];
+          over |= weigh_row(s[x], ks, far ? 0.f : m[x], less, sum[x], u, p[x]);
+          const floatx4 r = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, u[0], floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+          rounded[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, u[1], r, 0, 0, 0)[0];
+        }
+        return over;
+      };
+      auto move = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          const float down = move_row(s[x], all_ks, m[x]);
+          l[x] *= down;
+          lr[x] *= down;
+#pragma unroll
+          for (int v = 0; v < VC; ++v) o[x][v] *= down;
+        }
+      };
+      if (far) {
+        asm volatile("");
+        move();
+#pragma unroll
+        for (int x = 0; x < QT; ++x) from_reference(s[x], all_ks, m[x]);
+      }
+      if (__any(weigh(far ? 1.f : all_ks))) {
+        move();
+        if (far_from_zero<QT>(m)) {
+          far = true;
+#pragma unroll
+          for (int x = 0; x < QT; ++x) from_reference(s[x], all_ks, m[x]);
+        }
+        weigh(far ? 1.f : all_ks);
+      }
 #pragma unroll
       for (int x = 0; x < QT; ++x) {
-        float sum = 0.f, rounded = 0.f;
+        l[x] += sum[x];
+        lr[x] += rounded[x];
+      }
+      const uint32_t any_odd = (less[0].x | less[0].y | less[0].z | less[0].w | less[1].x | less[1].y | less[1].z | less[1].w) & 0x80008000u;
+      if (__any(any_odd != 0)) {
+        asm volatile("");
 #pragma unroll
-        for (int y = 0; y < 4; ++y)
-#pragma unroll
-          for (int e = 0; e < 4; e += 2) {
-            const floatx2 w = {__builtin_amdgcn_exp2f(s[x][y][e] - m[x]), __builtin_amdgcn_exp2f(s[x][y][e + 1] - m[x])};
-            sum += w[0] + w[1];
-            const bf16x2 b = __builtin_convertvector(w, bf16x2);
-            const float w0 = (float)b[0], w1 = (float)b[1];
-            rounded += w0 + w1;
-            floatx2 z = {w0 * vs[y][e], w1 * vs[y][e + 1]};          // (exact)
-            // a value that is NaN under a key that a row does not see must not reach it through 0 * NaN
-            if (partly) {
-              if (s[x][y][e] == -INFINITY) z[0] = 0.f;
-              if (s[x][y][e + 1] == -INFINITY) z[1] = 0.f;
-            }
-            const bf16x2 p2 = __builtin_convertvector(z, bf16x2);
-            p[x][y / 2][y % 2 * 4 + e] = p2[0];
-            p[x][y / 2][y % 2 * 4 + e + 1] = p2[1];
-          }
-        l[x] += sum;
-        lr[x] += rounded;
+        for (int x = 0; x < QT; ++x) odd_row(s[x], far ? 1.f : all_ks, far ? 0.f : m[x], less, p[x]);
       }
 #pragma unroll
       for (int v = 0; v < VC; ++v) {
@@ -261,8 +344,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void fourbit_attn_kernel(
   // join the four waves, 16 rows at a time
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
-    const float sum = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, l[x]), AddF32()), AddF32()));
-    const float rounded = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, lr[x]), AddF32()), AddF32()));
+    const float sum = ldexpf(__builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, l[x]), AddF32()), AddF32())), -(int)kBias);
+    const float rounded = ldexpf(lr[x], -(int)kBias);          // (of all keys of the wave)
     if (x > 0) __syncthreads();
     if (g == 0) {
       join_m[wave][n] = m[x];
@@ -311,20 +394,6 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void fourbit_attn_kernel(
       else if (a.lse) a.lse[((int64_t)t.b * r.heads + t.hk * G + row % G) * r.t + tok] = lse2 * kLn2;
     }
   }
-}
-
-// Weights are made 2^kBias too large, as large as a sum over 2^31 keys allows, so that a token's scale comes in by a subtraction of exponents
-// (16 bits, two at once; below 0 it stays 0): bits of the scale taken from those of 2^kBias say by how much. Scales above 2^kBias and NaN
-// go the long way.
-constexpr float kBias = 90.f;
-constexpr uint32_t kMostScale = 0x6c806c80u;     // 2^90 in bf16, twice
-typedef uint16_t ushortx2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ uint32_t less_than_most(uint32_t w) {      // (its own inverse)
-  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(ushortx2, kMostScale) - __builtin_bit_cast(ushortx2, w));
-}
-__device__ __forceinline__ bf16x2 scaled2(float a, float b, uint32_t less) {
-  const uint32_t w = pack_bf16x2(a, b);
-  return __builtin_bit_cast(bf16x2, __builtin_elementwise_sub_sat(__builtin_bit_cast(ushortx2, w), __builtin_bit_cast(ushortx2, less)));
 }
 
 // The same for many query rows. 64 QT rows to a workgroup, 16 QT to a wave: every wave needs all codes, so they are widened once for
@@ -491,92 +560,47 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void fourbit_tile_kernel(Cach
             for (int e = 0; e < 4; ++e) s[x][y][e] = 16 * y + 4 * g + e < left ? s[x][y][e] : -INFINITY;
         }
       }
-      // Weights over the running reference. It is moved only when a lane's weights add up to more than 2^8 (bf16 and fp32 have the range), so
-      // that no maximum is taken otherwise; then they are made once more, over the new one at most 2^1.25.
-      float ks = all_ks;
-      if (far) {
-        asm volatile("");
-        ks = 1.f;
-#pragma unroll
-        for (int x = 0; x < QT; ++x)
-#pragma unroll
-          for (int y = 0; y < 4; ++y) s[x][y] *= all_ks;
-      }
       bf16x8 p[QT][2];
       float sum[QT];
-      // Weights times 2^kBias over the running reference, and their sums; in P their tokens' scales are taken in.
-      auto weigh = [&]() __attribute__((always_inline)) {
+      auto weigh = [&](float ks) __attribute__((always_inline)) {
         bool over = false;
 #pragma unroll
         for (int x = 0; x < QT; ++x) {
-          const float ref = m[x] - kBias;
-          sum[x] = 0.f;
-#pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            float w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              w[e] = __builtin_amdgcn_exp2f(fmaf(s[x][y][e], ks, -ref));
-              sum[x] += w[e];
-            }
-            const uint32_t d0 = y % 2 ? less[y / 2].z : less[y / 2].x, d1 = y % 2 ? less[y / 2].w : less[y / 2].y;
-            const bf16x2 lo = scaled2(w[0], w[1], d0), hi = scaled2(w[2], w[3], d1);
-            p[x][y / 2][y % 2 * 4 + 0] = lo[0]; p[x][y / 2][y % 2 * 4 + 1] = lo[1];
-            p[x][y / 2][y % 2 * 4 + 2] = hi[0]; p[x][y / 2][y % 2 * 4 + 3] = hi[1];
-          }
-          over |= sum[x] > 0x1p98f;
-          asm volatile("" : "+v"(p[x][0]), "+v"(p[x][1]));     // (made here, not behind the branches)
+          bf16x8 u[2];
+          over |= weigh_row(s[x], ks, far ? 0.f : m[x], less, sum[x], u, p[x]);
         }
         return over;
       };
-      if (__any(weigh())) {
+      auto move = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int x = 0; x < QT; ++x) {
-          float mx = -INFINITY;
-#pragma unroll
-          for (int y = 0; y < 4; ++y)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[x][y][e]);
-          mx = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, mx), MaxF32()), MaxF32())) * ks;
-          const float to = mx > m[x] ? floorf(mx) : m[x];           // the same in the four lanes of a column; whole, so that what is taken from it stays exact
-          const float down = __builtin_amdgcn_exp2f(m[x] - to);
-          m[x] = to;
+          const float down = move_row(s[x], all_ks, m[x]);
           l[x] *= down;
 #pragma unroll
           for (int v = 0; v < VC; ++v) o[x][v] *= down;
         }
-        // Far from zero a multiply-add would leave a product's own rounding, which may be 2^8 and more: rounded products from here on, as m is one
-        if (!far && far_from_zero<QT>(m)) {
+      };
+      if (far) {
+        asm volatile("");
+        move();
+#pragma unroll
+        for (int x = 0; x < QT; ++x) from_reference(s[x], all_ks, m[x]);
+      }
+      if (__any(weigh(far ? 1.f : all_ks))) {
+        move();
+        if (far_from_zero<QT>(m)) {
           far = true;
-          ks = 1.f;
 #pragma unroll
-          for (int x = 0; x < QT; ++x)
-#pragma unroll
-            for (int y = 0; y < 4; ++y) s[x][y] *= all_ks;
+          for (int x = 0; x < QT; ++x) from_reference(s[x], all_ks, m[x]);
         }
-        weigh();
+        weigh(far ? 1.f : all_ks);
       }
 #pragma unroll
       for (int x = 0; x < QT; ++x) l[x] += sum[x];
-      if (odd) {                                   // rare: P by products, and no NaN of a token that a row does not see into 0 * NaN
+      if (odd) {                                   // rare
         asm volatile("");
-        uint4 vw[2];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const uint32_t* z = &lds_s[i & 1][g * 8 + x * 4];
-          vw[x] = make_uint4(less_than_most(z[0]), less_than_most(z[1]), less_than_most(z[2]), less_than_most(z[3]));
-        }
-        float vs[4][4];
-        value_scales(vw, vs);
-#pragma unroll
-        for (int x = 0; x < QT; ++x)
-#pragma unroll
-          for (int y = 0; y < 4; ++y)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float w = __builtin_amdgcn_exp2f(fmaf(s[x][y][e], ks, -m[x])) * vs[y][e];
-              p[x][y / 2][y % 2 * 4 + e] = (__bf16)(s[x][y][e] == -INFINITY ? 0.f : w);
-            }
+        for (int x = 0; x < QT; ++x) odd_row(s[x], far ? 1.f : all_ks, far ? 0.f : m[x], less, p[x]);
       }
       __builtin_amdgcn_sched_barrier(0);
       odd = store((i + 1) & 1, raw);

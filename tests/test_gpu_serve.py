@@ -392,6 +392,31 @@ def test_scores_far_from_zero(size, d, t, G):
 
 
 @pytest.mark.parametrize("d,t,G", KINDS)
+@pytest.mark.parametrize("up", [True, False])
+@pytest.mark.parametrize("first", [22, 25, 26, 27, 28, 31])
+def test_scores_farther_apart_than_weights_reach(first, up, d, t, G):
+    """The greatest scores double from block to block, 3 * 2^first and on, up or down the cache: outputs are the mean of the two values whose keys
+    are the greatest of all. A weight is rounded to 2^-8 of it, and so is the output."""
+    p = Pair(1, 1, d, 64, 5)
+    n = 5 * 64
+    K = np.zeros((1, 1, n, d))
+    best = []
+    for j in range(5):
+        of = 2.0 ** (j if up else 4 - j)
+        K[0, 0, 64 * j:64 * j + 64, 0] = p.rng.choice([0, 0.5, 1.0, 1.5], size=64) * of
+        best.append(64 * j + p.rng.permutation(64)[:2])
+        K[0, 0, best[-1], 0] = 3.0 * of
+    V = p.rng.normal(size=K.shape)
+    p.write(K, V, [0])
+    Q = np.zeros((1, G, t, d))
+    Q[..., 0] = 2.0 ** first
+    O, lse, ref = attend(p, Q, [n], scale=1.0)
+    compare(O, lse, ref, d)
+    two = np.stack([so.stored(f64(bf16(V[0, 0, i])), d) for i in best[4 if up else 0]])
+    assert (np.abs(O - two.mean(0)) <= 2.0 ** -7 * np.abs(two).mean(0) + 2.0 ** -100).all()
+
+
+@pytest.mark.parametrize("d,t,G", KINDS)
 def test_small_and_large_keys(d, t, G):
     """Runs of channels 2^-100 .. 2^100 apart, each with a query that brings it back."""
     p = Pair(1, 1, d, 64, 4)
