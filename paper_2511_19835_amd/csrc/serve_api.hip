@@ -88,9 +88,12 @@ int rsa_cache_assign(const rsa_pages* pages, int t, const int32_t* kv_len, const
   for (size_t i = 0; i < sizeof out / sizeof *out; ++i) {
     for (size_t j = 0; j < i; ++j)
       if (out[i] == out[j]) return RSA_E_RANGE;
-    if (out[i] == add || (shared && out[i] == shared) || (out[i] == kv_len && out[i] != kv_new) || (out[i] == free_count && out[i] != free_left))
+    if (out[i] == add || out[i] == positions || out[i] == slots || (shared && out[i] == shared) || (out[i] == kv_len && out[i] != kv_new) || (out[i] == free_count && out[i] != free_left))
       return RSA_E_RANGE;
   }
+  for (const void* p : {(const void*)kv_len, (const void*)add, (const void*)shared, (const void*)free_count})
+    if (p && (p == positions || p == slots)) return RSA_E_RANGE;
+  if (positions && (const void*)positions == (const void*)slots) return RSA_E_RANGE;
   rsa::AssignArgs a = {};
   a.batch = pages->batch;
   a.max_blocks = pages->max_blocks;

@@ -198,6 +198,10 @@ def test_bad_pages_are_refused(lib):
     for kw in (dict(start=0x7000), dict(new=0x2000), dict(start=0x1000), dict(count=0x3000), dict(left=0x4000), dict(free_pages=0x8000), dict(start=0x2000),
                dict(shared=0x4000), dict(new=0x3000), dict(left=0x1000), dict(table=0x1000)):
         assert call(**kw) == -5, kw
+    # the maps of the new rows over anything that is read or written
+    for at in (0x1000, 0x2000, 0x3000, 0x4000, 0x5000, 0x6000, 0x7000, 0x8000, 0x9000, 0xa000):
+        assert call(shared=0xa000, pos=at) == -5 and call(shared=0xa000, slots=at) == -5, at
+    assert call(pos=0xb000, slots=0xb000) == -5
 
 
 def test_bad_rotary_is_refused(lib):
