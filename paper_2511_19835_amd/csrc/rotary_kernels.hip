@@ -29,8 +29,31 @@ __device__ __forceinline__ void turn(double turns, float& co, float& si) {
 }
 
 // Where a thread's pairs are: kHalf: pairs 8 u .. of (channel j, channel pairs + j), pairs a multiple of 8; kInterleaved: channels 16 u ..
-// 16 u + 15; kOdd: as kHalf for any number of pairs, element by element.
+// 16 u + 15; kOdd: as kHalf for any number of pairs, 16 bytes at a time from any channel on. There the last piece, if it is not a whole one, takes
+// the eight pairs (or copied channels) up to the end and stores only its own, so that no thread reads what another writes and uses it.
+// 24 + 24 heads of 119 056 tokens, 55 pairs of 128 channels: 873 us (element by element 3354; 56 pairs 544).
 enum Form { kHalf, kInterleaved, kOdd };
+
+// (the compiler takes pointers that are chosen by an index for generic ones otherwise)
+typedef __attribute__((address_space(1))) const uint16_t* In;
+typedef __attribute__((address_space(1))) uint16_t* Out;
+typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t uintx2 __attribute__((ext_vector_type(2)));
+// Vectors at addresses of whole channels.
+typedef uintx4 __attribute__((aligned(2))) uintx4_any;
+typedef uintx2 __attribute__((aligned(2))) uintx2_any;
+typedef uint32_t __attribute__((aligned(2))) uint_any;
+
+__device__ __forceinline__ uintx4 load8(In src) {
+  return *(const __attribute__((address_space(1))) uintx4_any*)src;
+}
+// The last n channels of eight.
+__device__ __forceinline__ void store_last(Out dst, const uintx4& v, int n) {
+  if (n == 8) *(__attribute__((address_space(1))) uintx4_any*)dst = v;
+  if (n & 4) *(__attribute__((address_space(1))) uintx2_any*)(dst + 4) = uintx2{v[2], v[3]};
+  if (n & 2) *(__attribute__((address_space(1))) uint_any*)(dst + (n & 4 ? 2 : 6)) = n & 4 ? v[1] : v[3];
+  if (n & 1) dst[8 - n] = (uint16_t)((n == 7 ? v[0] : n == 5 ? v[1] : n == 3 ? v[2] : v[3]) >> 16);    // channel 1, 3, 5, 7
+}
 
 // HEADS: heads of a wave that are in flight together. 48 heads of 119 056 tokens: 4, 6, 8, 12 at once 583, 564, 550, 528 us (5.5 TB/s); 24 of 6231
 // tokens of 64 channels, in two groups: 2, 4, 12 at once 7.0, 6.9, 8.6 (the registers of twelve cost more than they bring there).
@@ -43,11 +66,13 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int units, in
   const int64_t row = id / units;
   const int u = (int)(id % units);
   const int b = (int)(row / a.t), i = (int)(row % a.t);
+  // its first pair; kOdd: of the last eight, if there are so many
+  const int j0 = F == kOdd && a.pairs >= 8 ? min(8 * u, a.pairs - 8) : 8 * u;
   const bool is = row < (int64_t)a.batch * a.t && !(a.count && i >= a.count[b]);
   if (is && u < turning) {
 #pragma unroll
     for (int z = 0; z < 2; ++z) {
-      const int e = 2 * wave + z, j = 8 * u + e;
+      const int e = 2 * wave + z, j = j0 + e;
       float co = 1.f, si = 0.f;
       if (j < a.pairs) {
         double pos = (double)(a.start ? a.start[b] : 0) + i;
@@ -74,68 +99,74 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int units, in
     }
   }
   const int h1 = min((int)(blockIdx.y + 1) * heads_per, a.x[0].heads + a.x[1].heads);
-  // two chunks of eight channels
-  int c0, c1;
+  // two chunks of eight channels, of which the last n0 and n1 are the thread's own
+  int c0, c1, n0 = 8, n1 = 8;
   if (F == kInterleaved) {
     c0 = 16 * u;
     c1 = c0 + 8;
   } else if (u < turning) {
-    c0 = 8 * u;
-    c1 = a.pairs + 8 * u;
+    c0 = j0;
+    c1 = a.pairs + j0;
+    if (F == kOdd) n0 = n1 = min(a.pairs - 8 * u, 8);
   } else {
     c0 = 2 * a.pairs + (u - turning) * 16;
     c1 = c0 + 8;
+    if (F == kOdd) {
+      n0 = min(a.head_dim - c0, 8);
+      n1 = min(a.head_dim - c1, 8);
+      c0 = min(c0, a.head_dim - 8);
+      c1 = n1 > 0 ? min(c1, a.head_dim - 8) : a.head_dim;
+    }
   }
   const bool both = c1 < a.head_dim;
-  auto place = [&](int h, const uint16_t*& in, uint16_t*& out) __attribute__((always_inline)) {
+  auto place = [&](int h, In& in, Out& out) __attribute__((always_inline)) {
     const bool second = h >= a.x[0].heads;
     const RotaryArgs::Rows& x = a.x[second];
     const int64_t at = (int64_t)b * x.sb + (int64_t)(second ? h - a.x[0].heads : h) * x.sh + (int64_t)i * x.st;
-    in = x.in + at;
-    out = x.out + at;
+    in = (In)x.in + at;
+    out = (Out)x.out + at;
   };
-  if (F == kOdd) {
+  if (F == kOdd && a.pairs < 8 && u < turning) {   // fewer than eight pairs: one by one
     for (int h = blockIdx.y * heads_per + wave; h < h1; h += 4) {
-      const uint16_t* in;
-      uint16_t* out;
+      In in;
+      Out out;
       place(h, in, out);
-      if (u < turning) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int j = 8 * u + e;
-          if (j < a.pairs) {
-            const float p = bf16_bits_to_float(in[j]), q = bf16_bits_to_float(in[a.pairs + j]);
-            out[j] = to_bf16_bits(p * co[e] - q * si[e]);
-            out[a.pairs + j] = to_bf16_bits(p * si[e] + q * co[e]);
-          }
+      for (int e = 0; e < 8; ++e)
+        if (e < a.pairs) {
+          const float p = bf16_bits_to_float(in[e]), q = bf16_bits_to_float(in[a.pairs + e]);
+          out[e] = to_bf16_bits(p * co[e] - q * si[e]);
+          out[a.pairs + e] = to_bf16_bits(p * si[e] + q * co[e]);
         }
-      } else if (in != out) {
-        for (int ch = c0, n = 0; n < 16 && ch < a.head_dim; ++n, ++ch) out[ch] = in[ch];
-      }
     }
     return;
   }
   for (int first = blockIdx.y * heads_per + wave; first < h1; first += 4 * HEADS) {
-    uint4 v[HEADS], w[HEADS];
-    uint16_t* out[HEADS];
+    uintx4 v[HEADS], w[HEADS];
+    Out out[HEADS];
     bool skip[HEADS];
 #pragma unroll
     for (int z = 0; z < HEADS; ++z) {
       skip[z] = first + 4 * z >= h1;
       if (skip[z]) continue;
-      const uint16_t* in;
+      In in;
       place(first + 4 * z, in, out[z]);
       skip[z] = u >= turning && in == out[z];
-      v[z] = *reinterpret_cast<const uint4*>(in + c0);
-      w[z] = make_uint4(0, 0, 0, 0);
-      if (both) w[z] = *reinterpret_cast<const uint4*>(in + c1);
+      w[z] = uintx4{0, 0, 0, 0};
+      if (F == kOdd) {
+        v[z] = load8(in + c0);
+        if (both) w[z] = load8(in + c1);
+      } else {
+        v[z] = *(const __attribute__((address_space(1))) uintx4*)(in + c0);
+        if (both) w[z] = *(const __attribute__((address_space(1))) uintx4*)(in + c1);
+      }
     }
 #pragma unroll
     for (int z = 0; z < HEADS; ++z) {
       if (skip[z]) continue;
       if (u < turning) {
-        uint32_t p[4] = {v[z].x, v[z].y, v[z].z, v[z].w}, q[4] = {w[z].x, w[z].y, w[z].z, w[z].w};
-        if (F == kHalf) {
+        uint32_t p[4] = {v[z][0], v[z][1], v[z][2], v[z][3]}, q[4] = {w[z][0], w[z][1], w[z][2], w[z][3]};
+        if (F != kInterleaved) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float p0 = bf16_bits_to_float(p[e] & 0xffffu), p1 = __builtin_bit_cast(float, p[e] & 0xffff0000u);
@@ -152,11 +183,16 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int units, in
             x = 8 * u + e < a.pairs ? y : x;       // (a channel behind the pairs is no product: 0 * infinity)
           }
         }
-        v[z] = make_uint4(p[0], p[1], p[2], p[3]);
-        w[z] = make_uint4(q[0], q[1], q[2], q[3]);
+        v[z] = uintx4{p[0], p[1], p[2], p[3]};
+        w[z] = uintx4{q[0], q[1], q[2], q[3]};
       }
-      *reinterpret_cast<uint4*>(out[z] + c0) = v[z];
-      if (both) *reinterpret_cast<uint4*>(out[z] + c1) = w[z];
+      if (F == kOdd) {
+        store_last(out[z] + c0, v[z], n0);
+        if (both) store_last(out[z] + c1, w[z], n1);
+      } else {
+        *(__attribute__((address_space(1))) uintx4*)(out[z] + c0) = v[z];
+        if (both) *(__attribute__((address_space(1))) uintx4*)(out[z] + c1) = w[z];
+      }
     }
   }
 }
@@ -178,7 +214,7 @@ hipError_t launch_rotary(const RotaryArgs& a, hipStream_t s) {
   const dim3 block(256);
   auto launch = [&](auto form) {
     constexpr Form F = decltype(form)::value;
-    if (F == kOdd || of_wave <= 4) hipLaunchKernelGGL((rotary_kernel<F, 4>), grid, block, 0, s, a, units, per);
+    if (of_wave <= 4) hipLaunchKernelGGL((rotary_kernel<F, 4>), grid, block, 0, s, a, units, per);
     else if (of_wave <= 8) hipLaunchKernelGGL((rotary_kernel<F, 8>), grid, block, 0, s, a, units, per);
     else hipLaunchKernelGGL((rotary_kernel<F, 12>), grid, block, 0, s, a, units, per);
   };
