@@ -182,32 +182,32 @@ __global__ __launch_bounds__(256) void fourbit_write_kernel(CacheDims c, RowDims
     for (int p = 0; p < NP; ++p) {
       const int slot0 = (p * QUADS + quad) * 4, u0 = slot0 % 64, s = slot0 / 64;
       if (slot0 < sp.hi) {
-        uint32_t vw[4];
+        if (slot0 + 4 > sp.lo) {                   // a new token (the lanes of a run of tokens go the same way)
+          uint32_t vw[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int slot = slot0 + i, u = u0 + i;
-          const bool is = slot >= sp.lo && slot < sp.hi;
-          int most = (int)largest8(x[0][p][i]);     // over the 32 channels of the run
-          most = MaxU32()(most, row_lane<kXor1>(most));
-          most = MaxU32()(most, row_lane<kXor2>(most));
-          const int e = fourbit_exponent((uint32_t)most);
-          const uint32_t w = to_codes(x[0][p][i], e);
-          if (is) {
-            kd[p][i] = w;
-            ke[p][i] = e;
-            *reinterpret_cast<uint32_t*>(&img_k[s][At<D>::k_row(u, cc)][u % 16 * 16 + cc % 4 * 4]) = w;
-            if (cc % 4 == 0) img_ks[s][At<D>::k_scale(u, cc / 4)] = (uint8_t)(e + 127);
+          for (int i = 0; i < 4; ++i) {
+            const int slot = slot0 + i, u = u0 + i;
+            const bool is = slot >= sp.lo && slot < sp.hi;
+            int most = (int)largest8(x[0][p][i]);     // over the 32 channels of the run
+            most = MaxU32()(most, row_lane<kXor1>(most));
+            most = MaxU32()(most, row_lane<kXor2>(most));
+            const int e = fourbit_exponent((uint32_t)most);
+            const uint32_t w = to_codes(x[0][p][i], e);
+            if (is) {
+              kd[p][i] = w;
+              ke[p][i] = e;
+              *reinterpret_cast<uint32_t*>(&img_k[s][At<D>::k_row(u, cc)][u % 16 * 16 + cc % 4 * 4]) = w;
+              if (cc % 4 == 0) img_ks[s][At<D>::k_scale(u, cc / 4)] = (uint8_t)(e + 127);
+            }
+            int mv = (int)largest8(x[1][p][i]);       // over the row
+            mv = MaxU32()(mv, row_lane<kXor1>(mv));
+            mv = MaxU32()(mv, row_lane<kXor2>(mv));
+            mv = MaxU32()(mv, row_lane<kFlip8>(mv));
+            if (D == 128) mv = MaxU32()(mv, row_lane<kFlip16>(mv));
+            const int ev = fourbit_exponent((uint32_t)mv);
+            vw[i] = to_codes(x[1][p][i], ev);
+            if (is && cc == 0) img_vs[s][At<D>::v_scale(u)] = ev == 128 ? 0x7fc0u : (uint16_t)((ev + 127) << 7);
           }
-          int mv = (int)largest8(x[1][p][i]);       // over the row
-          mv = MaxU32()(mv, row_lane<kXor1>(mv));
-          mv = MaxU32()(mv, row_lane<kXor2>(mv));
-          mv = MaxU32()(mv, row_lane<kFlip8>(mv));
-          if (D == 128) mv = MaxU32()(mv, row_lane<kFlip16>(mv));
-          const int ev = fourbit_exponent((uint32_t)mv);
-          vw[i] = to_codes(x[1][p][i], ev);
-          if (is && cc == 0) img_vs[s][At<D>::v_scale(u)] = ev == 128 ? 0x7fc0u : (uint16_t)((ev + 127) << 7);
-        }
-        if (slot0 + 4 > sp.lo) {
           uint32_t hw[4], fresh = 0xffffu;         // half bytes of the four tokens that are new
           tokens_to_channels(vw, hw);
           if (sp.lo > slot0) fresh &= 0xffffu << (4 * (sp.lo - slot0));
@@ -276,21 +276,23 @@ __global__ __launch_bounds__(256) void fourbit_write_kernel(CacheDims c, RowDims
   // the mean of the block's keys in 8 bits
   if (tid < D) {
     const double n = (double)sp.hi;
-    auto mean = [&](int ch) __attribute__((always_inline)) { return ((sums[0][ch] + sums[1][ch]) + (sums[2][ch] + sums[3][ch])) / n; };
-    double most = fabs(mean(lane));
-    if (D == 128) most = fmax(most, fabs(mean(lane + 64)));
+    auto sum = [&](int ch) __attribute__((always_inline)) { return (sums[0][ch] + sums[1][ch]) + (sums[2][ch] + sums[3][ch]); };
+    const double own = sum(tid) / n;
+    double most = fabs(sum(lane));
+    if (D == 128) most = fmax(most, fabs(sum(lane + 64)));
     most = fmax(most, row_lane64<kXor1>(most));
     most = fmax(most, row_lane64<kXor2>(most));
     most = fmax(most, row_lane64<kFlip8>(most));
     most = fmax(most, row_lane64<kFlip16>(most));
     most = with_xor32_64(with_xor16_64(most, MaxF64()), MaxF64());
+    most /= n;                                     // (the largest mean: a division keeps the order)
     int em = -100;
     if (most > 0) {
       int xp;
       const double f = frexp(most, &xp);
       em = max(xp - 7 + (f > 127.0 / 128.0 ? 1 : 0), -100);
     }
-    c.mean[((int64_t)sp.page * c.heads_kv + h) * D + tid] = (int8_t)(int)rint(ldexp(mean(tid), -em));
+    c.mean[((int64_t)sp.page * c.heads_kv + h) * D + tid] = (int8_t)(int)rint(ldexp(own, -em));
     if (tid == 0) *reinterpret_cast<float4*>(c.scales + ((int64_t)sp.page * c.heads_kv + h) * 4) = make_float4(0.f, 0.f, exp2_int(em), 0.f);
   }
 }
@@ -341,13 +343,13 @@ __global__ __launch_bounds__(256) void fourbit_read_kernel(CacheDims c, RowDims 
 
 template <int D, int BLK>
 hipError_t launch_write_t(const CacheDims& c, const RowDims& r, const CacheWriteArgs& a, hipStream_t s) {
-  const int blocks = (r.t - 1) / BLK + 2;          // a run of t tokens touches at most these
+  const int blocks = (r.t + BLK - 2) / BLK + 1;    // a run of t tokens touches at most these
   hipLaunchKernelGGL((fourbit_write_kernel<D, BLK>), dim3(blocks * c.batch * c.heads_kv), dim3(256), 0, s, c, r, a, blocks);
   return hipGetLastError();
 }
 template <int D, int BLK>
 hipError_t launch_read_t(const CacheDims& c, const RowDims& r, const CacheReadArgs& a, hipStream_t s) {
-  const int blocks = (r.t - 1) / BLK + 2;
+  const int blocks = (r.t + BLK - 2) / BLK + 1;
   hipLaunchKernelGGL((fourbit_read_kernel<D, BLK>), dim3(blocks * c.batch * c.heads_kv), dim3(256), 0, s, c, r, a, blocks);
   return hipGetLastError();
 }
