@@ -5,16 +5,16 @@
 // a sequence whose sum is over the list's length gets none, so who is served does not depend on timing. Positions and slots of
 // the new rows need only start, count and the table: the same workgroup writes few of them, many are a launch of their own.
 // Bound by latency: lengths, sums, free list, table, slot, each waiting for the one before. A token for each of 32 sequences 3.0 us (5.7 with
-// sums by exchanges through LDS in 64 bits and 1024 threads whatever the batch), 48 prompts of 4096 tokens 8.1 (17.0 with one wave for
-// all of their pages).
+// sums by exchanges through LDS in 64 bits and 1024 threads whatever the batch), 48 prompts of 4096 tokens 8.3 in two launches (17.0 with one
+// wave for all of their pages), one of 240 000 tokens 8.2 (13.8 with one wave to a sequence).
 #include "serve_common.hpp"
 
 namespace rsa {
 namespace {
 
 constexpr int kMostThreads = 1024;
-// Rows of positions and slots that the one workgroup writes itself.
-constexpr int64_t kFewRows = 8192;
+// Rows of positions and slots that the one workgroup writes itself (8000 rows: 9.8 us by itself, 7.4 with the second launch).
+constexpr int64_t kFewRows = 4096;
 
 // Sum of `x` over the lanes of the wave up to this one, by exchanges on the vector ALU.
 __device__ __forceinline__ int wave_prefix(int x) {
@@ -172,10 +172,11 @@ __global__ __launch_bounds__(kMostThreads) void assign_kernel(AssignArgs a) {
       had_of[tid] = w.had;
       top_of[tid] = top;
       __syncthreads();
-      for (int k = wave; k < min(threads, a.batch - q * threads); k += waves) {
+      const int here = min(threads, a.batch - q * threads), share = 31 - __builtin_clz(max(waves / here, 1));      // 2^share waves to a sequence
+      for (int k = wave >> share; k < here; k += waves >> share) {
         int32_t* row = a.table + (int64_t)(q * threads + k) * a.max_blocks + had_of[k];
         const int64_t from = top_of[k];
-        for (int e = lane; e < more_of[k]; e += 64) row[e] = a.free_pages[from - e];
+        for (int e = (wave & ((1 << share) - 1)) * 64 + lane; e < more_of[k]; e += 64 << share) row[e] = a.free_pages[from - e];
       }
       __syncthreads();
     }
@@ -194,7 +195,7 @@ __global__ __launch_bounds__(kMostThreads) void assign_kernel(AssignArgs a) {
     }
   }
   if (tid == 0) a.free_left[0] = (int32_t)(have - taken);
-  if ((int64_t)a.batch * a.t > kFewRows || a.t == 1) return;       // (the whole workgroup)
+  if ((int64_t)a.batch * a.t > kFewRows || a.t == 1 || (!a.positions && !a.slots)) return;       // (the whole workgroup)
   __syncthreads();
   for (int u = tid; u < a.batch * a.t; u += threads) {
     const int b = u / a.t;

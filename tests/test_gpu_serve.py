@@ -582,6 +582,23 @@ def test_assign(batch, width, block, t, spare, in_place):
         run_assign(table, free, len(free), kv, add.tolist(), t, block, pages, shared, in_place, maps=seed != 1)
 
 
+@pytest.mark.parametrize("batch", [1, 2, 3, 7, 9, 16, 17])
+@pytest.mark.parametrize("t", [300, 4097, 9000])
+def test_assign_long_prompts(batch, t):
+    """Hundreds and thousands of pages to a sequence, shared out over waves; the last sequence finds the list short."""
+    rng = np.random.default_rng(batch)
+    held = rng.integers(0, 50, size=batch)
+    need = [-(-(int(x) + t) // 3) - -(-int(x) // 3) for x in held]
+    pages = sum(need) + sum(-(-int(x) // 3) for x in held) + 3
+    order = rng.permutation(pages).tolist()
+    table = np.full((batch, 3100), -1)
+    for b, x in enumerate(held):
+        for e in range(-(-int(x) // 3)):
+            table[b, e] = order.pop()
+    for spare in (sum(need), sum(need) - 1):
+        run_assign(table, order[:spare], spare, held.tolist(), [t] * batch, t, 3, pages, maps=t * batch < 40000)
+
+
 def test_assign_at_its_edges():
     # no page is left; the one that needs none is served
     run_assign([[3, -1], [4, -1]], [], 0, [64, 10], [1, 1], 1, 64, 8)
