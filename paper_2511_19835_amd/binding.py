@@ -637,7 +637,8 @@ def serve_step(cache: KVCache, pages: Pages, rotary: Rotary, Q, K, V, O, kv_len,
     start and count say what was served), Q and K turned in place by their positions, keys and values into the cache, and the causal
     attention of the new queries over their sequences. Rows of sequences that were not served are left as they were."""
     # (all of it before the first call: that one moves the lengths on)
-    if pages.table.data_ptr() != cache.table.data_ptr() or pages.desc.block != cache.desc.block or pages.batch != cache.batch:
+    if (pages.table.data_ptr() != cache.table.data_ptr() or pages.desc.block != cache.desc.block or pages.batch != cache.batch
+            or pages.desc.pages != cache.desc.pages):
         raise ValueError("the pages are not those of the cache's table")
     if K.shape[2] != Q.shape[2] or rotary.dev != cache.dev:
         raise ValueError(f"a step brings keys and queries for the same rows, on one device: got {K.shape[2]} and {Q.shape[2]} rows")
@@ -649,9 +650,15 @@ def serve_step(cache: KVCache, pages: Pages, rotary: Rotary, Q, K, V, O, kv_len,
     if rotary.axes != 1:
         raise ValueError("a step's tokens stand in a row: positions along one axis")
     write, attn = (rsa_fourbit_write, rsa_fourbit_attn) if cache.bits == 4 else (rsa_cache_write, rsa_cache_attn)
-    need = rsa_fourbit_workspace_bytes(cache, rows) if cache.bits == 4 else rsa_cache_workspace_bytes(cache, rows)[1]
-    if ws is not None and _scratch(cache, ws)[1] < need:
-        raise ValueError(f"the attention's workspace has {need} bytes")
+    at = [x.data_ptr() for x in (Q, K, V, O)]
+    if any(x % 16 for x in at) or at[0] == at[1]:
+        raise ValueError("queries, keys, values and outputs begin at multiples of 16 bytes, and queries are not the keys")
+    sizes = rsa_fourbit_workspace_bytes if cache.bits == 4 else lambda *x: rsa_cache_workspace_bytes(*x)[1]
+    need, _ = sizes(cache, rows), sizes(cache, rows_kv)          # (strides that the calls do not take raise here)
+    if ws is not None:
+        where, size = _scratch(cache, ws)
+        if size < need or where % 256:
+            raise ValueError(f"the attention's workspace has {need} bytes, from a multiple of 256 on")
     if lse is not None and (lse.dtype is not torch.float32 or lse.shape != rows.shape[:3] or lse.get_device() != cache.dev or not lse.is_contiguous()):
         raise ValueError("expect a contiguous fp32 lse [batch, heads, t] on the cache's device")
     rsa_cache_assign(pages, Q.shape[2], kv_len, add, free_count, kv_len, free_count, start, count, positions, slots, shared, stream)

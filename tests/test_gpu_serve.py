@@ -836,11 +836,15 @@ def test_binding_refusals():
     good = dict(cache=four, pages=rec, rotary=half, Q=x, K=x.clone(), V=x.clone(), O=x.clone(), kv_len=i32([0, 0]), add=i32([3, 3]), free_count=i32([4]), start=i32([0, 0]),
                 count=i32([0, 0]))
     wide = torch.zeros(2, 2, 3, 128, dtype=torch.bfloat16, device=DEV)
+    odd = torch.zeros(2, 2, 3, 68, dtype=torch.bfloat16, device=DEV)[..., :64]          # rows 136 bytes apart
     for bad in (dict(K=x[:, :, :2].contiguous(), V=x[:, :, :2].contiguous()), dict(O=x[:, :, :2]), dict(V=x[:, :1]), dict(Q=wide, O=wide), dict(K=x[:, :1].contiguous(), V=x[:, :1].contiguous()),
                 dict(lse=torch.zeros(2, 2, 2, device=DEV)), dict(rotary=rb.make_rotary(torch.ones(33, dtype=torch.float64, device=DEV))),
                 dict(rotary=rb.make_rotary(torch.ones(32, dtype=torch.float64, device=DEV), axis_pairs=[16, 16])),
-                dict(pages=rb.pages_of(four.table, torch.arange(4, dtype=torch.int32, device=DEV), 128))):
-        with pytest.raises(ValueError):
+                dict(pages=rb.pages_of(four.table, torch.arange(4, dtype=torch.int32, device=DEV), 128)),
+                dict(pages=rb.pages_of(four.table, torch.arange(5, dtype=torch.int32, device=DEV), 64)), dict(K=x), dict(ws=torch.zeros(1, device=DEV).expand(2)),
+                dict(ws=torch.zeros(4096, dtype=torch.uint8, device=DEV)[16:]), dict(V=torch.zeros(2 * 2 * 3 * 64 + 1, dtype=torch.bfloat16, device=DEV)[1:].view(2, 2, 3, 64)),
+                dict(Q=odd, O=odd), dict(K=odd, V=odd)):
+        with pytest.raises((ValueError, RuntimeError)):
             rb.serve_step(**{**good, **bad})
     assert int(good["free_count"]) == 4 and good["kv_len"].tolist() == [0, 0] and (four.table == -1).all()
     rb.serve_step(**good)
