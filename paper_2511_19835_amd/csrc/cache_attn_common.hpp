@@ -145,7 +145,8 @@ struct Plan {
 };
 // Up to 32 rows of a group: tiles of 16 or 32 rows whose keys the waves share out; more: tiles of 64 or 128 rows. us, 8 heads, four
 // sequences of 32 768 keys, d = 128, and sixteen of 8192, d = 64: 20 rows in tiles of 32 59 and 43, of 64 61 and 43; 40 rows in tiles
-// of 64 65 and 45, of 32 87 and 68, of 128 82 and 55; 80 rows in tiles of 128 88 and 58, of 64 109 and 76.
+// of 64 65 and 45, of 32 87 and 68, of 128 82 and 55; 80 rows in tiles of 128 88 and 58, of 64 109 and 76. (All in 8 bits; the first in 4
+// bits: 16 rows 32 us, 32 in tiles of 32 36, 64 in tiles of 64 56, 128 in tiles of 128 77.)
 Plan plan_of(const CacheDims& c, const RowDims& r, int group, int list_len) {
   Plan p;
   const int G = r.heads / c.heads_kv;

@@ -131,6 +131,11 @@ struct Step64 {
   uint4 vs[2];
 };
 
+// Few rows: a wave's steps go from memory to registers to products, no barrier until the end. Bound by memory: a token of 32 sequences of up to 32 768
+// keys, 32 heads over 8 (0.72 GB), 134 us and 6 of joining; all of them full 170 us, 6.6 TB/s. Sums of what the weights are in bf16, by which
+// outputs are divided so that the rounding of a few large weights cancels, are a product with ones: it runs beside the vector ALU, which is
+// what 32 rows are bound by (4 x 8 heads on 32 768 keys 36 us; sums and scales on the vector ALU and a maximum each step 46).
+// 3 rows of 2 heads on 1088 keys 7.2 us: lengths, pages, codes, products and the join one after the other.
 template <int D, int BLK, int QT, int NW>
 __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void fourbit_attn_kernel(CacheDims c, RowDims r, CacheAttnArgs a, TileGrid tg) {
   constexpr int KM = D / 32, VC = D / 16;          // products of a tile of 16 keys / channel tiles
@@ -397,9 +402,14 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void fourbit_attn_kernel(
 }
 
 // The same for many query rows. 64 QT rows to a workgroup, 16 QT to a wave: every wave needs all codes, so they are widened once for
-// the workgroup, a quarter by each wave, into LDS in the order of the operands. Two buffers, one barrier a step of 64 keys.
-// Three workgroups to a compute unit at d = 64, two at d = 128. us with two and
-// three: 128 rows of 16 x 8 heads on 8192 keys 63, 58; 1000 rows 343, 310; 1000 rows of 12 heads on 30 000 keys 137, 124.
+// the workgroup, a quarter by each wave, into LDS in the order of the operands. Two buffers, one barrier a step of 64 keys; codes are requested
+// two steps ahead and widened between the softmax and the products of the values.
+// 24 heads, 1560 tokens on 20 280 keys: 360 us and 12.6 of joining, 1040 TFLOP/s (a library product 1219); the matrix pipe is busy 50 % of the
+// time, the vector ALU 58 %, LDS 40 %. Scores of the next step beside this one's weights 456 us, each wave widening for itself without LDS
+// 417, two groups of waves a phase apart 486, products of 32x32x16 421 (against 383 to 392 of the form of the day).
+// 64 rows (56 us where 32 rows take 36): neither half the LDS reads, nor eight waves, nor four steps ahead are faster.
+// Three workgroups to a compute unit at d = 64, two at d = 128. us with two and three:
+// 128 rows of 16 x 8 heads on 8192 keys 63, 58; 1000 rows 343, 310; 1000 rows of 12 heads on 30 000 keys 137, 124.
 constexpr int kAhead = 256;                        // steps that are looked up together
 template <int D, int BLK, int QT>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void fourbit_tile_kernel(CacheDims c, RowDims r, CacheAttnArgs a, TileGrid tg) {
