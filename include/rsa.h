@@ -381,9 +381,11 @@ int rsa_fourbit_read(const rsa_cache* cache, const rsa_rows* rows, const int32_t
 /*
  * As rsa_cache_attn, arguments and rules alike, but for the roundings: scores are those of the stored keys, summed in fp32; a weight times
  * its token's scale is rounded to bf16, so that beside the rounding of O to bf16 and those of the fp32 steps an output is off by at
- * most 2^-8 sum p |v| / sum p, however far apart the tokens' scales are. Values are to be below 2^100, and those below 2^-100 may
- * vanish (2^8 of them times their number has to stay in the range of fp32, and their products with weights are taken in it). A NaN among the stored
- * keys or values reaches the queries that see its token and no others.
+ * most 2^-8 sum p |v| / sum p, however far apart the tokens' scales are (2^-7 where a group has at most 32 rows of tokens times heads that share
+ * keys: there outputs are divided by the weights as they were rounded, so that a row that sees one key gets its value as it is stored).
+ * Values are to be below 2^100 (2^8 of them times their number has to stay in the range of fp32); those below 2^-100 may vanish, and so may a
+ * weight below 2^-125 of its row's largest, whatever its value (weights and their products with values are numbers of fp32). A NaN among
+ * the stored keys or values reaches the queries that see its token and no others.
  */
 int rsa_fourbit_attn(const rsa_cache* cache, const rsa_rows* rows, const void* Q, const int32_t* kv_len,
                      const int32_t* q_len, float scale, int flags, const int32_t* block_idx, const int32_t* kept, int group,

@@ -140,10 +140,15 @@ def attend(pair, Q, kv_len, q_len=None, scale=0.0, causal=False, lists=None, gro
     rb.rsa_fourbit_attn(pair.gpu, rows, Qd, i32(kv_len), i32(q_len), scale, rb.RSA_CACHE_CAUSAL if causal else 0, idx, kept, group, O, lse, scratch, stream)
     torch.cuda.synchronize()
     ref = pair.ref.attend(f64(Qd), kv_len, q_len, scale, causal, lists, group)
-    return f64(O), lse.cpu().double().numpy(), ref
+    few = (min(group, Q.shape[2]) if lists is not None else Q.shape[2]) * (Q.shape[1] // pair.hk) <= 32
+    return f64(O), lse.cpu().double().numpy(), {**ref, "P": 2.0 ** -7 if few else 2.0 ** -8}
 
 
 def compare(O, lse, ref, d):
+    """Weights p are rounded to p (1 + r), |r| <= u / (1 + u) with u = 2^-8. Divided by the sum of p, an output is off by at most u sum p |v| / sum p = u A.
+    Divided by the sum of the rounded ones, as up to 32 rows are, it is sum p (r - R) v / sum p (1 + r) off, R the mean of r over the weights: |r - R| <= 2 u / (1 + u)
+    and sum p (1 + r) >= sum p / (1 + u), so at most 2 u A (and nothing where one weight is all). What vanishes: a weight times its token's scale below 2^-126, and a weight below
+    2^-133 under a scale of at most 2^7, both times a code of at most 6: 6 * 2^-126 for each key."""
     isq = ref["isq"]
     assert (O[~isq] == 7.0).all() and (lse[~isq] == 7.0).all(), "rows behind the last query were written"
     O, lse = O[isq], lse[isq]
@@ -153,7 +158,7 @@ def compare(O, lse, ref, d):
     O, lse, want, A, want_lse, S, n = (x[~empty] for x in (O, lse, want, A, want_lse, S, n))
     assert np.array_equal(np.isnan(O), np.isnan(want)) and np.array_equal(np.isnan(lse), np.isnan(want_lse))
     es = (d + 16) * 2.0 ** -24 * S
-    bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2 * es + 4 * n * 2.0 ** -24)[:, None] * A + n[:, None] * 2.0 ** -126
+    bound = 2.0 ** -8 * np.abs(want) + (ref["P"] + 2 * es + 4 * n * 2.0 ** -24)[:, None] * A + n[:, None] * 6 * 2.0 ** -126
     ok = ~np.isnan(want)
     worst = (np.abs(O - want)[ok] / bound[ok]).max(initial=0)
     fine = ~np.isnan(want_lse)
@@ -414,6 +419,43 @@ def test_scores_farther_apart_than_weights_reach(first, up, d, t, G):
     compare(O, lse, ref, d)
     two = np.stack([so.stored(f64(bf16(V[0, 0, i])), d) for i in best[4 if up else 0]])
     assert (np.abs(O - two.mean(0)) <= 2.0 ** -7 * np.abs(two).mean(0) + 2.0 ** -100).all()
+
+
+@pytest.mark.parametrize("d,t,G", KINDS)
+@pytest.mark.parametrize("keys", [1, 2, 3])
+def test_log_sum_exps_of_few_keys(keys, d, t, G):
+    """Where next to nothing is summed the log-sum-exp is as exact as a score: 2^-21 and the scores' own bound."""
+    p = Pair(24, 1, d, 64, 1, seed=keys)
+    p.fill([keys] * 24)
+    Q = p.rng.normal(size=(24, G, t, d)) * 0.3
+    O, lse, ref = attend(p, Q, [keys] * 24)
+    compare(O, lse, ref, d)
+    if keys == 1 and t * G <= 32:                                              # the one value as it is stored
+        for b in range(24):
+            assert (O[b] == ref["O"][b]).all()
+
+
+@pytest.mark.parametrize("d,t,G", KINDS)
+@pytest.mark.parametrize("up", [True, False])
+@pytest.mark.parametrize("gap,size", [(60, 99), (100, 9), (120, 40), (124, 9), (124, 99)])
+def test_large_values_of_small_weight(gap, size, up, d, t, G):
+    """Half of the channels have values of 2^size in one block alone, whose scores are 2^-gap of the other's: before it and behind it."""
+    p = Pair(1, 1, d, 64, 2)
+    K, V = np.zeros((1, 1, 128, d)), p.rng.normal(size=(1, 1, 128, d))
+    low = slice(0, 64) if up else slice(64, 128)
+    high = slice(64, 128) if up else slice(0, 64)
+    K[0, 0, low, 0] = -1
+    V[0, 0, high, :d // 2] = 0
+    V[0, 0, low] *= 2.0 ** size
+    V[0, 0, low, d // 2:] = 0
+    p.write(K, V, [0])
+    Q = np.zeros((1, G, t, d))
+    Q[..., 0] = gap * np.log(2)                                               # (in bf16: 2^-8 of it more at most)
+    O, lse, ref = attend(p, Q, [128], scale=1.0)
+    compare(O, lse, ref, d)
+    if size - gap > -110:
+        some = np.abs(ref["O"]) >= 2.0 ** (size - gap - 8)                      # (codes of 64 equal weights may add up to nothing)
+        assert some[..., :d // 2].any() and (O[some] != 0).all()
 
 
 @pytest.mark.parametrize("d,t,G", KINDS)
