@@ -158,7 +158,7 @@ def compare(O, lse, ref, d):
     O, lse, want, A, want_lse, S, n = (x[~empty] for x in (O, lse, want, A, want_lse, S, n))
     assert np.array_equal(np.isnan(O), np.isnan(want)) and np.array_equal(np.isnan(lse), np.isnan(want_lse))
     es = (d + 16) * 2.0 ** -24 * S
-    bound = 2.0 ** -8 * np.abs(want) + (ref["P"] + 2 * es + 4 * n * 2.0 ** -24)[:, None] * A + n[:, None] * 6 * 2.0 ** -126
+    bound = 2.0 ** -8 * np.abs(want) + (ref.get("P", 2.0 ** -8) + 2 * es + 4 * n * 2.0 ** -24)[:, None] * A + n[:, None] * 6 * 2.0 ** -126
     ok = ~np.isnan(want)
     worst = (np.abs(O - want)[ok] / bound[ok]).max(initial=0)
     fine = ~np.isnan(want_lse)
