@@ -381,8 +381,8 @@ int rsa_fourbit_read(const rsa_cache* cache, const rsa_rows* rows, const int32_t
 /*
  * As rsa_cache_attn, arguments and rules alike, but for the roundings: scores are those of the stored keys, summed in fp32; a weight times
  * its token's scale is rounded to bf16, so that beside the rounding of O to bf16 and those of the fp32 steps an output is off by at
- * most 2^-8 sum p |v| / sum p, however far apart the tokens' scales are (2^-7 where a group has at most 32 rows of tokens times heads that share
- * keys: there outputs are divided by the weights as they were rounded, so that a row that sees one key gets its value as it is stored).
+ * most 2^-8 sum p |v| / sum p, however far apart the tokens' scales are. Where a group has at most 32 rows (tokens times heads that share
+ * keys) what that rounding leaves is multiplied too: 2^-15 sum p |v| / sum p.
  * Values are to be below 2^100 (2^8 of them times their number has to stay in the range of fp32); those below 2^-100 may vanish, and so may a
  * weight below 2^-125 of its row's largest, whatever its value (weights and their products with values are numbers of fp32). A NaN among
  * the stored keys or values reaches the queries that see its token and no others.

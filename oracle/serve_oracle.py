@@ -48,7 +48,7 @@ class Cache(co.Cache):
         p.mean = np.rint(np.ldexp(mean, -p.em)).astype(np.int64)
 
     def attend(self, *args, **kw):
-        """cache_oracle's, with A = sum p |v| / sum p: a weight's rounding to bf16 costs an output at most 2^-8 of that (2^-7 over rounded weights)."""
+        """cache_oracle's, with A = sum p |v| / sum p: a weight's rounding to bf16 costs an output at most 2^-8 of that."""
         out = super().attend(*args, **kw)
         return {**out, "A": self._weighted(*args, **kw)}
 

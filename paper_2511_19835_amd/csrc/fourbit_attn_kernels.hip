@@ -8,8 +8,8 @@
 // keys, summed in fp32; a value's code is widened alone, and its token's scale goes into P.
 //
 // P in bf16: half a step is 2^-8 of a weight, and a scale only moves its exponent, whatever the scales of the tokens are to each other, so no
-// running scale of the outputs is needed. The log-sum-exp takes the weights as they are in fp32. The running reference m of a row is moved
-// only when the weights of a step have become large beside it, so most steps take no maximum.
+// running scale of the outputs is needed. Few rows, which wait for memory, take what the rounding leaves of it as a second product (2^-16 remains). The
+// running reference m of a row is moved only when the weights of a step have become large beside it, so most steps take no maximum.
 #include "fourbit_common.hpp"
 
 #include "cache_attn_common.hpp"
@@ -56,10 +56,16 @@ __device__ __forceinline__ bf16x2 scaled2(uint32_t w, uint32_t less) {
   return __builtin_bit_cast(bf16x2, __builtin_elementwise_sub_sat(__builtin_bit_cast(ushortx2, w), __builtin_bit_cast(ushortx2, less)));
 }
 
-// Weights of a lane's 16 scores of a row (times `ks`), 2^kBias too large, over the reference: their sum, the weights in bf16, and P, in which their
-// tokens' scales are taken in. -> whether the reference has to follow: it is moved only when the sum is more than 2^8 (bf16 and fp32 have the
-// range), so that no maximum is taken otherwise; then they are made once more, over the new one at most 2^1.25.
-__device__ __forceinline__ bool weigh_row(const floatx4 (&s)[4], float ks, float m, const uint4 (&less)[2], float& sum, bf16x8 (&u)[2], bf16x8 (&p)[2]) {
+// The upper half of two weights, and what it leaves of one (exact).
+__device__ __forceinline__ uint32_t cut_bf16x2(float a, float b) {
+  return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x07060302u);
+}
+__device__ __forceinline__ float behind_bf16(float a) { return a - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, a) & 0xffff0000u); }
+// Weights of a lane's 16 scores of a row (times `ks`), 2^kBias too large, over the reference: their sum, and P, the weights in bf16 with their tokens'
+// scales taken in; FINE: cut to bf16, and what that leaves of them. -> whether the reference has to follow: it is moved only when the sum is more than
+// 2^8 (bf16 and fp32 have the range), so that no maximum is taken otherwise; then they are made once more, over the new one at most 1.
+template <bool FINE>
+__device__ __forceinline__ bool weigh_row(const floatx4 (&s)[4], float ks, float m, const uint4 (&less)[2], float& sum, bf16x8 (&p)[2], bf16x8 (&rest)[2]) {
   const float ref = m - kBias;
   sum = 0.f;
 #pragma unroll
@@ -70,18 +76,26 @@ __device__ __forceinline__ bool weigh_row(const floatx4 (&s)[4], float ks, float
       w[e] = __builtin_amdgcn_exp2f(fmaf(s[y][e], ks, -ref));
       sum += w[e];
     }
-    const uint32_t d0 = y % 2 ? less[y / 2].z : less[y / 2].x, d1 = y % 2 ? less[y / 2].w : less[y / 2].y;
-    const uint32_t u0 = pack_bf16x2(w[0], w[1]), u1 = pack_bf16x2(w[2], w[3]);
-    const bf16x2 a = __builtin_bit_cast(bf16x2, u0), b = __builtin_bit_cast(bf16x2, u1), lo = scaled2(u0, d0), hi = scaled2(u1, d1);
-    const int at = y % 2 * 4;
-    u[y / 2][at] = a[0]; u[y / 2][at + 1] = a[1]; u[y / 2][at + 2] = b[0]; u[y / 2][at + 3] = b[1];
-    p[y / 2][at] = lo[0]; p[y / 2][at + 1] = lo[1]; p[y / 2][at + 2] = hi[0]; p[y / 2][at + 3] = hi[1];
+#pragma unroll
+    for (int e = 0; e < 4; e += 2) {
+      const uint4 d = less[y / 2];
+      const uint32_t of = y % 2 ? e ? d.w : d.z : e ? d.y : d.x;
+      const bf16x2 z = scaled2(FINE ? cut_bf16x2(w[e], w[e + 1]) : pack_bf16x2(w[e], w[e + 1]), of);
+      p[y / 2][y % 2 * 4 + e] = z[0];
+      p[y / 2][y % 2 * 4 + e + 1] = z[1];
+      if constexpr (FINE) {
+        const bf16x2 r = scaled2(pack_bf16x2(behind_bf16(w[e]), behind_bf16(w[e + 1])), of);
+        rest[y / 2][y % 2 * 4 + e] = r[0];
+        rest[y / 2][y % 2 * 4 + e + 1] = r[1];
+      }
+    }
   }
   asm volatile("" : "+v"(p[0]), "+v"(p[1]));       // (made here, not behind the branches)
+  if constexpr (FINE) asm volatile("" : "+v"(rest[0]), "+v"(rest[1]));
   return sum > 0x1p15f;                            // 2^(8 + kBias)
 }
 // The reference goes up to the row's largest score, where that is larger -> what is to be taken of what was summed over the old one (0 from 2^-126
-// down). The same in the four lanes of a column; whole, so that what is taken from it stays exact.
+// down). The same in the four lanes of a column. (The score itself, so that the weight of a key that outweighs the others is 1, and exact in bf16.)
 __device__ __forceinline__ float move_row(const floatx4 (&s)[4], float ks, float& m) {
   float mx = -INFINITY;
 #pragma unroll
@@ -89,7 +103,7 @@ __device__ __forceinline__ float move_row(const floatx4 (&s)[4], float ks, float
 #pragma unroll
     for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[y][e]);
   mx = __builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, mx), MaxF32()), MaxF32())) * ks;
-  const float to = mx > m ? floorf(mx) : m;
+  const float to = mx > m ? mx : m;
   const float down = __builtin_amdgcn_exp2f(m - to);
   m = to;
   return down;
@@ -107,7 +121,8 @@ __device__ __forceinline__ void from_reference(floatx4 (&s)[4], float ks, float 
     }
 }
 // P of tokens with a scale above 2^kBias or NaN, by products; no NaN of a token that the row does not see into 0 * NaN.
-__device__ __forceinline__ void odd_row(const floatx4 (&s)[4], float ks, float m, const uint4 (&less)[2], bf16x8 (&p)[2]) {
+template <bool FINE>
+__device__ __forceinline__ void odd_row(const floatx4 (&s)[4], float ks, float m, const uint4 (&less)[2], bf16x8 (&p)[2], bf16x8 (&rest)[2]) {
   uint4 w[2];
 #pragma unroll
   for (int x = 0; x < 2; ++x) w[x] = make_uint4(less_than_most(less[x].x), less_than_most(less[x].y), less_than_most(less[x].z), less_than_most(less[x].w));
@@ -118,7 +133,13 @@ __device__ __forceinline__ void odd_row(const floatx4 (&s)[4], float ks, float m
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float z = __builtin_amdgcn_exp2f(fmaf(s[y][e], ks, -m)) * vs[y][e];
-      p[y / 2][y % 2 * 4 + e] = (__bf16)(s[y][e] == -INFINITY ? 0.f : z);
+      const float w = s[y][e] == -INFINITY ? 0.f : z;
+      if constexpr (FINE) {
+        p[y / 2][y % 2 * 4 + e] = (__bf16)(w - behind_bf16(w));
+        rest[y / 2][y % 2 * 4 + e] = (__bf16)behind_bf16(w);
+      } else {
+        p[y / 2][y % 2 * 4 + e] = (__bf16)w;
+      }
     }
 }
 
@@ -132,9 +153,8 @@ struct Step64 {
 };
 
 // Few rows: a wave's steps go from memory to registers to products, no barrier until the end. Bound by memory: a token of 32 sequences of up to 32 768
-// keys, 32 heads over 8 (0.72 GB), 134 us and 6 of joining; all of them full 170 us, 6.6 TB/s. Sums of what the weights are in bf16, by which
-// outputs are divided so that the rounding of a few large weights cancels, are a product with ones: it runs beside the vector ALU, which is
-// what 32 rows are bound by (4 x 8 heads on 32 768 keys 36 us; sums and scales on the vector ALU and a maximum each step 46).
+// keys, 32 heads over 8 (0.72 GB), 136 us and 6 of joining; all of them full 172 us, 6.5 TB/s (170 with P rounded once: the second product costs 1 to 3 %,
+// d = 64 up to 12 %). 17 to 32 rows by the vector ALU (4 x 8 heads on 32 768 keys 40 us, 36 with P rounded once).
 // 3 rows of 2 heads on 1088 keys 7.2 us: lengths, pages, codes, products and the join one after the other.
 template <int D, int BLK, int QT, int NW>
 __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void fourbit_attn_kernel(CacheDims c, RowDims r, CacheAttnArgs a, TileGrid tg) {
@@ -143,7 +163,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void fourbit_attn_kernel(
   constexpr int KR = fourbit_k_record(D), VR = fourbit_v_record(D);
   constexpr int PITCH = D + 4;                     // floats of a row in the joining buffer
   __shared__ __align__(16) float join[NW][16][PITCH];
-  __shared__ float join_m[NW][16], join_l[NW][16], join_r[NW][16];
+  __shared__ float join_m[NW][16], join_l[NW][16];
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
   const int g = lane / 16, n = lane % 16;
   const int split = blockIdx.x % tg.splits;
@@ -168,20 +188,17 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void fourbit_attn_kernel(
     }
   }
   floatx4 o[QT][VC];
-  float m[QT], l[QT], lr[QT];                       // reference, sums of the weights and of what they are in P
+  float m[QT], l[QT];                              // reference, sum of the weights
   bool far = false;                                // a reference is 2^23 and more
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
     m[x] = kNoReference;
-    l[x] = lr[x] = 0.f;
+    l[x] = 0.f;
 #pragma unroll
     for (int v = 0; v < VC; ++v) o[x][v] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
 
   const float all_ks = fmaxf(a.scale_log2e, 0x1p-149f);      // (above 0, so that a masked score stays -inf)
-  bf16x8 ones;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.f;
 
   const int u0 = (int)((int64_t)t.units * split / tg.splits), u1 = (int)((int64_t)t.units * (split + 1) / tg.splits);
   const int steps = (u1 - u0) * SPB;
@@ -253,17 +270,12 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void fourbit_attn_kernel(
       uint4 less[2];
 #pragma unroll
       for (int x = 0; x < 2; ++x) less[x] = make_uint4(less_than_most(z.vs[x].x), less_than_most(z.vs[x].y), less_than_most(z.vs[x].z), less_than_most(z.vs[x].w));
-      bf16x8 p[QT][2];
-      float sum[QT], rounded[QT];
+      bf16x8 p[QT][2], rest[QT][2];
+      float sum[QT];
       auto weigh = [&](float ks) __attribute__((always_inline)) {
         bool over = false;
 #pragma unroll
-        for (int x = 0; x < QT; ++x) {
-          bf16x8 u[2];
-          over |= weigh_row(s[x], ks, far ? 0.f : m[x], less, sum[x], u, p[x]);
-          const floatx4 r = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, u[0], floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-          rounded[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, u[1], r, 0, 0, 0)[0];
-        }
+        for (int x = 0; x < QT; ++x) over |= weigh_row<true>(s[x], ks, far ? 0.f : m[x], less, sum[x], p[x], rest[x]);
         return over;
       };
       auto move = [&]() __attribute__((always_inline)) {
@@ -271,7 +283,6 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void fourbit_attn_kernel(
         for (int x = 0; x < QT; ++x) {
           const float down = move_row(s[x], all_ks, m[x]);
           l[x] *= down;
-          lr[x] *= down;
 #pragma unroll
           for (int v = 0; v < VC; ++v) o[x][v] *= down;
         }
@@ -292,15 +303,12 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void fourbit_attn_kernel(
         weigh(far ? 1.f : all_ks);
       }
 #pragma unroll
-      for (int x = 0; x < QT; ++x) {
-        l[x] += sum[x];
-        lr[x] += rounded[x];
-      }
+      for (int x = 0; x < QT; ++x) l[x] += sum[x];
       const uint32_t any_odd = (less[0].x | less[0].y | less[0].z | less[0].w | less[1].x | less[1].y | less[1].z | less[1].w) & 0x80008000u;
       if (__any(any_odd != 0)) {
         asm volatile("");
 #pragma unroll
-        for (int x = 0; x < QT; ++x) odd_row(s[x], far ? 1.f : all_ks, far ? 0.f : m[x], less, p[x]);
+        for (int x = 0; x < QT; ++x) odd_row<true>(s[x], far ? 1.f : all_ks, far ? 0.f : m[x], less, p[x], rest[x]);
       }
 #pragma unroll
       for (int v = 0; v < VC; ++v) {
@@ -310,6 +318,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void fourbit_attn_kernel(
         for (int x = 0; x < QT; ++x) {
           o[x][v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, p[x][0], o[x][v], 0, 0, 0);
           o[x][v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, p[x][1], o[x][v], 0, 0, 0);
+          o[x][v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, rest[x][0], o[x][v], 0, 0, 0);
+          o[x][v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, rest[x][1], o[x][v], 0, 0, 0);
         }
       }
       if (SETS == 1) load_v(z, again);
@@ -350,25 +360,19 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void fourbit_attn_kernel(
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
     const float sum = ldexpf(__builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, l[x]), AddF32()), AddF32())), -(int)kBias);
-    const float rounded = ldexpf(lr[x], -(int)kBias);          // (of all keys of the wave)
     if (x > 0) __syncthreads();
     if (g == 0) {
       join_m[wave][n] = m[x];
       join_l[wave][n] = sum;
-      join_r[wave][n] = rounded;
     }
     __syncthreads();
     float most = join_m[0][n];
 #pragma unroll
     for (int w = 1; w < NW; ++w) most = fmaxf(most, join_m[w][n]);
-    float total = 0.f, divisor = 0.f;
+    float total = 0.f;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const float down = exp2f(join_m[w][n] - most);
-      total += join_l[w][n] * down;
-      divisor += join_r[w][n] * down;
-    }
-    const float f = divisor == 0.f ? 0.f : exp2f(m[x] - most) / divisor;
+    for (int w = 0; w < NW; ++w) total += join_l[w][n] * exp2f(join_m[w][n] - most);
+    const float f = total == 0.f ? 0.f : exp2f(m[x] - most) / total;
 #pragma unroll
     for (int v = 0; v < VC; ++v) *reinterpret_cast<floatx4*>(&join[wave][n][16 * v + 4 * g]) = o[x][v] * f;
     __syncthreads();
@@ -570,15 +574,12 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void fourbit_tile_kernel(Cach
             for (int e = 0; e < 4; ++e) s[x][y][e] = 16 * y + 4 * g + e < left ? s[x][y][e] : -INFINITY;
         }
       }
-      bf16x8 p[QT][2];
+      bf16x8 p[QT][2], none[2];
       float sum[QT];
       auto weigh = [&](float ks) __attribute__((always_inline)) {
         bool over = false;
 #pragma unroll
-        for (int x = 0; x < QT; ++x) {
-          bf16x8 u[2];
-          over |= weigh_row(s[x], ks, far ? 0.f : m[x], less, sum[x], u, p[x]);
-        }
+        for (int x = 0; x < QT; ++x) over |= weigh_row<false>(s[x], ks, far ? 0.f : m[x], less, sum[x], p[x], none);
         return over;
       };
       auto move = [&]() __attribute__((always_inline)) {
@@ -610,7 +611,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void fourbit_tile_kernel(Cach
       if (odd) {                                   // rare
         asm volatile("");
 #pragma unroll
-        for (int x = 0; x < QT; ++x) odd_row(s[x], far ? 1.f : all_ks, far ? 0.f : m[x], less, p[x]);
+        for (int x = 0; x < QT; ++x) odd_row<false>(s[x], far ? 1.f : all_ks, far ? 0.f : m[x], less, p[x], none);
       }
       __builtin_amdgcn_sched_barrier(0);
       odd = store((i + 1) & 1, raw);

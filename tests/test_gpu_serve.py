@@ -141,14 +141,13 @@ def attend(pair, Q, kv_len, q_len=None, scale=0.0, causal=False, lists=None, gro
     torch.cuda.synchronize()
     ref = pair.ref.attend(f64(Qd), kv_len, q_len, scale, causal, lists, group)
     few = (min(group, Q.shape[2]) if lists is not None else Q.shape[2]) * (Q.shape[1] // pair.hk) <= 32
-    return f64(O), lse.cpu().double().numpy(), {**ref, "P": 2.0 ** -7 if few else 2.0 ** -8}
+    return f64(O), lse.cpu().double().numpy(), {**ref, "P": 2.0 ** -15 if few else 2.0 ** -8}
 
 
 def compare(O, lse, ref, d):
-    """Weights p are rounded to p (1 + r), |r| <= u / (1 + u) with u = 2^-8. Divided by the sum of p, an output is off by at most u sum p |v| / sum p = u A.
-    Divided by the sum of the rounded ones, as up to 32 rows are, it is sum p (r - R) v / sum p (1 + r) off, R the mean of r over the weights: |r - R| <= 2 u / (1 + u)
-    and sum p (1 + r) >= sum p / (1 + u), so at most 2 u A (and nothing where one weight is all). What vanishes: a weight times its token's scale below 2^-126, and a weight below
-    2^-133 under a scale of at most 2^7, both times a code of at most 6: 6 * 2^-126 for each key."""
+    """Weights are rounded by half a step of bf16, 2^-8 of them, and an output is off by at most that of A = sum p |v| / sum p. Up to 32 rows: they are cut to
+    bf16, which leaves less than 2^-7 of a weight, and that is rounded to bf16 in turn: 2^-15. What vanishes: a weight times its token's scale below
+    2^-126, and a weight below 2^-133 under a scale of at most 2^7, both times a code of at most 6: 6 * 2^-126 for each key."""
     isq = ref["isq"]
     assert (O[~isq] == 7.0).all() and (lse[~isq] == 7.0).all(), "rows behind the last query were written"
     O, lse = O[isq], lse[isq]
