@@ -147,18 +147,22 @@ struct Plan {
 // sequences of 32 768 keys, d = 128, and sixteen of 8192, d = 64: 20 rows in tiles of 32 59 and 43, of 64 61 and 43; 40 rows in tiles
 // of 64 65 and 45, of 32 87 and 68, of 128 82 and 55; 80 rows in tiles of 128 88 and 58, of 64 109 and 76. (All in 8 bits; the first in 4
 // bits: 16 rows 32 us, 32 in tiles of 32 36, 64 in tiles of 64 56, 128 in tiles of 128 77.)
-Plan plan_of(const CacheDims& c, const RowDims& r, int group, int list_len) {
+// `short_few`: steps up to which more rows are taken in tiles of 32 too, as long as there are two such tiles to a compute unit at most and four steps,
+// one for each wave (0: never). 4 bits, 24 heads, d = 128, on 256, 512, 1024 and 2048 keys: 64 rows 9.7, 13.6, 18.0, 19.9 us in tiles of 64 and 8.5, 10.0,
+// 12.9, 19.9 of 32; 500 rows on 512 and 1024 keys 19.3 and 29.9 in tiles of 128, 15.2 and 21.1 of 32; four times as many tiles 27 and 46.
+Plan plan_of(const CacheDims& c, const RowDims& r, int group, int list_len, int short_few = 0) {
   Plan p;
   const int G = r.heads / c.heads_kv;
   const int per = group > 0 && group < r.t ? group : r.t;
   const int64_t rows = (int64_t)per * G;
-  p.tiled = rows > 32;
-  p.qt = rows <= 16 || (rows > 32 && rows <= 64) ? 1 : 2;
+  const int64_t steps = (int64_t)(list_len > 0 && list_len < c.max_blocks ? list_len : c.max_blocks) * (c.blk / 64);
+  const int64_t of_32 = (int64_t)((r.t + per - 1) / per) * ((rows + 31) / 32) * c.batch * c.heads_kv;
+  p.tiled = rows > 32 && !(steps >= 4 && steps <= short_few && of_32 <= 2 * kCus);
+  p.qt = rows <= 16 || (p.tiled && rows <= 64) ? 1 : 2;
   p.grid.rows_per_tile = (p.tiled ? 64 : 16) * p.qt;
   p.grid.per_group = (int)((rows + p.grid.rows_per_tile - 1) / p.grid.rows_per_tile);
   p.grid.stored = (int)(rows < p.grid.rows_per_tile ? rows : p.grid.rows_per_tile);
   p.tiles = (int64_t)((r.t + per - 1) / per) * p.grid.per_group * c.batch * c.heads_kv;
-  const int64_t steps = (int64_t)(list_len > 0 && list_len < c.max_blocks ? list_len : c.max_blocks) * (c.blk / 64);
   int64_t best = 1;
   if (p.tiled) {
     // Rounds of workgroups over the slots (two to a compute unit, three at d = 64), the last one between what it fills and whole; what one
@@ -193,7 +197,7 @@ Plan plan_of(const CacheDims& c, const RowDims& r, int group, int list_len) {
   p.grid.splits = (int)(best < 1 ? 1 : best);
   // never more parts than without a limit on the lists: the workspace is sized for that
   if (steps < (int64_t)c.max_blocks * (c.blk / 64)) {
-    const int most = plan_of(c, r, group, 0).grid.splits;
+    const int most = plan_of(c, r, group, 0, short_few).grid.splits;
     if (p.grid.splits > most) p.grid.splits = most;
   }
   return p;

@@ -689,6 +689,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void fourbit_tile_kernel(Cach
   }
 }
 
+constexpr int kShortFew = 16;                      // steps up to which more than 32 rows go in tiles of 32 (plan_of)
 template <int D, int BLK>
 hipError_t launch_t(const CacheDims& c, const RowDims& r, const CacheAttnArgs& a, Plan p, hipStream_t s) {
   const dim3 grid((uint32_t)(p.tiles * p.grid.splits)), block(256);
@@ -707,17 +708,17 @@ hipError_t launch_t(const CacheDims& c, const RowDims& r, const CacheAttnArgs& a
 }  // namespace
 
 int64_t fourbit_attn_workgroups(const CacheDims& c, const RowDims& r, int group, int list_len) {
-  const Plan p = plan_of(c, r, group, list_len);
+  const Plan p = plan_of(c, r, group, list_len, kShortFew);
   return p.tiles * p.grid.splits;
 }
 
 size_t fourbit_attn_parts_bytes(const CacheDims& c, const RowDims& r, int group, int list_len) {
-  const Plan p = plan_of(c, r, group, list_len);
+  const Plan p = plan_of(c, r, group, list_len, kShortFew);
   return p.grid.splits == 1 ? 0 : (size_t)p.tiles * p.grid.splits * p.grid.stored * (c.d + 1) * sizeof(float);
 }
 
 hipError_t launch_fourbit_attn(const CacheDims& c, const RowDims& r, const CacheAttnArgs& a, hipStream_t s) {
-  Plan p = plan_of(c, r, a.block_idx ? a.group : 0, a.block_idx ? a.list_len : 0);
+  Plan p = plan_of(c, r, a.block_idx ? a.group : 0, a.block_idx ? a.list_len : 0, kShortFew);
   if (!a.parts) p.grid.splits = 1;
   if (c.d == 128) return c.blk == 128 ? launch_t<128, 128>(c, r, a, p, s) : launch_t<128, 64>(c, r, a, p, s);
   return c.blk == 128 ? launch_t<64, 128>(c, r, a, p, s) : launch_t<64, 64>(c, r, a, p, s);

@@ -58,12 +58,17 @@ def places(block, d):
 class Pair:
     """A 4-bit cache on the GPU and the oracle's, with the same table; pages that were not written hold 0xff everywhere."""
 
+    width = 0          # entries of a row of the table at least, the last ones empty (more than 32 rows are taken otherwise on a short one)
+
     def __init__(self, batch, hk, d, block, max_blocks, seed=0, table=None, pages=None):
         n = batch * max_blocks
         self.rng = np.random.default_rng(seed)
         if table is None:
             pages = pages or n + 2
             table = self.rng.permutation(pages)[:n].reshape(batch, max_blocks)
+        if max_blocks < self.width:
+            table = np.concatenate([np.asarray(table), np.full((batch, self.width - max_blocks), -1)], axis=1)
+            max_blocks = self.width
         self.gpu = rb.allocate_cache(batch, hk, d, block, pages, max_blocks, DEV, bits=4)
         self.gpu.k_codes.fill_(0xff)
         self.gpu.v_codes.fill_(0xff)
@@ -115,6 +120,16 @@ class Pair:
                 assert (code_k[~there] == 15).all() and (code_v[~there] == 15).all() and (e[~there] == 128).all() and (s[~there] == 0xffff0000).all()
                 np.testing.assert_array_equal(mean[page, h], p.mean)
                 assert scales[page, h].tolist() == [0.0, 0.0, 2.0 ** p.em, 0.0]
+
+
+@pytest.fixture
+def wide(request):
+    Pair.width = 20 if request.param else 0
+    yield
+    Pair.width = 0
+
+
+WIDE = pytest.mark.parametrize("wide", [False, True], indirect=True)
 
 
 def attend(pair, Q, kv_len, q_len=None, scale=0.0, causal=False, lists=None, group=0, layout="bhtd", ws=True, stream=None, list_len=0):
@@ -294,9 +309,10 @@ SHAPES = [  # d, block, G, t, lens, q_len, causal
 ]
 
 
+@WIDE
 @pytest.mark.parametrize("ws", [True, False])
 @pytest.mark.parametrize("d,block,G,t,lens,q_len,causal", SHAPES)
-def test_attention(d, block, G, t, lens, q_len, causal, ws):
+def test_attention(wide, d, block, G, t, lens, q_len, causal, ws):
     b = len(lens)
     p = Pair(b, 2, d, block, -(-max(lens) // block) + 1)
     p.fill(lens, spread=0.5)
@@ -304,11 +320,12 @@ def test_attention(d, block, G, t, lens, q_len, causal, ws):
     compare(*attend(p, Q, lens, q_len, causal=causal, layout="bthd" if t % 2 else "bhtd", ws=ws), d)
 
 
+@WIDE
 @pytest.mark.parametrize("ws", [True, False])
 @pytest.mark.parametrize("d,block,G,t,group,causal", [(64, 64, 1, 1, 1, True), (128, 64, 4, 1, 1, True), (128, 128, 3, 5, 1, True),
                                                       (128, 128, 1, 200, 128, False), (128, 64, 2, 90, 64, True), (64, 128, 1, 77, 20, True),
                                                       (128, 128, 1, 129, 1 << 30, False)])
-def test_attention_over_lists(d, block, G, t, group, causal, ws):
+def test_attention_over_lists(wide, d, block, G, t, group, causal, ws):
     p = Pair(2, 2, d, block, 9)
     lens = [9 * block - 5, 4 * block + max(0, t - 4 * block)]
     p.fill(lens)
@@ -321,7 +338,8 @@ def test_attention_over_lists(d, block, G, t, group, causal, ws):
     compare(*attend(p, Q, lens, q_len, causal=causal, lists=odd, group=min(group, t), ws=ws, list_len=70), d)   # longer than the table, too
 
 
-def test_attention_passes_over_what_is_no_page():
+@WIDE
+def test_attention_passes_over_what_is_no_page(wide):
     table = np.arange(20).reshape(2, 10)
     table[0, 3], table[0, 9], table[1, 0], table[1, 5] = -1, 1000, 77, -3
     p = Pair(2, 2, 128, 64, 10, table=table, pages=20)
@@ -337,8 +355,9 @@ def test_attention_passes_over_what_is_no_page():
 KINDS = [(64, 1, 1), (128, 1, 4), (128, 5, 4), (64, 40, 1), (128, 50, 1), (128, 70, 2)]
 
 
+@WIDE
 @pytest.mark.parametrize("d,t,G", [(128, 4, 2), (64, 4, 2), (128, 40, 1), (64, 40, 1), (128, 140, 1)])
-def test_nan_stays_with_the_rows_that_see_it(d, t, G):
+def test_nan_stays_with_the_rows_that_see_it(wide, d, t, G):
     """NaN among values and among keys of single tokens: causal rows before them are unharmed."""
     p = Pair(2, 1, d, 64, 4)
     K, V = p.rng.normal(size=(2, 2, 1, 200, d))
@@ -355,10 +374,11 @@ def test_nan_stays_with_the_rows_that_see_it(d, t, G):
     compare(*attend(p, Q, [198, 198 - t // 2], causal=False), d)              # behind the length: seen by nobody
 
 
+@WIDE
 @pytest.mark.parametrize("ws", [True, False])
 @pytest.mark.parametrize("by", [20, 60, 90])
 @pytest.mark.parametrize("d,t,G", KINDS)
-def test_values_of_very_different_size(d, t, G, by, ws):
+def test_values_of_very_different_size(wide, d, t, G, by, ws):
     """Every fourth block holds values 2^by times the others' and zeros in half of the channels; then none of its weight."""
     p = Pair(1, 1, d, 64, 16)
     n = 16 * 64
@@ -379,9 +399,10 @@ def test_values_of_very_different_size(d, t, G, by, ws):
     assert np.abs(O).max() < 4
 
 
+@WIDE
 @pytest.mark.parametrize("d,t,G", KINDS)
 @pytest.mark.parametrize("size", [2.0 ** 10, 2.0 ** 24, 2.0 ** 60, 2.0 ** 110])
-def test_scores_far_from_zero(size, d, t, G):
+def test_scores_far_from_zero(wide, size, d, t, G):
     """Whole scores of up to 6 * size, of both signs, a few of them equal: the greatest alone count from 2^24 on."""
     p = Pair(1, 1, d, 64, 6)
     n = 6 * 64
@@ -395,10 +416,11 @@ def test_scores_far_from_zero(size, d, t, G):
         compare(*attend(p, Q * sign, [n], scale=1.0), d)
 
 
+@WIDE
 @pytest.mark.parametrize("d,t,G", KINDS)
 @pytest.mark.parametrize("up", [True, False])
 @pytest.mark.parametrize("first", [22, 25, 26, 27, 28, 31])
-def test_scores_farther_apart_than_weights_reach(first, up, d, t, G):
+def test_scores_farther_apart_than_weights_reach(wide, first, up, d, t, G):
     """The greatest scores double from block to block, 3 * 2^first and on, up or down the cache: outputs are the mean of the two values whose keys
     are the greatest of all. A weight is rounded to 2^-8 of it, and so is the output."""
     p = Pair(1, 1, d, 64, 5)
@@ -420,9 +442,10 @@ def test_scores_farther_apart_than_weights_reach(first, up, d, t, G):
     assert (np.abs(O - two.mean(0)) <= 2.0 ** -7 * np.abs(two).mean(0) + 2.0 ** -100).all()
 
 
+@WIDE
 @pytest.mark.parametrize("d,t,G", KINDS)
 @pytest.mark.parametrize("keys", [1, 2, 3])
-def test_log_sum_exps_of_few_keys(keys, d, t, G):
+def test_log_sum_exps_of_few_keys(wide, keys, d, t, G):
     """Where next to nothing is summed the log-sum-exp is as exact as a score: 2^-21 and the scores' own bound."""
     p = Pair(24, 1, d, 64, 1, seed=keys)
     p.fill([keys] * 24)
@@ -434,10 +457,11 @@ def test_log_sum_exps_of_few_keys(keys, d, t, G):
             assert (O[b] == ref["O"][b]).all()
 
 
+@WIDE
 @pytest.mark.parametrize("d,t,G", KINDS)
 @pytest.mark.parametrize("up", [True, False])
 @pytest.mark.parametrize("gap,size", [(60, 99), (100, 9), (120, 40), (124, 9), (124, 99)])
-def test_large_values_of_small_weight(gap, size, up, d, t, G):
+def test_large_values_of_small_weight(wide, gap, size, up, d, t, G):
     """Half of the channels have values of 2^size in one block alone, whose scores are 2^-gap of the other's: before it and behind it."""
     p = Pair(1, 1, d, 64, 2)
     K, V = np.zeros((1, 1, 128, d)), p.rng.normal(size=(1, 1, 128, d))
@@ -457,8 +481,9 @@ def test_large_values_of_small_weight(gap, size, up, d, t, G):
         assert some[..., :d // 2].any() and (O[some] != 0).all()
 
 
+@WIDE
 @pytest.mark.parametrize("d,t,G", KINDS)
-def test_small_and_large_keys(d, t, G):
+def test_small_and_large_keys(wide, d, t, G):
     """Runs of channels 2^-100 .. 2^100 apart, each with a query that brings it back."""
     p = Pair(1, 1, d, 64, 4)
     e = np.repeat(p.rng.integers(-100, 101, size=d // 32), 32)
