@@ -441,7 +441,7 @@ typedef struct rsa_rotary {
   int32_t interleaved;   /* 0 or not */
   int32_t axes;          /* 1 .. 3 */
   int32_t axis_pairs[3]; /* >= 0, those of the axes add up to pairs */
-  float factor;          /* >= 0; 0 selects 1 */
+  float factor;          /* >= 0, finite; 0 selects 1 */
   const double* freq;    /* device, [pairs]: radians a position */
 } rsa_rotary;
 

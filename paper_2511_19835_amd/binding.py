@@ -8,6 +8,7 @@ tensors are not on the GPU the calls raise.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from dataclasses import dataclass
 from typing import Optional
@@ -582,6 +583,9 @@ class Rotary:
     freq: torch.Tensor         # fp64 [pairs], radians a position
 
     def __post_init__(self):
+        # (what rsa_rotary_apply refuses of the record, before a step has moved anything on; the factor as fp32 holds it)
+        if self.desc.pairs < 1 or not 0 <= self.desc.factor < math.inf:
+            raise ValueError(f"expect at least one pair and a finite factor of at least 0: got {self.desc.pairs} and {self.desc.factor}")
         self.device, self.dev, self.axes, self.refs = self.freq.device, self.freq.device.index, self.desc.axes, {}
 
     def ref(self, head_dim: int):
@@ -603,7 +607,9 @@ def make_rotary(freq: torch.Tensor, pairing: str = "half", axis_pairs=None, fact
     axis = list(axis_pairs) if axis_pairs is not None else [freq.shape[0]]
     if not 1 <= len(axis) <= 3 or sum(axis) != freq.shape[0] or min(axis) < 0:
         raise ValueError(f"pairs of up to three axes add up to {freq.shape[0]}: got {axis}")
-    return Rotary(rsa_rotary(0, freq.shape[0], int(pairing == "interleaved"), len(axis), (ctypes.c_int32 * 3)(*axis), float(factor), _ptr(freq)), freq)
+    rot = Rotary(rsa_rotary(0, freq.shape[0], int(pairing == "interleaved"), len(axis), (ctypes.c_int32 * 3)(*axis), float(factor), None), freq)
+    rot.desc.freq = _ptr(freq)
+    return rot
 
 
 def rsa_rotary_frequencies(pairs: int, base: float = 10000.0, scaling: int = RSA_ROTARY_PLAIN, stretch: float = 1.0, old_len: float = 0.0,

@@ -249,3 +249,17 @@ def test_binding_refuses_cpu_tensors_and_wrong_buffers(lib):
             rb.make_rotary(**bad)
     with pytest.raises(RuntimeError, match="device tensors only"):
         rb.make_rotary(f)
+
+
+def test_rotary_records_that_a_call_would_refuse_are_refused_when_they_are_made(lib):
+    """A step moves its lengths on before it turns anything, so a record that rsa_rotary_apply refuses must not get that far."""
+    f = torch.ones(8, dtype=torch.float64)
+    for bad in (dict(factor=-1.0), dict(factor=math.nan), dict(factor=math.inf), dict(factor=1e39), dict(freq=torch.ones(0, dtype=torch.float64))):
+        with pytest.raises(ValueError):
+            rb.make_rotary(**{**dict(freq=f), **bad})
+    record = lambda **kw: rb.rsa_rotary(**{**dict(head_dim=0, pairs=8, interleaved=0, axes=1, axis_pairs=(ctypes.c_int32 * 3)(8, 0, 0), factor=1.0, freq=ONE), **kw})
+    for bad in (dict(factor=-1.0), dict(factor=math.nan), dict(factor=1e39), dict(pairs=0)):
+        with pytest.raises(ValueError):
+            rb.Rotary(record(**bad), f)
+    for fine in (0.0, 1.2):
+        assert rb.Rotary(record(factor=fine), f).desc.factor == np.float32(fine)
