@@ -641,7 +641,7 @@ def serve_step(cache: KVCache, pages: Pages, rotary: Rotary, Q, K, V, O, kv_len,
     """One step of a batch of requests on one stream, with no host sync, so that it can be captured and replayed: sequence b brings add[b] new
     tokens (rows 0 .. add[b] - 1 of Q, K and V; less than 0: it is cut). Pages for them (rsa_cache_assign; kv_len and free_count move on in place,
     start and count say what was served), Q and K turned in place by their positions, keys and values into the cache, and the causal
-    attention of the new queries over their sequences. Rows of sequences that were not served are left as they were."""
+    attention of the new queries over their sequences. Rows of sequences that were not served are left as they were. Q, K and V must not overlap."""
     # (all of it before the first call: that one moves the lengths on)
     if (pages.table.data_ptr() != cache.table.data_ptr() or pages.desc.block != cache.desc.block or pages.batch != cache.batch
             or pages.desc.pages != cache.desc.pages):
@@ -657,8 +657,8 @@ def serve_step(cache: KVCache, pages: Pages, rotary: Rotary, Q, K, V, O, kv_len,
         raise ValueError("a step's tokens stand in a row: positions along one axis")
     write, attn = (rsa_fourbit_write, rsa_fourbit_attn) if cache.bits == 4 else (rsa_cache_write, rsa_cache_attn)
     at = [x.data_ptr() for x in (Q, K, V, O)]
-    if any(x % 16 for x in at) or at[0] == at[1]:
-        raise ValueError("queries, keys, values and outputs begin at multiples of 16 bytes, and queries are not the keys")
+    if any(x % 16 for x in at) or at[0] == at[1] or at[2] in at[:2]:
+        raise ValueError("queries, keys, values and outputs begin at multiples of 16 bytes, and queries, keys and values are three tensors")
     sizes = rsa_fourbit_workspace_bytes if cache.bits == 4 else lambda *x: rsa_cache_workspace_bytes(*x)[1]
     need, _ = sizes(cache, rows), sizes(cache, rows_kv)          # (strides that the calls do not take raise here)
     if ws is not None:

@@ -915,3 +915,43 @@ def test_binding_refusals():
     assert int(good["free_count"]) == 4 and good["kv_len"].tolist() == [0, 0] and (four.table == -1).all()
     rb.serve_step(**good)
     assert int(good["free_count"]) == 2 and good["kv_len"].tolist() == [3, 3]
+
+
+def step_of(batch, hq, hk, d, t, width=1, pages=4, strides=None):
+    """Arguments of a step that would be served: zeros, `t` new tokens for each sequence."""
+    def rows(h):
+        if strides is None:
+            return torch.zeros(batch, h, t, d, dtype=torch.bfloat16, device=DEV)
+        n = 1 + sum((m - 1) * s for m, s in zip((batch, h, t, d), strides))
+        return torch.zeros(n, dtype=torch.bfloat16, device=DEV).as_strided((batch, h, t, d), strides)
+    cache = rb.allocate_cache(batch, hk, d, 64, pages, width, DEV, bits=4)
+    n = lambda x: torch.full((batch,), x, dtype=torch.int32, device=DEV)
+    return dict(cache=cache, pages=rb.pages_of(cache.table, torch.arange(pages, dtype=torch.int32, device=DEV), 64),
+                rotary=rb.make_rotary(torch.ones(d // 2, dtype=torch.float64, device=DEV)), Q=rows(hq), K=rows(hk), V=rows(hk), O=rows(hq), kv_len=n(0), add=n(t),
+                free_count=i32([pages]), start=n(-9), count=n(-9))
+
+
+def refused(step, **bad):
+    """The step raises, and lengths, table and list are what they were."""
+    with pytest.raises((ValueError, RuntimeError)):
+        rb.serve_step(**{**step, **bad})
+    torch.cuda.synchronize()
+    assert int(step["free_count"]) == step["pages"].desc.pages and (step["kv_len"] == 0).all() and (step["cache"].table == -1).all() and (step["count"] == -9).all()
+
+
+def test_a_step_whose_values_are_its_keys_or_queries_is_refused():
+    """Queries and keys are turned where they stand, before the values are written."""
+    step = step_of(2, 2, 2, 64, 3)
+    refused(step, V=step["K"])
+    refused(step, V=step["Q"])
+    fused = torch.zeros(2, 3, 6, 64, dtype=torch.bfloat16, device=DEV).permute(0, 2, 1, 3)        # one product's rows: queries, keys, values of a token
+    Q, K, V = fused[:, :2], fused[:, 2:4], fused[:, 4:]
+    Q.copy_(bf16(np.random.default_rng(0).normal(size=(2, 2, 3, 64))))
+    K.copy_(Q)
+    V.copy_(Q)
+    rb.serve_step(**{**step, "Q": Q, "K": K, "V": V, "O": Q})
+    assert step["kv_len"].tolist() == [3, 3]
+    R, S = torch.zeros_like(step["K"]), torch.zeros_like(step["V"])
+    rb.rsa_fourbit_read(step["cache"], rb.make_rows(R), i32([0, 0]), None, R, S)
+    want = np.stack([so.stored(x, 64) for x in f64(V).reshape(-1, 64)]).reshape(2, 2, 3, 64)
+    np.testing.assert_array_equal(f64(S), want)                                  # as they came
