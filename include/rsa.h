@@ -463,7 +463,8 @@ int rsa_rotary_frequencies(int pairs, double base, int scaling, double stretch, 
  * Rows of Q and, in the same launch, of K (rows_k NULL: Q alone; other heads and strides, the same t): row i < count[b] of sequence b (NULL: all; rows
  * behind are left as they were) stands at positions[axis][b][i] (device int32 [axes][batch][t], any sign), or, where that is NULL and there
  * is one axis, at start[b] + i (start NULL: i). Qr and Kr have the strides of Q and K and may be Q and K; otherwise inputs and outputs must not
- * overlap. Channels that do not turn are copied. batch * heads * t < 2^28. Needs no workspace.
+ * overlap. Channels that do not turn are copied. batch * heads * t < 2^28 for Q and for K, batch * t * (head_dim / 8 + 2) < 2^29, 65535 heads of
+ * both at most (RSA_E_UNSUPPORTED). Needs no workspace.
  */
 int rsa_rotary_apply(const rsa_rotary* rotary, int batch, const rsa_rows* rows_q, const void* Q, void* Qr, const rsa_rows* rows_k,
                      const void* K, void* Kr, const int32_t* positions, const int32_t* start, const int32_t* count, int flags,

@@ -655,6 +655,8 @@ def serve_step(cache: KVCache, pages: Pages, rotary: Rotary, Q, K, V, O, kv_len,
         raise ValueError(f"{Q.shape[1]} and {K.shape[1]} heads of {cache.head_dim} channels, {rotary.desc.pairs} pairs: not for a cache of {cache.heads_kv} heads")
     if rotary.axes != 1:
         raise ValueError("a step's tokens stand in a row: positions along one axis")
+    if Q.shape[0] * Q.shape[2] * (cache.head_dim // 8 + 2) // 64 >= 1 << 23 or Q.shape[1] + K.shape[1] > 65535:
+        raise ValueError(f"{Q.shape[0]} times {Q.shape[2]} rows of {Q.shape[1]} and {K.shape[1]} heads are more than rsa_rotary_apply takes")
     write, attn = (rsa_fourbit_write, rsa_fourbit_attn) if cache.bits == 4 else (rsa_cache_write, rsa_cache_attn)
     at = [x.data_ptr() for x in (Q, K, V, O)]
     if any(x % 16 for x in at) or at[0] == at[1] or at[2] in at[:2]:

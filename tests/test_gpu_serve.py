@@ -955,3 +955,10 @@ def test_a_step_whose_values_are_its_keys_or_queries_is_refused():
     rb.rsa_fourbit_read(step["cache"], rb.make_rows(R), i32([0, 0]), None, R, S)
     want = np.stack([so.stored(x, 64) for x in f64(V).reshape(-1, 64)]).reshape(2, 2, 3, 64)
     np.testing.assert_array_equal(f64(S), want)                                  # as they came
+
+
+@pytest.mark.parametrize("sizes", [dict(batch=29128, hq=1, hk=1, d=128, t=1024, strides=(8, 8, 128, 1)),       # 29128 * 1024 * 18 / 64 >= 2^23 workgroups of the turning
+                                   dict(batch=1, hq=65535, hk=1, d=64, t=1)])                                  # 65536 heads of queries and keys
+def test_a_step_too_large_to_be_turned_is_refused(sizes):
+    """Sizes that pages and cache take, and rsa_rotary_apply does not: refused before the pages are given out."""
+    refused(step_of(**sizes))
