@@ -411,6 +411,8 @@ typedef struct rsa_pages {
  *   given back  where it gets shorter: its entries from ceil(new length / block) on become -1, and the pages that stood there go to the end of the
  *               free list, in the order of the sequences and their entries; not those of the first shared[b] entries (a prefix that others
  *               read too: device int32 [batch], NULL: none), and not entries that are no page. All of this comes before the first page is taken.
+ *               Where a sequence takes pages below shared[b], having been cut into its prefix, those are its own: shared[b] goes down
+ *               to the first of them, in place, so that they are given back in their turn.
  *   taken       entries from ceil(kv_len / block) to ceil(new length / block) get pages from the end of the free list, in the same order. A
  *               sequence is served if its new length fits the table and the list holds what all sequences up to it ask for (those that do
  *               not fit their table ask for none); one that needs no new page always is, if it fits. One that is not served stays as it is.
@@ -421,10 +423,10 @@ typedef struct rsa_pages {
  *                         the write calls and rsa_rotary_apply take them; count is the q_len of the attention
  *   positions [batch][t]  start + i for i < count, -1 behind     (NULL: not wanted)
  *   slots [batch][t]      int64, page * block + offset of each new token, -1 behind and where the entry is no page (NULL: not wanted)
- * table, free_pages, kv_new, free_left, start and count must not overlap each other or other arguments except as said (RSA_E_RANGE where two are
- * the same). batch * t < 2^28. Allocates nothing and needs no workspace; calls on the same buffers must not overlap in time.
+ * table, free_pages, shared, kv_new, free_left, start and count must not overlap each other or other arguments except as said (RSA_E_RANGE where two
+ * are the same). batch * t < 2^28. Allocates nothing and needs no workspace; calls on the same buffers must not overlap in time.
  */
-int rsa_cache_assign(const rsa_pages* pages, int t, const int32_t* kv_len, const int32_t* add, const int32_t* shared,
+int rsa_cache_assign(const rsa_pages* pages, int t, const int32_t* kv_len, const int32_t* add, int32_t* shared,
                      const int32_t* free_count, int32_t* kv_new, int32_t* free_left, int32_t* start, int32_t* count,
                      int32_t* positions, int64_t* slots, void* stream);
 

@@ -66,7 +66,8 @@ def _absolute(p):
 
 # ---- pages ---------------------------------------------------------------------------------------
 def assign(table, free_pages, free_count, kv_len, add, t, block, pages, shared=None):
-    """(table, free list as far as it is valid, new lengths, starts, counts, positions, slots); all as lists or int arrays."""
+    """(table, free list as far as it is valid, new lengths, starts, counts, positions, slots); all as lists or int arrays. The list `shared` goes
+    down in place where a sequence takes pages below it."""
     table = np.array(table)
     batch, width = table.shape
     free = list(free_pages[:max(0, min(int(free_count), pages))])
@@ -92,6 +93,8 @@ def assign(table, free_pages, free_count, kv_len, add, t, block, pages, shared=N
             continue
         for e in range(first, last):
             table[b, e] = free.pop()
+        if shared is not None and last > first:
+            shared[b] = min(shared[b], first)
         new[b], count[b] = held[b] + add[b], add[b]
         for i in range(add[b]):
             pos[b, i] = held[b] + i

@@ -151,6 +151,7 @@ __global__ __launch_bounds__(kMostThreads) void assign_kernel(AssignArgs a) {
       a.kv_new[b] = granted ? w.to : w.held;
       a.start[b] = add < 0 ? w.to : w.held;
       a.count[b] = n;
+      if (granted && more > 0 && a.shared && a.shared[b] > w.had) a.shared[b] = w.had;    // from here on the pages are its own
     }
     // Pages by whole waves, a sequence each, but for few pages to a sequence; a single new token finds its page on the way.
     const bool few = granted && more <= 4, many = granted && more > 4;

@@ -70,7 +70,7 @@ int rsa_fourbit_attn(const rsa_cache* cache, const rsa_rows* rows, const void* Q
   return rsa::launch_fourbit_attn(c, r, a, (hipStream_t)stream) == hipSuccess ? RSA_OK : RSA_E_LAUNCH;
 }
 
-int rsa_cache_assign(const rsa_pages* pages, int t, const int32_t* kv_len, const int32_t* add, const int32_t* shared,
+int rsa_cache_assign(const rsa_pages* pages, int t, const int32_t* kv_len, const int32_t* add, int32_t* shared,
                      const int32_t* free_count, int32_t* kv_new, int32_t* free_left, int32_t* start, int32_t* count,
                      int32_t* positions, int64_t* slots, void* stream) {
   if (!pages) return RSA_E_NULL;
@@ -84,15 +84,16 @@ int rsa_cache_assign(const rsa_pages* pages, int t, const int32_t* kv_len, const
     if (misaligned(p, 4)) return RSA_E_SHAPE;
   if (misaligned(slots, 8)) return RSA_E_SHAPE;
   // (in place: kv_new over kv_len, free_left over free_count; anything else would be read after it was written)
-  const void* out[] = {pages->table, pages->free_pages, kv_new, free_left, start, count};
+  const void* out[] = {pages->table, pages->free_pages, kv_new, free_left, start, count, shared};
   for (size_t i = 0; i < sizeof out / sizeof *out; ++i) {
+    if (!out[i]) continue;
     for (size_t j = 0; j < i; ++j)
       if (out[i] == out[j]) return RSA_E_RANGE;
-    if (out[i] == add || out[i] == positions || out[i] == slots || (shared && out[i] == shared) || (out[i] == kv_len && out[i] != kv_new) || (out[i] == free_count && out[i] != free_left))
+    if (out[i] == add || out[i] == positions || out[i] == slots || (out[i] == kv_len && out[i] != kv_new) || (out[i] == free_count && out[i] != free_left))
       return RSA_E_RANGE;
   }
-  for (const void* p : {(const void*)kv_len, (const void*)add, (const void*)shared, (const void*)free_count})
-    if (p && (p == positions || p == slots)) return RSA_E_RANGE;
+  for (const void* p : {(const void*)kv_len, (const void*)add, (const void*)free_count})
+    if (p == positions || p == slots) return RSA_E_RANGE;
   if (positions && (const void*)positions == (const void*)slots) return RSA_E_RANGE;
   rsa::AssignArgs a = {};
   a.batch = pages->batch;

@@ -9,8 +9,9 @@ struct AssignArgs {
   int batch, max_blocks, block, t;
   int64_t pages;
   int32_t *table, *free_pages;
-  const int32_t *kv_len, *add, *shared, *free_count;   // shared may be NULL (0)
+  const int32_t *kv_len, *add, *free_count;
   int32_t *kv_new, *free_left, *start, *count;
+  int32_t* shared;                                     // may be NULL (0)
   int32_t* positions;                                  // may be NULL
   int64_t* slots;                                      // may be NULL
 };

@@ -962,3 +962,52 @@ def test_a_step_whose_values_are_its_keys_or_queries_is_refused():
 def test_a_step_too_large_to_be_turned_is_refused(sizes):
     """Sizes that pages and cache take, and rsa_rotary_apply does not: refused before the pages are given out."""
     refused(step_of(**sizes))
+
+
+class Requests:
+    """Pages, lengths and shared prefixes on the GPU and in the oracle, moved on in place step by step."""
+
+    def __init__(self, table, free, kv, shared, block, pages, t):
+        dev = dict(dtype=torch.int32, device=DEV)
+        self.block, self.pages, self.t, self.batch = block, pages, t, len(kv)
+        self.table, self.free, self.kv, self.shared = np.array(table), list(free), list(kv), list(shared)
+        self.T, self.F = torch.tensor(np.asarray(table), **dev), torch.tensor(list(free) + [-77] * (pages - len(free)), **dev)
+        self.gkv, self.gsh, self.fc = i32(kv), i32(shared), i32([len(free)])
+        self.start, self.count = torch.zeros(self.batch, **dev), torch.zeros(self.batch, **dev)
+
+    def step(self, add):
+        rb.rsa_cache_assign(rb.pages_of(self.T, self.F, self.block), self.t, self.gkv, i32(add), self.fc, self.gkv, self.fc, self.start, self.count, shared=self.gsh)
+        self.table, self.free, self.kv, start, count, _, _ = so.assign(self.table, self.free, len(self.free), self.kv, add, self.t, self.block, self.pages, self.shared)
+        assert self.T.tolist() == self.table.tolist() and self.F[:int(self.fc)].tolist() == self.free and self.gkv.tolist() == self.kv
+        assert self.start.tolist() == start and self.count.tolist() == count and self.gsh.tolist() == self.shared
+        return count
+
+
+def test_pages_below_a_shared_prefix_come_back():
+    """Two sequences on a prefix of two pages; the second goes back to the first page, on, and back again."""
+    r = Requests([[0, 1, -1], [0, 1, 2]], [3, 4], [128, 192], [2, 2], 64, 5, 128)
+    r.step([0, -128])
+    assert sorted(r.free) == [2, 3, 4]
+    r.step([0, 128])
+    assert r.shared == [2, 1] and len(r.free) == 1
+    r.step([0, -128])
+    assert sorted(r.free) == [2, 3, 4] and r.table[0].tolist() == [0, 1, -1]
+
+
+@pytest.mark.parametrize("batch,t", [(3, 1), (5, 40), (200, 7), (1500, 3)])
+def test_no_page_is_lost_or_held_twice(batch, t):
+    """Sequences on two prefixes grow, are cut anywhere and grow again: every page is on the list, one sequence's or a prefix's."""
+    rng = np.random.default_rng(batch)
+    block, width, held = 4, 6, 3
+    pages = 2 * held + batch * 3
+    table, shared, kv = np.full((batch, width), -1), [], []
+    for b in range(batch):
+        n = int(rng.integers(0, held + 1))
+        table[b, :n] = np.arange(n) + b % 2 * held
+        shared.append(n)
+        kv.append(n * block)
+    r = Requests(table, rng.permutation(np.arange(2 * held, pages)).tolist(), kv, shared, block, pages, t)
+    for i in range(25):
+        r.step(np.where(rng.random(batch) < 0.3, -rng.integers(0, width * block, size=batch), rng.integers(0, t + 1, size=batch)).tolist())
+        own = [int(p) for b in range(batch) for e, p in enumerate(r.table[b]) if p >= 0 and e >= r.shared[b]]
+        assert sorted(own + r.free) == list(range(2 * held, pages))

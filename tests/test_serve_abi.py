@@ -263,3 +263,21 @@ def test_rotary_records_that_a_call_would_refuse_are_refused_when_they_are_made(
             rb.Rotary(record(**bad), f)
     for fine in (0.0, 1.2):
         assert rb.Rotary(record(factor=fine), f).desc.factor == np.float32(fine)
+
+
+def test_a_shared_prefix_over_other_arguments_is_refused(lib):
+    """It is written where pages are taken below it."""
+    pages = rb.rsa_pages(batch=2, max_blocks=4, block=64, pages=8, table=0x8000, free_pages=0x9000)
+    for at in range(0x1000, 0xc000, 0x1000):
+        args = [0x1000, 0x2000, at, 0x3000, 0x4000, 0x5000, 0x6000, 0x7000, 0xa000, 0xb000]
+        assert lib.rsa_cache_assign(ctypes.byref(pages), 1, *args, None) == -5, hex(at)
+    in_place = [0x1000, 0x2000, 0x1000, 0x3000, 0x1000, 0x3000, 0x6000, 0x7000, None, None]
+    assert lib.rsa_cache_assign(ctypes.byref(pages), 1, *in_place, None) == -5
+
+
+def test_pages_below_a_shared_prefix_are_the_sequences_own():
+    """Two sequences on a prefix of two pages; the second goes back to the first page, on, and back again: what it took comes back."""
+    table, free, kv, shared = [[0, 1, -1], [0, 1, 2]], [3, 4], [128, 192], [2, 2]
+    for add, want_free, want_shared, row in ((-128, [3, 4, 2], 2, [0, -1, -1]), (128, [3], 1, [0, 2, 4]), (-128, [3, 2, 4], 1, [0, -1, -1])):
+        table, free, kv, *_ = so.assign(table, free, len(free), kv, [0, add], 128, 64, 5, shared)
+        assert free == want_free and shared == [2, want_shared] and table.tolist()[1] == row
