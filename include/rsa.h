@@ -416,6 +416,8 @@ typedef struct rsa_pages {
  *   taken       entries from ceil(kv_len / block) to ceil(new length / block) get pages from the end of the free list, in the same order. A
  *               sequence is served if its new length fits the table and the list holds what all sequences up to it ask for (those that do
  *               not fit their table ask for none); one that needs no new page always is, if it fits. One that is not served stays as it is.
+ *               One that ends inside a block below shared[b] (cut there, or begun on a prefix that is no multiple of `block`) does not fit: its
+ *               tokens would go into a page that others read. Cut to a multiple of `block` it gets pages of its own from there on.
  * Outputs, all device int32 unless said:
  *   kv_new [batch]        the new lengths                   (may be kv_len)
  *   free_left [1]         entries of the list that are left  (may be free_count)

@@ -87,6 +87,8 @@ def assign(table, free_pages, free_count, kv_len, add, t, block, pages, shared=N
     for b in range(batch):
         if add[b] < 0 or held[b] + add[b] > width * block:
             continue
+        if shared is not None and add[b] > 0 and held[b] % block and held[b] // block < shared[b]:      # into a page of others
+            continue
         first, last = -(-held[b] // block), -(-(held[b] + add[b]) // block)
         asked += last - first
         if last > first and asked > have:

@@ -48,15 +48,16 @@ __device__ __forceinline__ int64_t prefix(int x, int* lds, int64_t* all) {
   return before + own;
 }
 
-struct Want { int held, to, had, need; bool fits; };   // tokens now and then, blocks now and then; fits: within the table
+struct Want { int held, to, had, need; bool fits; };   // tokens now and then, blocks now and then; fits: within the table, and in no page of others
 __device__ __forceinline__ Want want_of(const AssignArgs& a, int b) {
   Want w;
   const int64_t cap = (int64_t)a.max_blocks * a.block;
   w.held = (int)min((int64_t)max(a.kv_len[b], 0), cap);
   const int64_t to = (int64_t)w.held + min(a.add[b], a.t);
-  w.fits = to <= cap;
-  w.to = (int)(w.fits ? max(to, (int64_t)0) : w.held);
   w.had = (int)(((int64_t)w.held + a.block - 1) / a.block);
+  // (new tokens of a sequence that ends inside a block of its shared prefix would go into the page that others read)
+  w.fits = to <= cap && !(a.shared && to > w.held && (int64_t)w.had * a.block != w.held && w.had <= a.shared[b]);
+  w.to = (int)(w.fits ? max(to, (int64_t)0) : w.held);
   w.need = (int)(((int64_t)w.to + a.block - 1) / a.block);
   return w;
 }

@@ -1011,3 +1011,43 @@ def test_no_page_is_lost_or_held_twice(batch, t):
         r.step(np.where(rng.random(batch) < 0.3, -rng.integers(0, width * block, size=batch), rng.integers(0, t + 1, size=batch)).tolist())
         own = [int(p) for b in range(batch) for e, p in enumerate(r.table[b]) if p >= 0 and e >= r.shared[b]]
         assert sorted(own + r.free) == list(range(2 * held, pages))
+
+
+def test_no_token_goes_into_a_shared_page():
+    """Sequences that end inside a block of their prefix are not served and ask for no page; those behind them in the batch are."""
+    cases = [(70, 2), (64, 2), (128, 2), (130, 2), (70, 1), (1, 1), (0, 2), (70, -1), (100, 2)]
+    n = [-(-kv // 64) for kv, _ in cases]
+    table = [[10 * b + e if e < n[b] else -1 for e in range(4)] for b in range(len(cases))]
+    for t, add in ((1, 1), (80, 80), (80, 0), (80, -3)):
+        r = Requests(table, range(100, 120), [kv for kv, _ in cases], [s for _, s in cases], 64, 200, t)
+        count = r.step([add] * len(cases))
+        assert [c > 0 for c in count] == [add > 0 and b not in (0, 5, 8) for b in range(len(cases))]
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+def test_a_shared_prefix_stays_what_it_is(bits):
+    """Two sequences on a prefix of two pages, in a captured step: one is cut into its second page, asks for more, goes back to the border, grows."""
+    rng = np.random.default_rng(3)
+    cache = rb.allocate_cache(2, 1, 64, 64, 8, 4, DEV, bits=bits)
+    cache.table.copy_(torch.tensor([[0, 1, -1, -1], [0, 1, -1, -1]]))
+    rec = rb.pages_of(cache.table, torch.tensor([2, 3, 4, 5, 6, 7, 0, 0], dtype=torch.int32, device=DEV), 64)
+    K, V = (bf16(rng.normal(size=(2, 1, 128, 64))) for _ in range(2))
+    (rb.rsa_fourbit_write if bits == 4 else rb.rsa_cache_write)(cache, rb.make_rows(K), K, V, i32([0, 0]), i32([128, 0]))
+    before = [x[:2].clone() for x in (cache.k_codes, cache.v_codes, cache.scales, cache.k_mean)]
+    rot = rb.make_rotary(torch.ones(32, dtype=torch.float64, device=DEV))
+    kv, add, fc, shared, start, count = i32([128, 128]), i32([0, 0]), i32([6]), i32([2, 2]), i32([0, 0]), i32([0, 0])
+    Q, K, V, O = (bf16(rng.normal(size=(2, 1, 40, 64))) for _ in range(4))
+    step = lambda: rb.serve_step(cache, rec, rot, Q, K, V, O, kv, add, fc, start, count, shared=shared)
+    step()                                                        # (eagerly, of no token)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    # (adds, lengths, shared entries, pages left); the first sequence grows on its own pages beside it
+    for adds, lens, own, left in (([10, -50], [138, 78], [2, 2], 5), ([10, 40], [148, 78], [2, 2], 5), ([10, -14], [158, 64], [2, 2], 5), ([10, 40], [168, 104], [2, 1], 4),
+                                  ([10, 40], [178, 144], [2, 1], 3), ([-100, -144], [78, 0], [2, 1], 6), ([1, 40], [78, 40], [2, 0], 5)):
+        add.copy_(torch.tensor(adds))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (kv.tolist(), shared.tolist(), int(fc)) == (lens, own, left)
+        for x, y in zip((cache.k_codes, cache.v_codes, cache.scales, cache.k_mean), before):
+            assert torch.equal(x[:2], y)

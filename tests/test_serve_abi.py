@@ -281,3 +281,12 @@ def test_pages_below_a_shared_prefix_are_the_sequences_own():
     for add, want_free, want_shared, row in ((-128, [3, 4, 2], 2, [0, -1, -1]), (128, [3], 1, [0, 2, 4]), (-128, [3, 2, 4], 1, [0, -1, -1])):
         table, free, kv, *_ = so.assign(table, free, len(free), kv, [0, add], 128, 64, 5, shared)
         assert free == want_free and shared == [2, want_shared] and table.tolist()[1] == row
+
+
+def test_no_token_goes_into_a_shared_page():
+    """A sequence that ends inside a block of its prefix is not served; at the block's border, or with that block its own, it is."""
+    for kv, shared, served in ((70, 2, False), (64, 2, True), (128, 2, True), (130, 2, True), (70, 1, True), (1, 1, False), (0, 2, True), (70, -1, True)):
+        n = -(-kv // 64)
+        row = list(range(n)) + [-1] * (4 - n)
+        table, free, new, start, count, pos, slot = so.assign([row], [7, 8], 2, [kv], [1], 1, 64, 9, [shared])
+        assert (count, new) == (([1], [kv + 1]) if served else ([0], [kv])) and (served or (table.tolist() == [row] and free == [7, 8] and pos == [[-1]] and slot == [[-1]]))
