@@ -1,8 +1,9 @@
 // Rotary positions: each pair of channels turned by position * frequency, or (the gradient) turned back.
 //     y1 = f (x1 cos - x2 sin),  y2 = f (x1 sin + x2 cos)
-// The angle is taken in fp64 as turns, position * frequency / 2 pi, and only what is left of a whole turn goes on in fp32: far
-// positions lose nothing (in fp32 a position of 2^20 leaves 2^-4 radians). sine and cosine are the Taylor series on an eighth of a turn
-// to each side of the next quarter, off by less than 2^-23.
+// The angle is taken as turns, position * frequency / 2 pi, in fp64, with what the two products round away added to what is left of a whole turn:
+// 2^-26 of a turn up to 2^80 (in fp64 alone a position of 2^31 at a radian each leaves 2^-22 radians, in fp32 one of 2^20 2^-4). Only what is
+// left of a quarter goes on in fp32. sine and cosine are the Taylor series on an eighth of a turn to each side of the next quarter, off by less than
+// 2^-23 (9.2e-8 over four million angles on the host).
 //
 // A workgroup has 64 pieces, eight pairs of one token each: its four waves compute a quarter of the angles each, which go through LDS,
 // and then take every fourth head. Bound by memory: two bytes of each channel in and two out.
@@ -14,11 +15,14 @@
 namespace rsa {
 namespace {
 
-// cos and sin of 2 pi * turns.
-__device__ __forceinline__ void turn(double turns, float& co, float& si) {
-  const float f = (float)(turns - rint(turns));    // [-1/2, 1/2]
-  const float q = rintf(4.f * f);
-  const float y = (f - 0.25f * q) * 6.283185307179586f, z = y * y;      // |y| <= pi / 4; the difference is exact
+// cos and sin of pos * freq. (No contraction: a product that goes into a multiply-add brings along what `rest` adds.)
+__device__ __forceinline__ void turn(double pos, double freq, float& co, float& si) {
+#pragma clang fp contract(off)
+  constexpr double kTurn = 0.15915494309189535, kTurnRest = -9.839338337591243e-18;      // 1 / 2 pi in two parts
+  const double angle = pos * freq, angle_rest = fma(pos, freq, -angle);
+  const double turns = angle * kTurn, rest = fma(angle, kTurn, -turns) + fma(angle, kTurnRest, angle_rest * kTurn);
+  const double f = (turns - rint(turns)) + rest, q = rint(4. * f);
+  const float y = (float)(fma(-0.25, q, f) * 6.283185307179586), z = y * y;      // |y| <= pi / 4
   const float s = y * fmaf(z, fmaf(z, fmaf(z, fmaf(z, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), 1.f);
   const float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, 1.f / 40320.f, -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
   const int k = (int)q & 3;                        // quarters
@@ -80,7 +84,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int units, in
           const int axis = (j >= a.ends[0]) + (j >= a.ends[1]);
           pos = a.positions[((int64_t)axis * a.batch + b) * a.t + i];
         }
-        turn(pos * a.freq[j] * 0.15915494309189535, co, si);
+        turn(pos, a.freq[j], co, si);
         co *= a.factor;
         si *= a.inverse ? -a.factor : a.factor;
       }

@@ -1051,3 +1051,11 @@ def test_a_shared_prefix_stays_what_it_is(bits):
         assert (kv.tolist(), shared.tolist(), int(fc)) == (lens, own, left)
         for x, y in zip((cache.k_codes, cache.v_codes, cache.scales, cache.k_mean), before):
             assert torch.equal(x[:2], y)
+
+
+@pytest.mark.parametrize("far", [2 ** 31 - 40, -2 ** 31, 12345678])
+def test_rotary_many_radians_a_position(far):
+    """Frequencies of up to 1000 radians a position, so that angles reach 2^41, where a step of 64 bits is 2^-11 radians: what they round away counts."""
+    freq = 1000.0 ** (1 - np.arange(64) / 32)
+    run_rotary(np.random.default_rng(5), 1, 2, 2, 33, 128, 64, "half", start=[far], freq=freq)
+    run_rotary(np.random.default_rng(6), 1, 2, 2, 33, 64, 32, "interleaved", positions=far + np.arange(33).reshape(1, 1, 33), freq=freq[:32])
