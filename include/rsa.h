@@ -418,6 +418,8 @@ typedef struct rsa_pages {
  *               not fit their table ask for none); one that needs no new page always is, if it fits. One that is not served stays as it is.
  *               One that ends inside a block below shared[b] (cut there, or begun on a prefix that is no multiple of `block`) does not fit: its
  *               tokens would go into a page that others read. Cut to a multiple of `block` it gets pages of its own from there on.
+ * Codes, scales and means of the pages are not touched. A block that a cut leaves in part keeps the mean of what it held, by which rsa_cache_select
+ * ranks it, until the next write into it; so does a page that goes to another sequence, which is to be written before it is used.
  * Outputs, all device int32 unless said:
  *   kv_new [batch]        the new lengths                   (may be kv_len)
  *   free_left [1]         entries of the list that are left  (may be free_count)

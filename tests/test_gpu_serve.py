@@ -1059,3 +1059,41 @@ def test_rotary_many_radians_a_position(far):
     freq = 1000.0 ** (1 - np.arange(64) / 32)
     run_rotary(np.random.default_rng(5), 1, 2, 2, 33, 128, 64, "half", start=[far], freq=freq)
     run_rotary(np.random.default_rng(6), 1, 2, 2, 33, 64, 32, "interleaved", positions=far + np.arange(33).reshape(1, 1, 33), freq=freq[:32])
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("d,block", [(64, 64), (128, 128)])
+def test_means_after_a_cut_are_renewed_by_the_next_write(bits, d, block):
+    """A sequence is cut inside a block whose last tokens made its mean, grows by one token, and the selection ranks the block by what it holds now."""
+    rng = np.random.default_rng(bits)
+    width, hk = 6, 2
+    cache = rb.allocate_cache(2, hk, d, block, 12, width, DEV, bits=bits)
+    ref = (so.Cache if bits == 4 else co.Cache)(hk, d, block, np.full((2, width), -1), 12)
+    write = rb.rsa_fourbit_write if bits == 4 else rb.rsa_cache_write
+    t = 5 * block
+    rec = rb.pages_of(cache.table, torch.arange(12, dtype=torch.int32, device=DEV), block)
+    kv, fc, start, count = i32([0, 0]), i32([12]), i32([0, 0]), i32([0, 0])
+    table, free, held = np.full((2, width), -1), list(range(12)), [0, 0]
+    kept_blocks = []
+    for add in ([t, t - 3], [-block - 20, -block // 2], [1, 2], [1, 1]):
+        rb.rsa_cache_assign(rec, t, kv, i32(add), fc, kv, fc, start, count)
+        table, free, held, st, ct, _, _ = so.assign(table, free, len(free), held, add, t, block, 12)
+        assert kv.tolist() == held and cache.table.tolist() == table.tolist()
+        K, V = (rng.normal(size=(2, hk, t, d)) for _ in range(2))
+        for b in range(2):                                                    # the tokens that the cut takes point one way, and outweigh the block's others
+            K[b, :, max(0, held[b] - block - 20):, 0] += 60 if sum(ct) > 4 else 0
+        Kd, Vd = bf16(K), bf16(V)
+        write(cache, rb.make_rows(Kd), Kd, Vd, start, count)
+        ref.table = table
+        ref.write(f64(Kd), f64(Vd), st, ct)
+        if max(ct) == 0:
+            continue                                                          # (after the cut alone the means are those of before)
+        Q = np.zeros((2, hk, 1, d))
+        Q[..., 0] = 1
+        Q = bf16(Q + rng.normal(size=Q.shape) * 2.0 ** -4)
+        idx, kept = torch.zeros(2, hk, 1, 3, dtype=torch.int32, device=DEV), torch.zeros(2, hk, 1, dtype=torch.int32, device=DEV)
+        rb.rsa_cache_select(cache, rb.make_rows(Q), Q, kv, None, 1, 2, 0, 0, rb.RSA_CACHE_CAUSAL, idx, kept)
+        for (b, h, g), x in ref.select(f64(Q), held, None, 1, 2, 0, 0, True).items():
+            assert int(kept[b, h, g]) == len(x) and idx[b, h, g].tolist() == x + [-1] * (3 - len(x))
+            kept_blocks.append((sum(ct) > 4, (held[b] - 1) // block in x))
+    assert all(last for many, last in kept_blocks if many) and not all(last for many, last in kept_blocks if not many)
