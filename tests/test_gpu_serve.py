@@ -1097,3 +1097,19 @@ def test_means_after_a_cut_are_renewed_by_the_next_write(bits, d, block):
             assert int(kept[b, h, g]) == len(x) and idx[b, h, g].tolist() == x + [-1] * (3 - len(x))
             kept_blocks.append((sum(ct) > 4, (held[b] - 1) // block in x))
     assert all(last for many, last in kept_blocks if many) and not all(last for many, last in kept_blocks if not many)
+
+
+@pytest.mark.parametrize("d,block,ws", [(64, 64, True), (128, 128, False)])
+def test_causal_prompts_of_many_tiles(d, block, ws):
+    """More workgroups than the chip takes at once, so that the last tokens go first: outputs and log-sum-exps of the first, middle and last tiles."""
+    hk, G, t, n = 2, 8, 4120, 4200
+    p = Pair(1, hk, d, block, -(-n // block))
+    p.fill([n], spread=0.3)
+    Q = bf16(video_like(p.rng, 1, hk * G, t, d))
+    assert hk * -(-t * G // 128) > 2 * 256                         # tiles of 128 rows and compute units, twice
+    O, lse, rows = torch.full_like(Q, 7.0), torch.full(Q.shape[:3], 7.0, device=DEV), rb.make_rows(Q)
+    scratch = torch.empty(max(256, rb.rsa_fourbit_workspace_bytes(p.gpu, rows)), dtype=torch.uint8, device=DEV) if ws else None
+    rb.rsa_fourbit_attn(p.gpu, rows, Q, i32([n]), None, 0.0, rb.RSA_CACHE_CAUSAL, None, None, 0, O, lse, scratch)
+    for i in (0, 1, 15, 16, 17, t // 2 - 1, t // 2, t - 25, t - 24, t - 9, t - 8, t - 1):
+        ref = p.ref.attend(f64(Q[:, :, i:i + 1]), [n - t + i + 1], None, 0.0, False)
+        compare(f64(O[:, :, i:i + 1]), lse[:, :, i:i + 1].cpu().double().numpy(), ref, d)
