@@ -438,7 +438,7 @@ int rsa_cache_assign(const rsa_pages* pages, int t, const int32_t* kv_len, const
  * Rotary positions. Pair j < pairs of a head's channels (2 j and 2 j + 1 if interleaved, j and pairs + j if not; channels from 2 pairs on
  * are left out) is turned by the angle position * freq[j]:
  *   y1 = factor (x1 cos - x2 sin),  y2 = factor (x1 sin + x2 cos)
- * in fp32, rounded once to bf16; the angle is reduced in fp64. With several axes (time, height, width) the first axis_pairs[0]
+ * in fp32, rounded once to bf16; the angle is reduced in fp64 with the rests of its products. With several axes (time, height, width) the first axis_pairs[0]
  * pairs turn by the position along axis 0, and so on.
  */
 typedef struct rsa_rotary {

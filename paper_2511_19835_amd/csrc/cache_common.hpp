@@ -1,6 +1,7 @@
-// Shared declarations of the translation units of the 8-bit key/value cache (gfx950 only).
+// Shared declarations of the translation units of the key/value cache (gfx950 only): records, pages, spans and lane exchanges of the caches of 8 and of 4
+// bits, launchers of the first (those of the second and the order of its pages are in fourbit_common.hpp).
 //
-// A page holds one block of BLK tokens of every key/value head. Inside (page, head) the e4m3 codes stand in the order in
+// A page holds one block of BLK tokens of every key/value head. In 8 bits, inside (page, head) the e4m3 codes stand in the order in
 // which the 16x16x32 matrix instructions of cache_attn_kernels.hip take them, so that a wave loads 1 KB in one piece and
 // lane L finds its operands in its 16 bytes:
 //   K  [BLK/16][d/64][g 0..3][key 0..15][16 channels]     lane 16 g + key: row `key`, channels 16 g .. 16 g + 15 of 64

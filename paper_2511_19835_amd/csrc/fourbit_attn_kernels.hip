@@ -8,8 +8,9 @@
 // keys, summed in fp32; a value's code is widened alone, and its token's scale goes into P.
 //
 // P in bf16: half a step is 2^-8 of a weight, and a scale only moves its exponent, whatever the scales of the tokens are to each other, so no
-// running scale of the outputs is needed. Few rows, which wait for memory, take what the rounding leaves of it as a second product (2^-16 remains). The
-// running reference m of a row is moved only when the weights of a step have become large beside it, so most steps take no maximum.
+// running scale of the outputs is needed. Few rows, which wait for memory, take what the rounding leaves of it as a second product (2^-15 of a weight
+// remains at most). The running reference m of a row is moved only when a lane's 16 weights of a step have become large beside it, so most steps take no
+// maximum.
 #include "fourbit_common.hpp"
 
 #include "cache_attn_common.hpp"
@@ -95,7 +96,8 @@ __device__ __forceinline__ bool weigh_row(const floatx4 (&s)[4], float ks, float
   return sum > 0x1p15f;                            // 2^(8 + kBias)
 }
 // The reference goes up to the row's largest score, where that is larger -> what is to be taken of what was summed over the old one (0 from 2^-126
-// down). The same in the four lanes of a column. (The score itself, so that the weight of a key that outweighs the others is 1, and exact in bf16.)
+// down). The same in the four lanes of a column. (The score itself, so that the weight of the key that moves it is 1, exact in bf16; one that outweighs the
+// others by less than it takes to move the reference is rounded like any other.)
 __device__ __forceinline__ float move_row(const floatx4 (&s)[4], float ks, float& m) {
   float mx = -INFINITY;
 #pragma unroll
@@ -356,7 +358,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void fourbit_attn_kernel(
     }
   }
 
-  // join the four waves, 16 rows at a time
+  // join the waves, 16 rows at a time
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
     const float sum = ldexpf(__builtin_bit_cast(float, with_xor32(with_xor16(__builtin_bit_cast(int, l[x]), AddF32()), AddF32())), -(int)kBias);
@@ -408,12 +410,13 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void fourbit_attn_kernel(
 // The same for many query rows. 64 QT rows to a workgroup, 16 QT to a wave: every wave needs all codes, so they are widened once for
 // the workgroup, a quarter by each wave, into LDS in the order of the operands. Two buffers, one barrier a step of 64 keys; codes are requested
 // two steps ahead and widened between the softmax and the products of the values.
-// 24 heads, 1560 tokens on 20 280 keys: 360 us and 12.6 of joining, 1040 TFLOP/s (a library product 1219); the matrix pipe is busy 50 % of the
-// time, the vector ALU 58 %, LDS 40 %. Scores of the next step beside this one's weights 456 us, each wave widening for itself without LDS
+// 24 heads, 1560 tokens on 20 280 keys, repeated: 360 us and 12.6 of joining, 1040 TFLOP/s (a library product 1219; on another box 1056 and 1404, and 897
+// after a pause of 0.2 s); the matrix pipe is busy 50 % of the time, the vector ALU 58 %, LDS 40 %. Scores of the next step beside this one's weights 456 us, each wave widening for itself without LDS
 // 417, two groups of waves a phase apart 486, products of 32x32x16 421 (against 383 to 392 of the form of the day).
 // 64 rows (56 us where 32 rows take 36): neither half the LDS reads, nor eight waves, nor four steps ahead are faster.
 // Three workgroups to a compute unit at d = 64, two at d = 128. us with two and three:
-// 128 rows of 16 x 8 heads on 8192 keys 63, 58; 1000 rows 343, 310; 1000 rows of 12 heads on 30 000 keys 137, 124.
+// 128 rows of 16 x 8 heads on 8192 keys 63, 58; 1000 rows 343, 310 (866 TFLOP/s); 1000 rows of 12 heads on 30 000 keys 137, 124 (743 TFLOP/s); the
+// last two on another box 323 and 139.
 constexpr int kAhead = 256;                        // steps that are looked up together
 template <int D, int BLK, int QT>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void fourbit_tile_kernel(CacheDims c, RowDims r, CacheAttnArgs a, TileGrid tg) {
