@@ -639,7 +639,7 @@ def rsa_rotary_apply(rotary: Rotary, rows_q, Q, Qr, rows_k=None, K=None, Kr=None
 def serve_step(cache: KVCache, pages: Pages, rotary: Rotary, Q, K, V, O, kv_len, add, free_count, start, count, positions=None, slots=None, shared=None,
                lse=None, ws=None, stream=None):
     """One step of a batch of requests on one stream, with no host sync, so that it can be captured and replayed: sequence b brings add[b] new
-    tokens (rows 0 .. add[b] - 1 of Q, K and V; less than 0: it is cut). Pages for them (rsa_cache_assign; kv_len and free_count move on in place,
+    tokens (rows 0 .. add[b] - 1 of Q, K and V; less than 0: it is cut). Pages for them (rsa_cache_assign; kv_len, free_count and shared move on in place,
     start and count say what was served), Q and K turned in place by their positions, keys and values into the cache, and the causal
     attention of the new queries over their sequences. Rows of sequences that were not served are left as they were. Q, K and V must not overlap.
     ws: bytes of the attention's workspace (rsa_fourbit_workspace_bytes, or the second of rsa_cache_workspace_bytes); None: the keys of a tile are not
